@@ -294,6 +294,82 @@ int sprinter_set_tau(sprinter_ctx* ctx, float tau);
  * host_target_calls, if not NULL, receives the per-row number of target calls [B]. */
 int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* host_target_calls);
 
+/* ---- operators of expert models and of norms around a block --------------------------------------------------
+ * The pieces of a decoder block whose feed-forward part is a set of experts, each callable by itself on device
+ * arrays and a stream; a context made by sprinter_create_blocks runs the same kernels inside its forward passes.
+ * They enqueue work on hip_stream of the current device and wait for nothing; pointers are device memory (the
+ * configurations are host memory), dtype is SPRINTER_F32 or SPRINTER_BF16, a row stride (ld_*) counts elements.
+ * No call keeps anything between calls, so two calls may run at once when their outputs and workspaces differ, and
+ * all of them can be recorded into a HIP graph.  Errors as above, with the text in sprinter_last_error(NULL); a call
+ * that is refused enqueues nothing. */
+
+enum { SPRINTER_SCORE_SOFTMAX = 0, SPRINTER_SCORE_SIGMOID = 1 };
+enum { SPRINTER_GROUP_MAX = 0, SPRINTER_GROUP_BEST_TWO = 1 };
+enum { SPRINTER_NORM_LAYER = 0, SPRINTER_NORM_RMS = 1 };
+
+/* Routing of a row: scores p = softmax(logits) or sigmoid(logits), keys p + bias (the bias only decides who is taken).
+ *   n_group     1: no groups; else the experts form n_group runs of n_expert / n_group, and only those of the
+ *               top_group runs with the largest key (SPRINTER_GROUP_MAX) or the largest sum of their two best keys
+ *               (SPRINTER_GROUP_BEST_TWO) can be taken
+ *   top_k       experts taken, largest key first, equal keys by index
+ *   renormalize 1: the weights are p / (sum of the taken p); 0: p itself.  Either times scale.
+ *   n_shared    appends the ids n_expert, n_expert + 1, ... with a weight of 1 (shared experts behind the routed ones)
+ * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16. */
+typedef struct {
+  int32_t n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared;
+  float scale;
+} sprinter_route_cfg;
+
+/* ids and weights [n_rows, top_k + n_shared] of logits [n_rows, n_expert] (float32; rows ld_logits apart).  dev_bias
+ * [n_expert] or NULL.  An expert whose logit is -inf or NaN is never taken; where fewer than top_k are left (a row may
+ * have none) the remaining ids are -1 with weight 0.  Scores, keys and their sums are held in 64 bits. */
+int sprinter_route(const sprinter_route_cfg* cfg, const float* dev_logits, int64_t ld_logits, const float* dev_bias,
+                   int n_rows, int32_t* dev_ids, float* dev_weights, void* hip_stream);
+
+/* A set of experts, each y = W2 (silu(Wg x) * (Wu x)) with Wg, Wu [d_ff, d_model] and W2 [d_model, d_ff].  d_model and
+ * d_ff are multiples of 8 up to 8192 and 65536, n_expert up to 1024 (shared experts counted in). */
+typedef struct {
+  int32_t dtype, n_expert, d_model, d_ff;
+} sprinter_experts_cfg;
+
+/* Bytes of the packed form of each of the three weight arrays (bf16; 0 in float32 mode, which reads them as they are)
+ * and of the workspace of calls of up to max_rows rows with up to top_k ids each.  out pointers may be NULL. */
+int sprinter_experts_bytes(const sprinter_experts_cfg* cfg, int max_rows, int top_k, size_t* out_packed_up,
+                           size_t* out_packed_down, size_t* out_workspace);
+
+/* bf16: brings one array (down 0: Wg or Wu [n_expert, d_ff, d_model], 1: W2 [n_expert, d_model, d_ff]) into the layout
+ * that sprinter_experts reads: float16 operand tiles, as sprinter_load_weights makes them. */
+int sprinter_experts_pack(const sprinter_experts_cfg* cfg, int down, const void* dev_weights, void* dev_packed,
+                          void* hip_stream);
+
+/* y[t] = sum over j < top_k of dev_route_weights[t, j] * expert dev_ids[t, j] (x[t]), t < n_rows; ids and weights are
+ * [n_rows, top_k] as sprinter_route writes them.  An id outside [0, n_expert) adds nothing (padding, experts of another
+ * device); a row without any gives zeros; an expert that is named twice counts twice.  x and y have cfg->dtype, rows 16-byte aligned (ld_x, ld_y);
+ * rows of y from n_rows on are not written.  The three weight arrays: packed (bf16) or row-major (float32), 16-byte
+ * aligned.  Arithmetic of bf16: float16 operands (x and silu(..) * .. above 65504 become infinite), float32 sums.
+ * n_rows * top_k is at most 2^20, top_k at most 64; the result does not depend on the rows beside a row nor on the
+ * run.  dev_workspace: at least sprinter_experts_bytes for n_rows, 256-byte aligned, in use until the call's work is
+ * done. */
+int sprinter_experts(const sprinter_experts_cfg* cfg, const void* dev_gate, const void* dev_up, const void* dev_down,
+                     const void* dev_x, int64_t ld_x, const int32_t* dev_ids, const float* dev_route_weights,
+                     int n_rows, int top_k, void* dev_y, int64_t ld_y, void* dev_workspace, size_t workspace_bytes,
+                     void* hip_stream);
+
+/* The norms around a block, with the block's gate and residual scale:
+ *   u = norm(y) (post_gain, post_offset; post_gain NULL: y itself);  h_out = h + scale * gate * u;
+ *   out = norm(h_out) (gain, offset), what the next block reads.
+ * norm is LayerNorm or RMSNorm over d columns (1 to 16384) with eps; offsets may be NULL.  gate [i * gate_row + c * gate_col] is float32
+ * (NULL: 1): a gain per column (strides 0, 1), a weight per row (1, 0), or one for each element.  h and h_out are float32 (h_out may be
+ * h itself), y and out have cfg->dtype. */
+typedef struct {
+  int32_t dtype, kind, d;
+  float eps, scale;
+} sprinter_block_norm_cfg;
+int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, int64_t ld_h, const void* dev_y,
+                        int64_t ld_y, const float* dev_post_gain, const float* dev_post_offset, const float* dev_gate,
+                        int64_t gate_row, int64_t gate_col, const float* dev_gain, const float* dev_offset, int n_rows,
+                        float* dev_h_out, int64_t ld_h_out, void* dev_out, int64_t ld_out, void* hip_stream);
+
 /* Waits for the stream, frees the context and its pinned word; the workspace stays with the caller. */
 void sprinter_destroy(sprinter_ctx* ctx);
 

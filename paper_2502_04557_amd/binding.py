@@ -18,6 +18,7 @@ F32, BF16 = 0, 1
 
 EXPORTS = ("sprinter_workspace_bytes", "sprinter_create", "sprinter_create_static", "sprinter_load_weights", "sprinter_prefill",
            "sprinter_step", "sprinter_generate", "sprinter_sd_generate", "sprinter_set_tau", "sprinter_get_stats",
+           "sprinter_route", "sprinter_experts_bytes", "sprinter_experts_pack", "sprinter_experts", "sprinter_block_norm",
            "sprinter_destroy", "sprinter_last_error")
 
 
@@ -66,6 +67,12 @@ def load_library(path: str = LIB_PATH):
     lib.sprinter_sd_generate.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp]
     lib.sprinter_set_tau.argtypes = [vp, C.c_float]
     lib.sprinter_get_stats.argtypes = [vp, C.POINTER(StatsC), C.POINTER(C.c_int64)]
+    i64, psz = C.c_int64, C.POINTER(sz)
+    lib.sprinter_route.argtypes = [vp, vp, i64, vp, i32, vp, vp, vp]
+    lib.sprinter_experts_bytes.argtypes = [vp, i32, i32, psz, psz, psz]
+    lib.sprinter_experts_pack.argtypes = [vp, i32, vp, vp, vp]
+    lib.sprinter_experts.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, i32, i32, vp, i64, vp, sz, vp]
+    lib.sprinter_block_norm.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, i64, vp, i64, vp]
     lib.sprinter_destroy.argtypes = [vp]
     lib.sprinter_destroy.restype = None
     lib.sprinter_last_error.argtypes = [vp]

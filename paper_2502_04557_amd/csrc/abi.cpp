@@ -3,6 +3,7 @@
 // All device work is issued through the launchers in the k_*.hip files.
 #include "../../include/sprinter.h"
 #include "internal.h"
+#include "ops.h"
 
 #include <cstdarg>
 #include <cstdio>
@@ -125,6 +126,18 @@ int fail(sprinter_ctx* ctx, int code, const char* fmt, ...) {
   snprintf(g_err, sizeof g_err, "%s", buf);
   return code;
 }
+
+}  // namespace
+
+int sprinter::op_fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+namespace {
 
 int rows_alloc_for(int max_batch) {
   if (max_batch <= 16) return 16;

@@ -1,0 +1,194 @@
+"""The operators of include/sprinter.h on torch tensors: routing to experts, the experts' products, the norms around a block.
+
+Argument marshalling only; every call runs the library's HIP kernels on the device and the current stream of its tensors, allocates its
+outputs (and workspace) through torch and waits for nothing.  What the library refuses raises SprinterError, what is no tensor of the
+right type, shape or device ValueError.  There are no gradients: a tensor that asks for one is refused.
+"""
+from __future__ import annotations
+import ctypes as C
+from functools import lru_cache
+import torch
+
+from .binding import F32, BF16, SprinterError, load_library
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORES = {"max": 0, "sum2": 1}
+NORMS = {"layer": 0, "rms": 1}
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class RouteCfgC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_expert", "top_k", "score", "n_group", "top_group", "group_score", "renormalize",
+                                         "n_shared")] + [("scale", C.c_float)]
+
+
+class ExpertsCfgC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_expert", "d_model", "d_ff")]
+
+
+class BlockNormCfgC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "kind", "d")] + [("eps", C.c_float), ("scale", C.c_float)]
+
+
+def _call(name, device, *args):
+    """One entry point on `device` and its current stream (the last argument of them all)."""
+    lib = load_library()
+    fn = getattr(lib, name)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != 0:
+        raise SprinterError(rc, lib.sprinter_last_error(None).decode())
+
+
+def _tensor(name, t, device, dtype, shape, contiguous=False):
+    """Checks one argument: shape with None for any size; rows may lie apart unless contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
+    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: gradients are not computed here; detach it")
+    if contiguous:
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: not contiguous")
+    elif t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of a row are not adjacent")
+
+
+def _device(t, name):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name}: a tensor on a GPU is needed")
+    return t.device
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+@lru_cache(maxsize=256)
+def _route_cfg(n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale):
+    if score not in SCORES or group_score not in GROUP_SCORES:
+        raise ValueError(f"score is one of {tuple(SCORES)}, group_score one of {tuple(GROUP_SCORES)}")
+    c = RouteCfgC(n_expert, top_k, SCORES[score], n_group, top_group, GROUP_SCORES[group_score], bool(renormalize), n_shared, scale)
+    return c, C.byref(c)
+
+
+def route(logits, top_k, *, score="softmax", bias=None, n_group=1, top_group=1, group_score="max", renormalize=True, scale=1.0,
+          n_shared=0):
+    """logits [T, E] float32 -> (ids int32, weights float32), both [T, top_k + n_shared] (sprinter_route)."""
+    dev = _device(logits, "logits")
+    _tensor("logits", logits, dev, torch.float32, (None, None))
+    T, E = logits.shape
+    if bias is not None:
+        _tensor("bias", bias, dev, torch.float32, (E,), True)
+    cfg = _route_cfg(E, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale)
+    n = max(0, top_k + n_shared)
+    ids = torch.empty(T, n, dtype=torch.int32, device=dev)
+    weights = torch.empty(T, n, dtype=torch.float32, device=dev)
+    _call("sprinter_route", dev, cfg[1], logits.data_ptr(), logits.stride(0), _ptr(bias), T, ids.data_ptr(), weights.data_ptr())
+    return ids, weights
+
+
+class Experts:
+    """A set of experts on one device: gate, up [E, d_ff, d_model], down [E, d_model, d_ff], bfloat16 or float32.
+
+    bfloat16 weights are laid out once here (on the current stream) and may go afterwards; float32 ones are kept and read as they are."""
+
+    def __init__(self, gate, up, down):
+        dev = _device(gate, "gate")
+        if gate.dtype not in DTYPES or gate.dim() != 3:
+            raise ValueError("gate: bfloat16 or float32 [n_expert, d_ff, d_model] is needed")
+        E, ff, d = gate.shape
+        for name, t, shape in (("gate", gate, (E, ff, d)), ("up", up, (E, ff, d)), ("down", down, (E, d, ff))):
+            _tensor(name, t, dev, gate.dtype, shape, True)
+        self.device, self.dtype = dev, gate.dtype
+        self.n_expert, self.d_ff, self.d_model = E, ff, d
+        self._cfg = ExpertsCfgC(DTYPES[gate.dtype], E, d, ff)
+        self._ref = C.byref(self._cfg)
+        self._need = {}
+        n_up, n_down, _ = self._bytes(0, 1)
+        if gate.dtype == torch.float32:
+            self._weights = (gate, up, down)
+        else:
+            self._weights = tuple(torch.empty(n, dtype=torch.uint8, device=dev) for n in (n_up, n_up, n_down))
+            for i, t in enumerate((gate, up, down)):
+                _call("sprinter_experts_pack", dev, self._ref, int(i == 2), t.data_ptr(), self._weights[i].data_ptr())
+        self._ptrs = tuple(t.data_ptr() for t in self._weights)
+
+    def _bytes(self, rows, top_k):
+        n = self._need.get((rows, top_k))
+        if n is None:
+            lib = load_library()
+            v = [C.c_size_t(0) for _ in range(3)]
+            rc = lib.sprinter_experts_bytes(self._ref, rows, top_k, *(C.byref(x) for x in v))
+            if rc:
+                raise SprinterError(rc, lib.sprinter_last_error(None).decode())
+            if len(self._need) >= 4096:
+                self._need.clear()
+            n = self._need[rows, top_k] = tuple(x.value for x in v)
+        return n
+
+    def __call__(self, x, ids, weights, out=None):
+        """x [T, d_model] -> y [T, d_model] of its type; ids int32, weights float32 [T, top_k] as `route` gives them (sprinter_experts)."""
+        dev = self.device
+        _tensor("x", x, dev, self.dtype, (None, self.d_model))
+        T = x.shape[0]
+        _tensor("ids", ids, dev, torch.int32, (T, None), True)
+        k = ids.shape[1]
+        _tensor("weights", weights, dev, torch.float32, (T, k), True)
+        if out is None:
+            out = torch.empty(T, self.d_model, dtype=self.dtype, device=dev)
+        else:
+            _tensor("out", out, dev, self.dtype, (T, self.d_model))
+        need = self._bytes(T, k)[2]
+        work = torch.empty(need, dtype=torch.uint8, device=dev)
+        _call("sprinter_experts", dev, self._ref, *self._ptrs, x.data_ptr(), x.stride(0), ids.data_ptr(), weights.data_ptr(), T, k,
+              out.data_ptr(), out.stride(0), work.data_ptr(), need)
+        return out
+
+
+@lru_cache(maxsize=256)
+def _norm_cfg(dtype, kind, d, eps, scale):
+    if dtype not in DTYPES or kind not in NORMS:
+        raise ValueError(f"y is bfloat16 or float32, kind one of {tuple(NORMS)}")
+    c = BlockNormCfgC(DTYPES[dtype], NORMS[kind], d, eps, scale)
+    return c, C.byref(c)
+
+
+def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gate=None, scale=1.0, eps=1e-5, kind="rms", h_out=None):
+    """u = norm(y) (or y without post_gain), h' = h + scale * gate * u, out = norm(h') -> (h', out) (sprinter_block_norm).
+
+    h [T, d] float32, y [T, d] bfloat16 or float32; gate float32 of any shape that broadcasts to [T, d].  h_out: where h' goes (h itself
+    updates it in place); by default a new tensor."""
+    dev = _device(h, "h")
+    _tensor("h", h, dev, torch.float32, (None, None))
+    T, d = h.shape
+    if not isinstance(y, torch.Tensor):
+        raise ValueError("y: a tensor is needed")
+    cfg = _norm_cfg(y.dtype, kind, d, eps, scale)
+    _tensor("y", y, dev, y.dtype, (T, d))
+    for name, t in (("gain", gain), ("offset", offset), ("post_gain", post_gain), ("post_offset", post_offset)):
+        if t is not None or name == "gain":
+            _tensor(name, t, dev, torch.float32, (d,), True)
+    gate_row = gate_col = 0
+    if gate is not None:
+        if not isinstance(gate, torch.Tensor) or gate.dtype != torch.float32 or gate.device != dev:
+            raise ValueError(f"gate: a float32 tensor on {dev} is needed")
+        if gate.requires_grad and torch.is_grad_enabled():
+            raise ValueError("gate: gradients are not computed here; detach it")
+        try:
+            gate = gate.expand(T, d)
+        except RuntimeError as e:
+            raise ValueError(f"gate: shape {tuple(gate.shape)} does not broadcast to {(T, d)}") from e
+        gate_row, gate_col = gate.stride()
+    if h_out is None:
+        h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
+    else:
+        _tensor("h_out", h_out, dev, torch.float32, (T, d))
+    out = torch.empty(T, d, dtype=y.dtype, device=dev)
+    _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr(post_gain), _ptr(post_offset),
+          _ptr(gate), gate_row, gate_col, gain.data_ptr(), _ptr(offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
+    return h_out, out
