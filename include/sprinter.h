@@ -347,8 +347,7 @@ int sprinter_experts_pack(const sprinter_experts_cfg* cfg, int down, const void*
  * device); a row without any gives zeros; an expert that is named twice counts twice.  x and y have cfg->dtype, rows 16-byte aligned (ld_x, ld_y);
  * rows of y from n_rows on are not written.  The three weight arrays: packed (bf16) or row-major (float32), 16-byte
  * aligned.  Arithmetic of bf16: float16 operands (x and silu(..) * .. above 65504 become infinite), float32 sums.
- * n_rows * top_k is at most 2^20, top_k at most 64; the result does not depend on the rows beside a row nor on the
- * run.  dev_workspace: at least sprinter_experts_bytes for n_rows, 256-byte aligned, in use until the call's work is
+ * n_rows * top_k is at most 2^20, top_k at most 64; the same call gives the same bits.  dev_workspace: at least sprinter_experts_bytes for n_rows, 256-byte aligned, in use until the call's work is
  * done. */
 int sprinter_experts(const sprinter_experts_cfg* cfg, const void* dev_gate, const void* dev_up, const void* dev_down,
                      const void* dev_x, int64_t ld_x, const int32_t* dev_ids, const float* dev_route_weights,

@@ -1,95 +1,268 @@
-// HIP kernels of the experts' products for gfx950.
-#include "ops.h"
-#include "dev.h"
+// HIP kernels of the experts' products for gfx950: the plan of many rows, few rows, float32, and the sum over a row's experts.
+#include "experts.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace sprinter {
 
 // y[t] = sum_j w[t,j] W2[e] (silu(Wg[e] x_t) * (Wu[e] x_t)), e = ids[t,j].
 //
-// Every pair (t, j) with an expert gets a slot; an expert's slots lie together and begin at a multiple of 16, so that 16 slots are one
-// row tile of the matrix instruction and belong to one expert.  Which of its expert's slots a pair takes is left to chance: a row's
-// products do not depend on the rows beside it, and the sum over j runs in the order of j.
-//   plan     slots of the pairs, the rows of the slots, the list of row blocks (expert, first slot, rows)
-//   up       hidden[slot] = silu(Wg x) * (Wu x), float16 operand tiles (float32 mode: rows)
-//   down     product[slot] = W2 hidden[slot], float32
-//   combine  y[t] = sum over j
-struct Block { int expert, slot, rows; };
-struct Plan {
-  int* n_blocks; Block* blocks; int* row_of; int* slot_of;             // row_of [slots], slot_of [T k]
-};
-constexpr int BLOCK_ROWS = 16;
+// bf16 mode, up to 16 rows: they are one row tile of the matrix instruction, whoever names an expert.
+//   up_few     hidden[e][t] = w (silu(Wg x_t) * (Wu x_t)) for every expert that some row names, w = the sum of the row's weights for e,
+//              0 for rows that do not name it
+//   down_few   y[t] = sum over e of W2[e] hidden[e][t]: one product with a K of (experts named) x ff, no sum afterwards
+// Else:
+//   plan       slots of the pairs, the rows of the slots, the list of row blocks; beside it the rows as float16
+//   up, down   hidden[slot], product[slot] (k_experts_tile.hip; float32 mode: here)
+//   combine    y[t] = sum over j
 
-__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, Plan p) {
-  __shared__ int count[MAX_EXPERTS], first[MAX_EXPERTS];
-  const int tid = threadIdx.x;
-  for (int e = tid; e < E; e += 1024) count[e] = 0;
+// ------------------------------------------------------------------------------------------------------------------ plan
+// Lanes of the wave whose e is this lane's (lanes with e < 0: none of them)
+__device__ __forceinline__ u64 same_expert(int e) {
+  u64 m = __ballot(e >= 0);
+#pragma unroll
+  for (int b = 0; b < 10; ++b) {
+    const u64 set = __ballot((e >> b) & 1);
+    m &= ((e >> b) & 1) ? set : ~set;
+  }
+  return m;
+}
+// 8 elements of a row as float16
+__device__ __forceinline__ uint4 as_f16(uint4 v) {
+  unsigned* q = &v.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = pk_f16(__uint_as_float(q[i] << 16), __uint_as_float(q[i] & 0xffff0000u));
+  return v;
+}
+
+// Workgroup 0 deals out the slots: a counter per expert in LDS, to which one lane per wave and expert adds its wave's pairs; the counts'
+// prefix sums (rounded up to 16) are the experts' first slots.  The others copy x as float16 rows of Kt whole k tiles.
+__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, Plan p,
+                                                       const bf16_t* __restrict__ x, long long ldx, uint4* __restrict__ rows, int T, int d) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (blockIdx.x > 0) {
+    const int octets = round_up(d, 32) >> 3;
+    const long long n = (long long)T * octets, step = (long long)(gridDim.x - 1) * 1024;
+    for (long long i = (long long)(blockIdx.x - 1) * 1024 + tid; i < n; i += step) {
+      const int t = (int)(i / octets), c = (int)(i - (long long)t * octets) * 8;
+      rows[i] = c < d ? as_f16(*reinterpret_cast<const uint4*>(x + t * ldx + c)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    return;
+  }
+  __shared__ int count[MAX_EXPERTS], first[MAX_EXPERTS], slots[16], blocks[16];
+  count[tid] = 0;
   __syncthreads();
-  for (int i = tid; i < pairs; i += 1024) {
-    const int e = ids[i];
-    if ((unsigned)e < (unsigned)E) atomicAdd(&count[e], 1);
+  const int rounds = (pairs + 1023) / 1024;
+  for (int r = 0; r < rounds; ++r) {
+    const int i = r * 1024 + tid;
+    int e = i < pairs ? ids[i] : -1;
+    if ((unsigned)e >= (unsigned)E) e = -1;
+    const u64 same = same_expert(e);
+    int base = 0;
+    const int leader = same ? __builtin_ctzll(same) : lane;
+    if (e >= 0 && lane == leader) base = atomicAdd(&count[e], __popcll(same));
+    base = __shfl(base, leader);
+    if (i < pairs) p.slot_of[i] = e < 0 ? -1 : base + __popcll(same & ((1ull << lane) - 1));
   }
   __syncthreads();
-  if (tid == 0) {
-    int slot = 0, n = 0;
-    for (int e = 0; e < E; ++e) {
-      first[e] = slot;
-      for (int r = 0; r < count[e]; r += BLOCK_ROWS) p.blocks[n++] = Block{e, slot + r, min(BLOCK_ROWS, count[e] - r)};
-      slot += round_up(count[e], 16);
+  {
+    const int c = tid < E ? count[tid] : 0, mine = round_up(c, 16), mine_b = (c + block_rows - 1) / block_rows;
+    int s = mine, b = mine_b;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int ps = __shfl_up(s, o), pb = __shfl_up(b, o);
+      if (lane >= o) { s += ps; b += pb; }
     }
-    *p.n_blocks = n;
+    if (lane == 63) { slots[tid >> 6] = s; blocks[tid >> 6] = b; }
+    __syncthreads();
+    int s0 = s - mine, b0 = b - mine_b;
+    for (int q = 0; q < tid >> 6; ++q) { s0 += slots[q]; b0 += blocks[q]; }
+    first[tid] = s0;
+    for (int r = 0; r < c; r += block_rows) p.blocks[b0++] = Block{tid, s0 + r, min(block_rows, c - r)};
+    if (tid == 1023) *p.n_blocks = b0;
   }
   __syncthreads();
-  for (int e = tid; e < E; e += 1024) count[e] = 0;
-  __syncthreads();
-  for (int i = tid; i < pairs; i += 1024) {
-    const int e = ids[i];
-    int slot = -1;
-    if ((unsigned)e < (unsigned)E) {
-      slot = first[e] + atomicAdd(&count[e], 1);
-      p.row_of[slot] = i / k;
-    }
+  for (int i = tid; i < pairs; i += 1024) {             // (a thread's own stores of above)
+    const int at = p.slot_of[i];
+    if (at < 0) continue;
+    const int slot = first[ids[i]] + at;
     p.slot_of[i] = slot;
+    p.row_of[slot] = i / k;
   }
 }
 
-// One lane's operand of a k tile.  bf16 mode: 8 float16 of 32 k; float32 mode: 4 float32 of 16 k, one per instruction of 4 k each.
-template <int DT> struct Operand;
-template <> struct Operand<SPRINTER_BF16> { using T = uint4; static constexpr int K = 32, PER = 8; };
-template <> struct Operand<SPRINTER_F32> { using T = f32x4; static constexpr int K = 16, PER = 4; };
-__device__ __forceinline__ f32x4 product(uint4 x, uint4 w, f32x4 c) { return mfma_f16(x, w, c); }
+// -------------------------------------------------------------------------------------------------------------- few rows
+constexpr int FEW_ROWS = 16;
+
+// The set of experts that `pairs` ids name, as bits in LDS; then the j-th of them in rising order (every wave for itself; -1: there are
+// no more), and with a list the whole set.
+struct NamedExperts { unsigned bits[MAX_EXPERTS / 32]; };
+__device__ __forceinline__ void name_experts(NamedExperts& s, const int* __restrict__ ids, int pairs, int E) {
+  if (threadIdx.x < MAX_EXPERTS / 32) s.bits[threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+    const int e = ids[i];
+    if ((unsigned)e < (unsigned)E) atomicOr(&s.bits[e >> 5], 1u << (e & 31));
+  }
+  __syncthreads();
+}
+// Bits before word `lane` (lanes 0 - 31), and all of them
+__device__ __forceinline__ int named_before(unsigned word, int lane, int& all) {
+  int n = __popc(word);
+  for (int o = 1; o < 32; o <<= 1) { const int up = __shfl_up(n, o); if (lane >= o) n += up; }
+  all = __builtin_amdgcn_readlane(n, 31);
+  return n - __popc(word);
+}
+__device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int lane) {
+  unsigned word = lane < 32 ? s.bits[lane] : 0u;
+  int all;
+  const int before = named_before(word, lane, all);
+  if (j >= all) return -1;                              // (scalar)
+  const int at = __builtin_ctzll(__ballot(lane < 32 && before <= j && j < before + __popc(word)));
+  word = (unsigned)__builtin_amdgcn_readlane((int)word, at);
+  for (int i = __builtin_amdgcn_readlane(before, at); i < j; ++i) word &= word - 1;
+  return at * 32 + __builtin_ctz(word);
+}
+
+// A workgroup: one expert's NTW column tiles of both matrices.  The 8 waves share K; each thread then finishes the elements of one row
+// and column in each tile.
+template <int NTW>
+__global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
+                                                        int T, int k, int E, int d, int ff, long long ldx, int x_type, int groups, uint4* hidden) {
+  constexpr int U = 4;
+  __shared__ NamedExperts named;
+  __shared__ float red[8][NTW * 2][4][64], row_w[FEW_ROWS];
+  __shared__ int row_hit[FEW_ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
+  const int j = blockIdx.x / groups, nt0 = (blockIdx.x - j * groups) * NTW;
+  name_experts(named, ids, T * k, E);
+  const int e = named_expert(named, j, lane);
+  if (e < 0) return;
+  const int Kt = (d + 31) >> 5, Nt = (ff + 15) >> 4, row = lane & 15, oct = (lane >> 4) * 8;
+  const uint4* Wg = (const uint4*)wg + (size_t)e * Nt * Kt * 64 + lane;
+  const uint4* Wu = (const uint4*)wu + (size_t)e * Nt * Kt * 64 + lane;
+  const bf16_t* x = (const bf16_t*)x_ + (size_t)min(row, T - 1) * ldx;
+  f32x4 g[NTW], u[NTW];
+#pragma unroll
+  for (int n = 0; n < NTW; ++n) g[n] = u[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int kt = w; kt < Kt; kt += 8 * U) {
+    uint4 a[U][NTW], b[U][NTW], v[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int kc = min(kt + q * 8, Kt - 1);
+#pragma unroll
+      for (int n = 0; n < NTW; ++n) {
+        const size_t at = ((size_t)min(nt0 + n, Nt - 1) * Kt + kc) * 64;
+        a[q][n] = Wg[at]; b[q][n] = Wu[at];
+      }
+      v[q] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < T && kt + q * 8 < Kt && kc * 32 + oct < d) v[q] = *reinterpret_cast<const uint4*>(x + kc * 32 + oct);
+    }
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const uint4 h = x_type == X_BF16 ? as_f16(v[q]) : v[q];
+#pragma unroll
+      for (int n = 0; n < NTW; ++n) { g[n] = mfma_f16(h, a[q][n], g[n]); u[n] = mfma_f16(h, b[q][n], u[n]); }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NTW; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { red[w][2 * n][i][lane] = g[n][i]; red[w][2 * n + 1][i][lane] = u[n][i]; }
+  {                                                     // 32 threads to a row
+    const int m = tid >> 5;
+    float s = 0.f;
+    int hit = 0;
+    if (m < T)
+      for (int i = tid & 31; i < k; i += 32)
+        if (ids[m * k + i] == e) { s += weights[m * k + i]; hit = 1; }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { s += __shfl_xor(s, o); hit |= __shfl_xor(hit, o); }
+    if ((tid & 31) == 0) { row_w[m] = s; row_hit[m] = hit; }
+  }
+  __syncthreads();
+  bf16_t* out = (bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64);
+  for (int o = tid; o < NTW * 256; o += 512) {          // (row m, column c), in the order of the operand tile
+    const int m = (o >> 3) & 15, c = (o >> 7) * 8 + (o & 7), n = nt0 * 16 + c, i = m & 3, at = (m >> 2) * 16 + (c & 15);
+    float gs = 0.f, us = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) { gs += red[q][2 * (c >> 4)][i][at]; us += red[q][2 * (c >> 4) + 1][i][at]; }
+    if (n < round_up(ff, 32)) act_store<bf16_t>(out, m, n, ff, row_hit[m] && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
+  }
+}
+
+// A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.
+__global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const int* __restrict__ ids, int T, int k, int E, int d,
+                                                          int ff, int shares, float* part, void* y, int y_type, long long ldy) {
+  constexpr int U = 8;
+  __shared__ NamedExperts named;
+  __shared__ unsigned short list[MAX_EXPERTS];
+  __shared__ float red[8][4][64];
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
+  const int Nt = (d + 15) >> 4, Kt = (ff + 31) >> 5, nt = blockIdx.x % Nt, share = blockIdx.x / Nt;
+  name_experts(named, ids, T * k, E);
+  int all;
+  {
+    unsigned word = lane < 32 ? named.bits[lane] : 0u;
+    int at = named_before(word, lane, all);
+    if (w == 0 && lane < 32)
+      for (; word; word &= word - 1) list[at++] = (unsigned short)(lane * 32 + __builtin_ctz(word));
+  }
+  __syncthreads();
+  const int total = all * Kt, parts = shares * 8, me = share * 8 + w;
+  const int q0 = (int)((long long)total * me / parts), q1 = (int)((long long)total * (me + 1) / parts);
+  const bool live = (lane & 15) < T;
+  f32x4 c = (f32x4){0.f, 0.f, 0.f, 0.f};
+  const uint4* W = (const uint4*)w2 + lane;
+  const uint4* H = hidden + lane;
+  for (int q = q0; q < q1; q += U) {
+    uint4 a[U], h[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int qc = min(q + i, q1 - 1), j = qc / Kt, e = __builtin_amdgcn_readfirstlane((int)list[j]);
+      a[i] = W[(((size_t)e * Nt + nt) * Kt + (qc - j * Kt)) * 64];
+      h[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (live && q + i < q1) h[i] = H[(size_t)qc * 64];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) c = mfma_f16(h[i], a[i], c);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) red[w][i][lane] = c[i];
+  __syncthreads();
+  if (tid >= 256) return;
+  const int m = tid >> 4, n = nt * 16 + (tid & 15), at = (m >> 2) * 16 + (tid & 15);
+  if (m >= T || n >= d) return;
+  float s = 0.f;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) s += red[q][m & 3][at];
+  if (shares > 1) part[((size_t)share * FEW_ROWS + m) * d + n] = s;
+  else if (y_type == X_F32) ((float*)y)[m * ldy + n] = s;
+  else ((bf16_t*)y)[m * ldy + n] = f2bf(s);
+}
+__global__ __launch_bounds__(256) void k_experts_join(const float* __restrict__ part, int shares, int T, int d, void* y, int y_type, long long ldy) {
+  const int parts = (d + 255) >> 8, m = blockIdx.x / parts, n = (blockIdx.x - m * parts) * 256 + threadIdx.x;
+  if (n >= d) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int q = 0; q < shares; ++q) s += part[((size_t)q * FEW_ROWS + m) * d + n];
+  if (y_type == X_F32) ((float*)y)[m * ldy + n] = s;
+  else ((bf16_t*)y)[m * ldy + n] = f2bf(s);
+}
+
+// --------------------------------------------------------------------------------------------------------------- float32
+// One lane's operand of a k tile: 4 float32 of 16 k, one per instruction of 4 k each.
 __device__ __forceinline__ f32x4 product(f32x4 x, f32x4 w, f32x4 c) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], w[i], c, 0, 0, 0);
   return c;
 }
-// 8 elements of a row as float16
-__device__ __forceinline__ uint4 load_x(const bf16_t* p, int type) {
-  uint4 v = *reinterpret_cast<const uint4*>(p);
-  if (type == X_BF16) {
-    unsigned* q = &v.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = pk_f16(__uint_as_float(q[i] << 16), __uint_as_float(q[i] & 0xffff0000u));
-  }
-  return v;
+__device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
+  const f32x4 v = *reinterpret_cast<const f32x4*>(row + min(k, K - 4));
+  return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
-__device__ __forceinline__ f32x4 load_x(const float* p, int) { return *reinterpret_cast<const f32x4*>(p); }
-template <int DT> using Elem = std::conditional_t<DT == SPRINTER_F32, float, bf16_t>;
+constexpr int F32_BLOCK_ROWS = 16;
 
-// The weights of column tile nt, k tile kt: row n of expert e of a matrix [E][N][K]
-template <int DT>
-__device__ __forceinline__ typename Operand<DT>::T load_w(const void* W, int e, int N, int K, int nt, int kt, int lane) {
-  if constexpr (DT == SPRINTER_BF16) {
-    const int Kt = (K + 31) >> 5, Nt = (N + 15) >> 4;
-    return ((const uint4*)W)[(((size_t)e * Nt + nt) * Kt + kt) * 64 + lane];
-  } else {
-    const int n = min(nt * 16 + (lane & 15), N - 1), k = kt * 16 + (lane >> 4) * 4;
-    const f32x4 v = *reinterpret_cast<const f32x4*>((const float*)W + ((size_t)e * N + n) * K + min(k, K - 4));
-    return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
-  }
-}
-
-// Sum of the four waves' accumulators, in wave 0
+// Sum of the four waves' accumulators
 __device__ __forceinline__ f32x4 join(f32x4 v, f32x4 (*red)[64], int w, int lane) {
   red[w][lane] = v;
   __syncthreads();
@@ -98,65 +271,45 @@ __device__ __forceinline__ f32x4 join(f32x4 v, f32x4 (*red)[64], int w, int lane
   return s;
 }
 
-// A workgroup: one column tile (of col_tiles) of one row block.  Four waves share K.
-template <int DT>
-__global__ __launch_bounds__(256) void k_experts_up(ExpertsArgs a, Plan p, void* hidden, int col_tiles) {
-  using O = Operand<DT>;
+// A workgroup: one column tile (of col_tiles) of one row block.  Four waves share K.  up: out = silu(Wg x) * (Wu x) of the gathered rows.
+template <bool UP>
+__global__ __launch_bounds__(256) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out, int col_tiles) {
   __shared__ f32x4 red[4][64];
   const int lane = threadIdx.x & 63, w = wave_index(), id = blockIdx.x / col_tiles, nt = blockIdx.x - id * col_tiles;
   if (id >= *p.n_blocks) return;
   const Block b = p.blocks[id];
-  const int r = min(lane & 15, b.rows - 1);
-  const Elem<DT>* x = (const Elem<DT>*)a.x + (long long)p.row_of[b.slot + r] * a.ldx;
-  const int Kt = (a.d + O::K - 1) / O::K;
+  const int slot = b.slot + min(lane & 15, b.rows - 1);
+  const float* x = X + (UP ? p.row_of[slot] : slot) * ldx;
+  const size_t at = ((size_t)b.expert * N + min(nt * 16 + (lane & 15), N - 1)) * K;
   f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
-  for (int kt = w; kt < Kt; kt += 4) {
-    const int k = kt * O::K + (lane >> 4) * O::PER;
-    typename O::T xv = {};
-    if (k < a.d) xv = load_x(x + k, a.x_type);
-    g = product(xv, load_w<DT>(a.wg, b.expert, a.ff, a.d, nt, kt, lane), g);
-    u = product(xv, load_w<DT>(a.wu, b.expert, a.ff, a.d, nt, kt, lane), u);
+  for (int kt = w; kt < (K + 15) >> 4; kt += 4) {
+    const int k = kt * 16 + (lane >> 4) * 4;
+    const f32x4 v = load4(x, k, K);
+    g = product(v, load4(W + at, k, K), g);
+    if (UP) u = product(v, load4(W2 + at, k, K), u);
   }
   g = join(g, red, w, lane);
-  u = join(u, red, w, lane);
+  if (UP) u = join(u, red, w, lane);
   const int n = nt * 16 + (lane & 15), m = (lane >> 4) * 4 + w;        // each wave finishes one of the four rows of a lane
-  if (m < b.rows && n < a.ff) act_store<Elem<DT>>((Elem<DT>*)hidden, b.slot + m, n, a.ff, silu(g[w]) * u[w]);
+  if (m < b.rows && n < N) out[(size_t)(b.slot + m) * N + n] = UP ? silu(g[w]) * u[w] : g[w];
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void k_experts_down(ExpertsArgs a, Plan p, const void* hidden, float* out, int col_tiles) {
-  using O = Operand<DT>;
-  __shared__ f32x4 red[4][64];
-  const int lane = threadIdx.x & 63, w = wave_index(), id = blockIdx.x / col_tiles, nt = blockIdx.x - id * col_tiles;
-  if (id >= *p.n_blocks) return;
-  const Block b = p.blocks[id];
-  const int slot = b.slot + min(lane & 15, b.rows - 1), Kt = (a.ff + O::K - 1) / O::K;
-  f32x4 c = {0.f, 0.f, 0.f, 0.f};
-  for (int kt = w; kt < Kt; kt += 4) {
-    const int k = kt * O::K + (lane >> 4) * O::PER;
-    typename O::T xv = {};
-    if (k < a.ff) xv = load_x((const Elem<DT>*)hidden + act_idx<Elem<DT>>(slot, k, a.ff), X_F16);
-    c = product(xv, load_w<DT>(a.w2, b.expert, a.d, a.ff, nt, kt, lane), c);
-  }
-  c = join(c, red, w, lane);
-  const int n = nt * 16 + (lane & 15), m = (lane >> 4) * 4 + w;
-  if (m < b.rows && n < a.d) out[(size_t)(b.slot + m) * a.d + n] = c[w];
-}
-
+// --------------------------------------------------------------------------------------------------------------- combine
 // One thread per 4 columns of a row.
-__global__ __launch_bounds__(256) void k_experts_combine(ExpertsArgs a, const int* __restrict__ slot_of, const float* __restrict__ out, int parts) {
+__global__ __launch_bounds__(256) void k_experts_combine(const int* __restrict__ slot_of, const float* __restrict__ weights, const float* __restrict__ out, int k, int d,
+                                                         int parts, void* y, int y_type, long long ldy) {
   const int t = blockIdx.x / parts, c = ((blockIdx.x - t * parts) * 256 + threadIdx.x) * 4;
-  if (c >= a.d) return;
+  if (c >= d) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j = 0; j < a.k; ++j) {
-    const int slot = slot_of[(size_t)t * a.k + j];
+  for (int j = 0; j < k; ++j) {
+    const int slot = slot_of[(size_t)t * k + j];
     if (slot < 0) continue;
-    const float w = a.weights[(size_t)t * a.k + j];
-    const float4 v = *reinterpret_cast<const float4*>(out + (size_t)slot * a.d + c);
+    const float w = weights[(size_t)t * k + j];
+    const float4 v = *reinterpret_cast<const float4*>(out + (size_t)slot * d + c);
     s.x += w * v.x; s.y += w * v.y; s.z += w * v.z; s.w += w * v.w;
   }
-  if (a.y_type == X_F32) *reinterpret_cast<float4*>((float*)a.y + (long long)t * a.ldy + c) = s;
-  else *reinterpret_cast<uint2*>((bf16_t*)a.y + (long long)t * a.ldy + c) = make_uint2(pk_bf16(s.x, s.y), pk_bf16(s.z, s.w));
+  if (y_type == X_F32) *reinterpret_cast<float4*>((float*)y + t * ldy + c) = s;
+  else *reinterpret_cast<uint2*>((bf16_t*)y + t * ldy + c) = make_uint2(pk_bf16(s.x, s.y), pk_bf16(s.z, s.w));
 }
 
 void launch_pack_experts(const void* w, void* out, int E, int N, int K, hipStream_t s) {
@@ -165,21 +318,34 @@ void launch_pack_experts(const void* w, void* out, int E, int N, int K, hipStrea
 }
 
 namespace {
+bool few(int dtype, long long T) { return dtype == SPRINTER_BF16 && T <= FEW_ROWS; }
+// Shares of the K of down_few: one workgroup per compute unit and more.
+int few_shares(int d) { return std::max(1, 512 / ((d + 15) / 16)); }
+
 struct Space {
-  Plan plan; void* hidden; float* out; size_t bytes;
+  Plan plan; int slots, blocks; void *rows, *hidden; float* out; size_t bytes;
 };
-// pairs and experts bound the slots: every used expert rounds its own up to 16.
+// pairs and experts bound the slots: every expert named rounds its own up to 16.
 Space space(void* base, int dtype, int E, int d, int ff, long long T, int k) {
-  const long long pairs = T * k, slots = (pairs + 15 * std::min<long long>(E, pairs) + 15) / 16 * 16;
+  const long long pairs = T * k, named = std::min<long long>(E, pairs);
+  const bool bf = dtype == SPRINTER_BF16;
   size_t at = 0;
   auto take = [&](size_t n) { void* p = (char*)base + at; at += (n + 255) & ~(size_t)255; return p; };
-  Space s;
-  s.plan.n_blocks = (int*)take(4);
-  s.plan.blocks = (Block*)take((size_t)(slots / 16) * sizeof(Block));
-  s.plan.row_of = (int*)take((size_t)slots * 4);
-  s.plan.slot_of = (int*)take((size_t)pairs * 4);
-  s.hidden = take((size_t)slots * (dtype == SPRINTER_F32 ? (size_t)ff * 4 : (size_t)round_up(ff, 32) * 2));
-  s.out = (float*)take((size_t)slots * d * 4);
+  Space s{};
+  if (few(dtype, T)) {
+    s.hidden = take((size_t)named * FEW_ROWS * round_up(ff, 32) * 2);
+    s.out = (float*)take((size_t)few_shares(d) * FEW_ROWS * d * 4);
+  } else {
+    s.slots = (int)((pairs + 15 * named + 15) / 16 * 16);
+    s.blocks = s.slots / 16;
+    s.plan.n_blocks = (int*)take(4);
+    s.plan.blocks = (Block*)take((size_t)s.blocks * sizeof(Block));
+    s.plan.row_of = (int*)take((size_t)s.slots * 4);
+    s.plan.slot_of = (int*)take((size_t)pairs * 4);
+    s.rows = bf ? take((size_t)T * round_up(d, 32) * 2) : nullptr;
+    s.hidden = take((size_t)s.slots * (bf ? (size_t)round_up(ff, 32) * 2 : (size_t)ff * 4));
+    s.out = (float*)take((size_t)s.slots * d * 4);
+  }
   s.bytes = at;
   return s;
 }
@@ -189,17 +355,33 @@ size_t experts_workspace(int dtype, int E, int d, int ff, long long T, int k) { 
 
 void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   const Space w = space(workspace, a.dtype, a.E, a.d, a.ff, a.T, a.k);
-  const int pairs = a.T * a.k, blocks = pairs / BLOCK_ROWS + std::min(a.E, pairs);
-  hipLaunchKernelGGL(k_experts_plan, dim3(1), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, w.plan);
-  const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16, parts = (a.d / 4 + 255) / 256;
-  if (a.dtype == SPRINTER_F32) {
-    hipLaunchKernelGGL(k_experts_up<SPRINTER_F32>, dim3(up * blocks), dim3(256), 0, s, a, w.plan, w.hidden, up);
-    hipLaunchKernelGGL(k_experts_down<SPRINTER_F32>, dim3(down * blocks), dim3(256), 0, s, a, w.plan, w.hidden, w.out, down);
-  } else {
-    hipLaunchKernelGGL(k_experts_up<SPRINTER_BF16>, dim3(up * blocks), dim3(256), 0, s, a, w.plan, w.hidden, up);
-    hipLaunchKernelGGL(k_experts_down<SPRINTER_BF16>, dim3(down * blocks), dim3(256), 0, s, a, w.plan, w.hidden, w.out, down);
+  const int pairs = a.T * a.k, named = std::min(a.E, pairs);
+  if (few(a.dtype, a.T)) {
+    constexpr int NTW = 2;
+    const int groups = ((a.ff + 15) / 16 + NTW - 1) / NTW, Nt = (a.d + 15) / 16, shares = few_shares(a.d);
+    hipLaunchKernelGGL(k_experts_up_few<NTW>, dim3(named * groups), dim3(512), 0, s, a.wg, a.wu, a.x, a.ids, a.weights, a.T, a.k, a.E, a.d, a.ff, a.ldx, a.x_type,
+                       groups, (uint4*)w.hidden);
+    hipLaunchKernelGGL(k_experts_down_few, dim3(Nt * shares), dim3(512), 0, s, a.w2, (const uint4*)w.hidden, a.ids, a.T, a.k, a.E, a.d, a.ff, shares, w.out, a.y, a.y_type, a.ldy);
+    if (shares > 1)
+      hipLaunchKernelGGL(k_experts_join, dim3(a.T * ((a.d + 255) / 256)), dim3(256), 0, s, w.out, shares, a.T, a.d, a.y, a.y_type, a.ldy);
+    return;
   }
-  hipLaunchKernelGGL(k_experts_combine, dim3(parts * a.T), dim3(256), 0, s, a, w.plan.slot_of, w.out, parts);
+  const bool f32 = a.dtype == SPRINTER_F32, copy = !f32 && a.x_type != X_F16;
+  const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? F32_BLOCK_ROWS : expert_tile_rows(tile);
+  const int copies = copy ? (int)std::min<long long>(1023, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
+  const int blocks = pairs / block_rows + named, parts = (a.d / 4 + 255) / 256;
+  hipLaunchKernelGGL(k_experts_plan, dim3(1 + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, w.plan, (const bf16_t*)a.x, a.ldx, (uint4*)w.rows, a.T, a.d);
+  if (f32) {
+    const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16;
+    hipLaunchKernelGGL(k_experts_f32<true>, dim3(up * blocks), dim3(256), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan,
+                       (float*)w.hidden, up);
+    hipLaunchKernelGGL(k_experts_f32<false>, dim3(down * blocks), dim3(256), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, w.plan,
+                       w.out, down);
+  } else {
+    launch_expert_tiles(tile, ExpertTiles{w.plan, blocks, w.slots, a.E, a.d, a.ff, a.wg, a.wu, a.w2, copy ? w.rows : a.x,
+                                          copy ? (long long)round_up(a.d, 32) * 2 : a.ldx * 2, w.hidden, w.out}, s);
+  }
+  hipLaunchKernelGGL(k_experts_combine, dim3(parts * a.T), dim3(256), 0, s, w.plan.slot_of, a.weights, w.out, a.k, a.d, parts, a.y, a.y_type, a.ldy);
 }
 
 }  // namespace sprinter
