@@ -8,7 +8,7 @@ namespace sprinter {
 // Every pair (t, j) with an expert gets a slot; an expert's slots lie together and begin at a multiple of 16, so that 16 slots are one
 // row tile of the matrix instruction and belong to one expert.  Which of its expert's slots a pair takes is left to chance: a row's
 // products do not depend on the rows beside it, and the sum over j runs in the order of j.
-struct Block { int expert, slot, rows; };              // up to block_rows slots of one expert
+struct Block { int expert, slot, rows, first, count; };   // up to block_rows slots of one expert, whose blocks are [first, first + count)
 struct Plan {
   int* n_blocks; Block* blocks; int* row_of; int* slot_of;             // row_of [slots], slot_of [T k]
 };

@@ -32,6 +32,7 @@ struct GemmTile {                                       // WM x WN waves, MT x N
 };
 using TileL = GemmTile<2, 2, 8, 8, 4>;                  // 256 x 256, 128 KiB: one workgroup per compute unit
 using TileH = GemmTile<2, 2, 8, 4, 4>;                  // 256 x 128, for the last round of the one above
+using TileT = GemmTile<2, 2, 4, 8, 4>;                  // 128 x 256, for row blocks of at most 128 rows among those of the first one
 using TileG = GemmTile<4, 2, 4, 8, 4>;                  // 256 x 256 of eight waves, for GELU
 using TileM = GemmTile<2, 2, 4, 4, 5>;                  // 128 x 128, 80 KiB: two
 using TileS = GemmTile<2, 2, 2, 4, 6>;                  // 64 x 128, 72 KiB: two
@@ -45,7 +46,9 @@ __device__ __forceinline__ int xcd_run(int id, int n_blk) {
 }
 
 // Row blocks of grouped products: the operand tiles from row tile tile0 on, rows up to `end`; or, with RowsGathered, row i is row
-// row_of[i] of a row-major float16 matrix (rows row_bytes apart, whole k tiles): a lane fetches its own 16 bytes of its row.
+// row_of[i] of a row-major float16 matrix (rows row_bytes apart, whole k tiles).  Four lanes next to each other fetch the 64 bytes of a
+// row's k tile (in the lane order of the operand they would be 16 lanes apart, which cost the 256 x 256 tile a fifth of its rate); in LDS
+// a row's octets are exchanged by row / 4, so that the fragment reads stay free of bank conflicts.
 struct RowsOfTiles { int tile0, end; };
 struct RowsGathered { int tile0, end; const int* row_of; long long row_bytes; };
 
@@ -76,7 +79,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, int x_tiles, int bm
     int tile;
     if (l < TMT) {
       if constexpr (GATHER) {
-        src[i] = (const char*)a.X + (long long)rows.row_of[min((row0 + l) * 16 + (lane & 15), rows.end - 1)] * rows.row_bytes + (lane >> 4) * 16;
+        src[i] = (const char*)a.X + (long long)rows.row_of[min((row0 + l) * 16 + (lane >> 2), rows.end - 1)] * rows.row_bytes + ((lane & 3) ^ (lane >> 4)) * 16;
         continue;
       }
       base = a.X;
@@ -104,13 +107,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, int x_tiles, int bm
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  // this lane's 16 bytes of an activation tile in LDS, relative to its own of a weight tile
+  const int x_at = GATHER ? (lane & 15) * 4 + ((lane >> 4) ^ ((lane >> 2) & 3)) - lane : 0;
   struct Frag { u32x4 x[MT], w[NT]; };
   auto read = [&](Frag& f, int kt) {
     const u32x4* s = &ring[(kt - k0) % S][0][lane];
 #pragma unroll
     for (int j = 0; j < NT; ++j) f.w[j] = s[(TMT + wn * NT + j) * 64];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) f.x[i] = s[(wm * MT + i) * 64];
+    for (int i = 0; i < MT; ++i) f.x[i] = s[(wm * MT + i) * 64 + x_at];
   };
   auto mul = [&](const Frag& f) {
 #pragma unroll
@@ -173,7 +178,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, int x_tiles, int bm
         const int r = i * RPR + j / GAP;
         if (j % GAP == GAP - 1 && j / GAP < RPR && r < MT + NT) {
           if (r < NT) nx.w[r] = sn[(TMT + wn * NT + r) * 64];
-          else nx.x[r - NT] = sn[(wm * MT + r - NT) * 64];
+          else nx.x[r - NT] = sn[(wm * MT + r - NT) * 64 + x_at];
           __builtin_amdgcn_sched_barrier(0);
         }
         if (j == NT - 1) {
@@ -360,5 +365,10 @@ __device__ __forceinline__ void tile_place(int t, int gm, int gn, int& bm, int& 
   const int band = t / (GM * gn), in_band = t - band * GM * gn, bh = min(GM, gm - band * GM);
   bm = band * GM + in_band % bh; bn = in_band / bh;
 }
+
+// One workgroup of the 256 x 256 tile runs per compute unit: a last round with work for at most half of them is dealt out in halves of
+// 256 x 128, 0.6 of a round.  us: 384 tiles (6144 x 4096 at 4096 rows) 196 -> 168, 336 (3528 rows) 182 -> 152, 602 (2 x 11008 x 4096 at
+// 1792 rows) 288 -> 259, 1376 (4096 rows) 596 -> 567, 1568 (2 x 14336 x 4096 at 3528 rows) 698 -> 678.
+static __host__ __device__ inline int tiles_in_halves(int tiles) { return tiles > 256 && tiles % 256 <= 128 ? tiles % 256 : 0; }
 
 }  // namespace sprinter

@@ -17,16 +17,6 @@ namespace sprinter {
 //   combine    y[t] = sum over j
 
 // ------------------------------------------------------------------------------------------------------------------ plan
-// Lanes of the wave whose e is this lane's (lanes with e < 0: none of them)
-__device__ __forceinline__ u64 same_expert(int e) {
-  u64 m = __ballot(e >= 0);
-#pragma unroll
-  for (int b = 0; b < 10; ++b) {
-    const u64 set = __ballot((e >> b) & 1);
-    m &= ((e >> b) & 1) ? set : ~set;
-  }
-  return m;
-}
 // 8 elements of a row as float16
 __device__ __forceinline__ uint4 as_f16(uint4 v) {
   unsigned* q = &v.x;
@@ -35,7 +25,7 @@ __device__ __forceinline__ uint4 as_f16(uint4 v) {
   return v;
 }
 
-// Workgroup 0 deals out the slots: a counter per expert in LDS, to which one lane per wave and expert adds its wave's pairs; the counts'
+// Workgroup 0 deals out the slots: a counter per expert in LDS gives each pair its place among its expert's, and the counts'
 // prefix sums (rounded up to 16) are the experts' first slots.  The others copy x as float16 rows of Kt whole k tiles.
 __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, Plan p,
                                                        const bf16_t* __restrict__ x, long long ldx, uint4* __restrict__ rows, int T, int d) {
@@ -50,19 +40,30 @@ __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ i
     return;
   }
   __shared__ int count[MAX_EXPERTS], first[MAX_EXPERTS], slots[16], blocks[16];
+  constexpr int N = 16;                                 // ids of a thread that are requested together
   count[tid] = 0;
   __syncthreads();
-  const int rounds = (pairs + 1023) / 1024;
-  for (int r = 0; r < rounds; ++r) {
-    const int i = r * 1024 + tid;
-    int e = i < pairs ? ids[i] : -1;
-    if ((unsigned)e >= (unsigned)E) e = -1;
-    const u64 same = same_expert(e);
-    int base = 0;
-    const int leader = same ? __builtin_ctzll(same) : lane;
-    if (e >= 0 && lane == leader) base = atomicAdd(&count[e], __popcll(same));
-    base = __shfl(base, leader);
-    if (i < pairs) p.slot_of[i] = e < 0 ? -1 : base + __popcll(same & ((1ull << lane) - 1));
+  int e[N], at[N];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int i = i0 + r * 1024 + tid;
+      e[r] = -1;
+      if (i0 + r * 1024 >= pairs) continue;             // (scalar)
+      if (i < pairs) e[r] = ids[i];
+      if ((unsigned)e[r] >= (unsigned)E) e[r] = -1;
+    }
+  };
+  const bool once = pairs <= N * 1024;                  // what a thread knows stays in its registers; else in slot_of
+  for (int i0 = 0; i0 < pairs; i0 += N * 1024) {
+    load(i0);
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      if (i0 + r * 1024 >= pairs) break;                // (scalar)
+      at[r] = e[r] < 0 ? -1 : atomicAdd(&count[e[r]], 1);
+      const int i = i0 + r * 1024 + tid;
+      if (!once && i < pairs) p.slot_of[i] = at[r];
+    }
   }
   __syncthreads();
   {
@@ -77,16 +78,27 @@ __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ i
     int s0 = s - mine, b0 = b - mine_b;
     for (int q = 0; q < tid >> 6; ++q) { s0 += slots[q]; b0 += blocks[q]; }
     first[tid] = s0;
-    for (int r = 0; r < c; r += block_rows) p.blocks[b0++] = Block{tid, s0 + r, min(block_rows, c - r)};
-    if (tid == 1023) *p.n_blocks = b0;
+    for (int i = 0; i < mine_b; ++i) p.blocks[b0 + i] = Block{tid, s0 + i * block_rows, min(block_rows, c - i * block_rows), b0, mine_b};
+    if (tid == 1023) *p.n_blocks = b0 + mine_b;
   }
   __syncthreads();
-  for (int i = tid; i < pairs; i += 1024) {             // (a thread's own stores of above)
-    const int at = p.slot_of[i];
-    if (at < 0) continue;
-    const int slot = first[ids[i]] + at;
-    p.slot_of[i] = slot;
-    p.row_of[slot] = i / k;
+  for (int i0 = 0; i0 < pairs; i0 += N * 1024) {
+    if (!once) {
+      load(i0);
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        at[r] = -1;
+        if (i0 + r * 1024 < pairs && e[r] >= 0) at[r] = p.slot_of[i0 + r * 1024 + tid];      // (this thread's own stores)
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int i = i0 + r * 1024 + tid;
+      if (i >= pairs) break;
+      if (e[r] >= 0) at[r] += first[e[r]];
+      p.slot_of[i] = at[r];
+      if (e[r] >= 0) p.row_of[at[r]] = i / k;
+    }
   }
 }
 

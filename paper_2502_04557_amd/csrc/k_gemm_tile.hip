@@ -53,11 +53,6 @@ static float tile_us(const TileCost& c, int epi, int rows, int N, int Kt, int sk
   return c.start_us + std::max(cycles / 2400.f, std::max(product, memory)) + part / 4.5e6f + (epi == EPI_PART && sk > 4 ? 0.3f : 0.f);
 }
 
-// One workgroup of the 256 x 256 tile runs per compute unit: a last round with work for at most half of them is dealt out in halves of
-// 256 x 128, 0.6 of a round.  us: 384 tiles (6144 x 4096 at 4096 rows) 196 -> 168, 336 (3528 rows) 182 -> 152, 602 (2 x 11008 x 4096 at
-// 1792 rows) 288 -> 259, 1376 (4096 rows) 596 -> 567, 1568 (2 x 14336 x 4096 at 3528 rows) 698 -> 678.
-static int tiles_in_halves(int tiles) { return tiles > 256 && tiles % 256 <= 128 ? tiles % 256 : 0; }
-
 template <typename T, int EPI>
 static void launch_tile(const GemmArgs& a, int rows, int sk, hipStream_t s) {
   constexpr int tm = T::wm * T::mt * 16, cols = T::wn * T::nt * 16 / (EPI == EPI_SWIGLU ? 2 : 1);
