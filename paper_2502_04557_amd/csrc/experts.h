@@ -20,9 +20,9 @@ struct ExpertTiles {
   const void *wg, *wu, *w2, *x; long long row_bytes;
   void* hidden; float* out;                            // operand tiles [slots, ff]; [slots, d]
 };
-constexpr int N_EXPERT_TILES = 5;
+constexpr int N_EXPERT_TILES = 4;
 int expert_tile_rows(int tile);
-// The tile whose two products are estimated to be the shortest.
+// 0 - 3: 256 x 256, 128 x 128, 64 x 128, 32 x 64.
 int expert_tile_choice(int E, long long pairs, int d, int ff);
 void launch_expert_tiles(int tile, const ExpertTiles& a, hipStream_t s);
 

@@ -25,44 +25,41 @@ __device__ __forceinline__ uint4 as_f16(uint4 v) {
   return v;
 }
 
-// Workgroup 0 deals out the slots: a counter per expert in LDS gives each pair its place among its expert's, and the counts'
-// prefix sums (rounded up to 16) are the experts' first slots.  The others copy x as float16 rows of Kt whole k tiles.
-__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, Plan p,
+// A counter per expert in LDS gives each pair its place among its expert's; the counts' prefix sums (rounded up to 16) are the experts'
+// first slots.  Every workgroup counts all pairs, those before its own share apart, and writes the slots of its share: the scattered
+// stores of one workgroup alone took 18 us for 14312 pairs.  The workgroups behind the `plans` of them copy x as float16 rows of whole k tiles.
+__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, int share, Plan p, int plans,
                                                        const bf16_t* __restrict__ x, long long ldx, uint4* __restrict__ rows, int T, int d) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  if (blockIdx.x > 0) {
+  __shared__ int count[MAX_EXPERTS], before[MAX_EXPERTS], slots[16], blocks[16];
+  constexpr int N = 8;                                  // ids of a thread that are requested together
+  const int tid = threadIdx.x, lane = tid & 63, p0 = blockIdx.x * share, p1 = min(p0 + share, pairs);
+  if ((int)blockIdx.x >= plans) {
     const int octets = round_up(d, 32) >> 3;
-    const long long n = (long long)T * octets, step = (long long)(gridDim.x - 1) * 1024;
-    for (long long i = (long long)(blockIdx.x - 1) * 1024 + tid; i < n; i += step) {
+    const long long n = (long long)T * octets, step = (long long)(gridDim.x - plans) * 1024;
+    for (long long i = (long long)(blockIdx.x - plans) * 1024 + tid; i < n; i += step) {
       const int t = (int)(i / octets), c = (int)(i - (long long)t * octets) * 8;
       rows[i] = c < d ? as_f16(*reinterpret_cast<const uint4*>(x + t * ldx + c)) : make_uint4(0u, 0u, 0u, 0u);
     }
     return;
   }
-  __shared__ int count[MAX_EXPERTS], first[MAX_EXPERTS], slots[16], blocks[16];
-  constexpr int N = 16;                                 // ids of a thread that are requested together
-  count[tid] = 0;
+  count[tid] = before[tid] = 0;
   __syncthreads();
-  int e[N], at[N];
-  auto load = [&](int i0) {
+  auto load = [&](int i0, int end, int (&e)[N]) {
 #pragma unroll
     for (int r = 0; r < N; ++r) {
       const int i = i0 + r * 1024 + tid;
-      e[r] = -1;
-      if (i0 + r * 1024 >= pairs) continue;             // (scalar)
-      if (i < pairs) e[r] = ids[i];
+      e[r] = i < end ? ids[i] : -1;
       if ((unsigned)e[r] >= (unsigned)E) e[r] = -1;
     }
   };
-  const bool once = pairs <= N * 1024;                  // what a thread knows stays in its registers; else in slot_of
+  int e[N];
   for (int i0 = 0; i0 < pairs; i0 += N * 1024) {
-    load(i0);
+    load(i0, pairs, e);
 #pragma unroll
     for (int r = 0; r < N; ++r) {
-      if (i0 + r * 1024 >= pairs) break;                // (scalar)
-      at[r] = e[r] < 0 ? -1 : atomicAdd(&count[e[r]], 1);
-      const int i = i0 + r * 1024 + tid;
-      if (!once && i < pairs) p.slot_of[i] = at[r];
+      if (e[r] < 0) continue;
+      atomicAdd(&count[e[r]], 1);
+      if (i0 + r * 1024 + tid < p0) atomicAdd(&before[e[r]], 1);
     }
   }
   __syncthreads();
@@ -77,27 +74,22 @@ __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ i
     __syncthreads();
     int s0 = s - mine, b0 = b - mine_b;
     for (int q = 0; q < tid >> 6; ++q) { s0 += slots[q]; b0 += blocks[q]; }
-    first[tid] = s0;
-    for (int i = 0; i < mine_b; ++i) p.blocks[b0 + i] = Block{tid, s0 + i * block_rows, min(block_rows, c - i * block_rows), b0, mine_b};
-    if (tid == 1023) *p.n_blocks = b0 + mine_b;
+    before[tid] += s0;
+    if (blockIdx.x == 0) {
+      for (int i = 0; i < mine_b; ++i) p.blocks[b0 + i] = Block{tid, s0 + i * block_rows, min(block_rows, c - i * block_rows), b0, mine_b};
+      if (tid == 1023) *p.n_blocks = b0 + mine_b;
+    }
   }
   __syncthreads();
-  for (int i0 = 0; i0 < pairs; i0 += N * 1024) {
-    if (!once) {
-      load(i0);
-#pragma unroll
-      for (int r = 0; r < N; ++r) {
-        at[r] = -1;
-        if (i0 + r * 1024 < pairs && e[r] >= 0) at[r] = p.slot_of[i0 + r * 1024 + tid];      // (this thread's own stores)
-      }
-    }
+  for (int i0 = p0; i0 < p1; i0 += N * 1024) {
+    load(i0, p1, e);
 #pragma unroll
     for (int r = 0; r < N; ++r) {
       const int i = i0 + r * 1024 + tid;
-      if (i >= pairs) break;
-      if (e[r] >= 0) at[r] += first[e[r]];
-      p.slot_of[i] = at[r];
-      if (e[r] >= 0) p.row_of[at[r]] = i / k;
+      if (i >= p1) continue;
+      const int slot = e[r] < 0 ? -1 : atomicAdd(&before[e[r]], 1);
+      p.slot_of[i] = slot;
+      if (slot >= 0) p.row_of[slot] = i / k;
     }
   }
 }
@@ -380,9 +372,11 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   }
   const bool f32 = a.dtype == SPRINTER_F32, copy = !f32 && a.x_type != X_F16;
   const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? F32_BLOCK_ROWS : expert_tile_rows(tile);
-  const int copies = copy ? (int)std::min<long long>(1023, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
   const int blocks = pairs / block_rows + named, parts = (a.d / 4 + 255) / 256;
-  hipLaunchKernelGGL(k_experts_plan, dim3(1 + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, w.plan, (const bf16_t*)a.x, a.ldx, (uint4*)w.rows, a.T, a.d);
+  const int share = std::max(1024, ((pairs + 15) / 16 + 1023) / 1024 * 1024), plans = (pairs + share - 1) / share;       // up to 16 workgroups
+  const int copies = copy ? (int)std::min<long long>(1024, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
+  hipLaunchKernelGGL(k_experts_plan, dim3(plans + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, share, w.plan, plans, (const bf16_t*)a.x, a.ldx,
+                     (uint4*)w.rows, a.T, a.d);
   if (f32) {
     const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16;
     hipLaunchKernelGGL(k_experts_f32<true>, dim3(up * blocks), dim3(256), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan,

@@ -51,7 +51,7 @@ static void launch_pair(const ExpertTiles& e, hipStream_t s) {
 }
 
 int expert_tile_rows(int tile) {
-  static const int rows[N_EXPERT_TILES] = {256, 128, 64, 64, 32};
+  static const int rows[N_EXPERT_TILES] = {256, 128, 64, 32};
   return rows[tile];
 }
 
@@ -60,38 +60,24 @@ void launch_expert_tiles(int tile, const ExpertTiles& a, hipStream_t s) {
     case 0: launch_pair<TileL>(a, s); break;
     case 1: launch_pair<TileM>(a, s); break;
     case 2: launch_pair<TileS>(a, s); break;
-    case 3: launch_pair<TileX>(a, s); break;
     default: launch_pair<TileN>(a, s); break;
   }
 }
 
-// Per tile as for the dense products: workgroups a compute unit holds, microseconds before the first product and after the last, cycles
-// per k tile of a workgroup alone and what each further one adds, PFLOP/s on a full chip.
-struct Cost { int tm, tn, per_cu; float start_us, cycles, shared, rate; };
-static float product_us(const Cost& c, int mats, float blocks, int E, int N, int K) {
-  const int cols = c.tn / mats, Kt = (K + 31) / 32, slots = 256 * c.per_cu;
-  const float wgs = blocks * ((N + cols - 1) / cols);
-  const int full = (int)(wgs / slots), rest = (int)(wgs - (float)full * slots);
-  float cycles = full * (c.cycles + c.shared * (c.per_cu - 1)) * Kt;
-  if (rest) cycles += (c.cycles + c.shared * ((rest + 255) / 256 - 1)) * Kt;
-  const float product = 2.f * wgs * c.tm * c.tn * Kt * 32 / c.rate * 1e-9f, memory = 64.f * N * Kt * mats * E / 6.0e6f;
-  return c.start_us + std::max(cycles / 2400.f, std::max(product, memory));
-}
+// Which tile, by the rows r that an expert has in the mean.  Whole calls, us, 256 x 256 / 128 x 128 / 64 x 128 / 32 x 64:
+//   8 experts of 4096 x 14336    r = 8: - / 497 / 477 / 489   24: 654 / 513 / 497 / 565   96: 723 / 757 / 803 / 1035   1024: 2599 / 3437 / 4399 / -
+//   64 of 2048 x 1024            r = 8: - / 151 / 148 / 149   24: 181 / 168 / 161 / 171   96: 249 / 231 / 225 / 307    128: 267 / 255 / 269 / 373   256: 342 / 383 / 439 / -
+//   16 of 1024 x 2816            r = 12: - / 70 / 64 / 57     32: 121 / 78 / 70 / 68      128: 141 / 100 / 113 / 152   512: 238 / 239 / 279 / -     1024: 397 / 419 / 488 / -
+//   4 of 2048 x 8192             r = 16: - / 128 / 115 / 96   32: 218 / 131 / 115 / 106   192: 233 / 172 / 177 / 271   512: 327 / 316 / 378 / -     1024: 482 / 554 / 661 / -
+//   32 of 512 x 1344             r = 8: - / 45 / 40 / 37      96: 85 / 57 / 52 / 63       256: 112 / 83 / 88 / -       1024: 271 / 240 / 281 / -
+// The largest tile has one workgroup per compute unit, so it needs three rounds of them and a K that hides its first loads and its
+// epilogue; the second narrowest one fills its two places per compute unit from 512 workgroups on.
 int expert_tile_choice(int E, long long pairs, int d, int ff) {
-  if (const char* v = getenv("ETILE")) return atoi(v);
-  static const Cost cost[N_EXPERT_TILES] = {{256, 256, 1, 8.0f, 1355.f, 0.f, 1.22f}, {128, 128, 2, 5.4f, 608.f, 465.f, 1.10f},
-                                            {64, 128, 2, 4.2f, 478.f, 200.f, 0.83f}, {64, 64, 2, 3.7f, 327.f, 517.f, 0.64f},
-                                            {32, 64, 3, 3.4f, 290.f, 293.f, 1.23f}};
-  const int used = (int)std::min<long long>(E, pairs);
-  int best = 0;
-  float best_us = 1e30f;
-  for (int i = 0; i < N_EXPERT_TILES; ++i) {
-    // an expert's last block is half empty in the mean
-    const float blocks = std::max((float)used, (float)pairs / cost[i].tm + 0.5f * used);
-    const float us = product_us(cost[i], 2, blocks, used, ff, d) + product_us(cost[i], 1, blocks, used, d, ff);
-    if (us < best_us) { best_us = us; best = i; }
-  }
-  return best;
+  const long long used = std::min<long long>(E, pairs), r = pairs / used;
+  const long long large = (pairs / 256 + (used + 1) / 2) * ((ff + 127) / 128);         // (an expert's last row block is half empty in the mean)
+  if (r >= 80 && d >= 1024 && std::max(large, used * ((ff + 127) / 128)) >= 768) return 0;
+  if (r > 112) return 1;
+  return r <= 12 || (r <= 32 && used * ((ff + 63) / 64) <= 512) ? 3 : 2;
 }
 
 }  // namespace sprinter

@@ -8,10 +8,8 @@ namespace sprinter {
 // (max key | sum of the two best keys) stay; ids = the top_k largest keys in descending order, equal ones by index; w = p[ids], over
 // their sum if renormalised, times scale.  -inf and NaN logits cannot be taken.  A +inf logit has its limit: it shares the softmax with
 // the others like it.
-// One wave per row; lane l holds experts l, 64 + l, ...  Scores and keys are float64: which expert is taken is decided by their order, and
-// float32 scores next to each other would round onto one another (256 sigmoid scores of 16384 rows: one row in ten would tell).
-// A selection round is a maximum over the lanes of the keys' upper words (six DPP steps of one v_max each), and of the lower words where
-// more than one lane holds the upper one.
+// Scores and keys are float64: which expert is taken is decided by their order, and float32 scores next to each other would round onto
+// one another (256 sigmoid scores of 16384 rows: one row in ten would tell).
 struct RouteArgs {
   const float* logits; long long ld; const float* bias; int* ids; float* weights;
   int T, E, k, sigmoid, G, top_group, sum2, renorm, shared; float scale;
@@ -33,14 +31,6 @@ __device__ __forceinline__ unsigned wave_umax(unsigned v) {
   v = dpp_max<0x142, 0xA>(v); v = dpp_max<0x143, 0xC>(v);
   return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
-__device__ __forceinline__ u64 wave_umax64(u64 v) {
-  const unsigned hi = wave_umax((unsigned)(v >> 32));
-  const u64 at = __ballot((unsigned)(v >> 32) == hi);
-  unsigned lo;
-  if ((at & (at - 1)) == 0) lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, __builtin_ctzll(at));   // (scalar)
-  else lo = wave_umax((unsigned)(v >> 32) == hi ? (unsigned)v : 0u);
-  return ((u64)hi << 32) | lo;
-}
 __device__ __forceinline__ double read_lane(double v, int lane) {
   const u64 u = (u64)__double_as_longlong(v);
   const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
@@ -53,21 +43,120 @@ __device__ __forceinline__ double wave_sum64(double v) {
   return v;
 }
 
-template <int N>                                       // experts per lane
+// Keys of 32 bits of a float, larger integer = larger float; -inf and NaN: 0, never taken.
+__device__ __forceinline__ unsigned sortable(float v) {
+  if (!(v > -INFINITY)) return 0;
+  const unsigned u = __float_as_uint(v + 0.0f);
+  return (u >> 31) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float from_sortable(unsigned u) { return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u); }
+
+// Reductions over the 16 lanes of a row, the result in each of them
+__device__ __forceinline__ unsigned max16(unsigned v) { return dpp_max<0x140, 0xF>(dpp_max<0x141, 0xF>(dpp_max<0x4E, 0xF>(dpp_max<0xB1, 0xF>(v)))); }
+__device__ __forceinline__ u64 max16(u64 v) { return group_umax64_16(v); }
+__device__ __forceinline__ double sum16(double v) {
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) v += shfl_xor_f64(v, o);
+  return v;
+}
+// The taken keys of a row, one after the other: lane j of the row gets the j-th's value and expert (-1: there is none).
+template <typename K, int N>
+__device__ __forceinline__ void take16(K (&key)[N], int k, int lane, K& mine, int& id) {
+  mine = 0; id = -1;
+  for (int j = 0; j < k; ++j) {
+    K best = key[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) best = best > key[i] ? best : key[i];
+    best = max16(best);
+    unsigned last = 0;                                 // ~ the lowest index of the largest key
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) last = key[i] == best ? ~(unsigned)(i * 16 + lane) : last;
+    const unsigned e = ~max16(last);
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = (unsigned)(i * 16 + lane) == e ? 0 : key[i];
+    if (lane == j && best) { mine = best; id = (int)e; }
+  }
+}
+
+// Without bias and groups, up to 256 experts and 16 of them: four rows per wave, 16 lanes each; lane l of a row holds experts l, 16 + l, ...
+// The scores rise with the logits, so the logits themselves are the keys, and only what is taken needs its exponential (and, unless the
+// weights are renormalised, the sum of the softmax all of them).  Where float64 scores meet although their logits do not - under- and
+// overflow - the wave takes the scores for keys, as the definition does.
+// What bounds it: the instructions of the selection rounds, about 45 for four rows (a row per wave: 50 for one).
+template <int N>
+__global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
+  const int lane = threadIdx.x & 15;
+  const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const bool live = row < a.T;
+  const float* __restrict__ l = a.logits + (live ? row : 0) * a.ld;
+  float x[N];
+  unsigned key[N], top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = l[min(i * 16 + lane, a.E - 1)];
+  float low = INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    key[i] = i * 16 + lane < a.E ? sortable(x[i]) : 0;
+    top = max(top, key[i]);
+    low = key[i] ? fminf(low, x[i]) : low;
+  }
+  top = max16(top);
+  const float most = from_sortable(top);               // (no expert at all: never used)
+  auto score = [&](float v) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : v == most ? 1.0 : exp((double)v - (double)most); };
+  float mine;
+  int id;
+  if (__ballot(top && (a.sigmoid ? most > 16.f || low < -700.f : !(most - low < 700.f)))) {
+    u64 wide[N], value;
+#pragma unroll
+    for (int i = 0; i < N; ++i) wide[i] = key[i] ? sortable(score(x[i])) : 0;
+    take16(wide, a.k, lane, value, id);
+    mine = l[max(id, 0)];
+  } else {
+    unsigned value, left[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) left[i] = key[i];
+    take16(left, a.k, lane, value, id);
+    mine = from_sortable(value);
+  }
+  double w = lane < a.k && id >= 0 ? score(mine) : 0.0;
+  if (a.renorm) {
+    const double total = sum16(w);
+    w = total > 0.0 ? w / total : 0.0;
+  } else if (!a.sigmoid) {
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += key[i] ? score(x[i]) : 0.0;
+    sum = sum16(sum);
+    w = id >= 0 ? w / sum : 0.0;
+  }
+  w *= (double)a.scale;
+  const int n_out = a.k + a.shared;
+  if (lane >= a.k) { id = a.E + lane - a.k; w = 1.0; }
+  if (live && lane < n_out) {
+    a.ids[row * n_out + lane] = id;
+    a.weights[row * n_out + lane] = (float)w;
+  }
+}
+
+// Every other case: one wave per row; lane l holds experts l, 64 + l, ...  A selection round looks at the keys' upper words, and at the
+// lower ones where more than one key has the largest upper word.
+template <int N>
 __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long long row = (long long)blockIdx.x * 4 + wave_index();
-  if (row >= a.T) return;                              // (scalar; no barrier below)
+  __shared__ u64 keys[4][N * 64];
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  const long long row = (long long)blockIdx.x * 4 + wave;
+  if (row >= a.T) return;                              // (scalar; no barrier below: a wave has its keys in LDS for itself)
   const float* __restrict__ l = a.logits + row * a.ld;
   float x[N];
   double p[N], bias[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int e = i * 64 + lane, c = min(e, a.E - 1);
+    const int c = min(i * 64 + lane, a.E - 1);
     x[i] = l[c];
     bias[i] = a.bias ? (double)a.bias[c] : 0.0;
-    if (e >= a.E || !(x[i] > -INFINITY)) x[i] = -INFINITY;             // (NaN too)
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) if (i * 64 + lane >= a.E || !(x[i] > -INFINITY)) x[i] = -INFINITY;       // (NaN too)
   if (a.sigmoid) {
 #pragma unroll
     for (int i = 0; i < N; ++i) p[i] = 1.0 / (1.0 + exp(-(double)x[i]));
@@ -94,56 +183,65 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     key[i] = x[i] > -INFINITY && v > -INFINITY ? sortable(v) : 0;
   }
   if (a.G > 1) {                                       // (uniform)
-    // each group's rank in lane g, in sortable order; a group's experts lie in up to E / G lanes of up to N registers
-    const int per = a.E / a.G;
-    u64 rank = 0;
-    for (int g = 0; g < a.G; ++g) {
-      u64 best = 0, second = 0;
+    // 64 / (G rounded up to a power of two) lanes per group find its two best keys
+    const int per = a.E / a.G, wide = a.G == 1 ? 1 : 1 << (32 - __clz(a.G - 1)), lanes = 64 / wide, g = lane / lanes, s = lane % lanes;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const u64 v = (i * 64 + lane) / per == g ? key[i] : 0;
+    for (int i = 0; i < N; ++i) keys[wave][i * 64 + lane] = key[i];
+    __builtin_amdgcn_wave_barrier();                   // (LDS operations of one wave complete in order)
+    u64 best = 0, second = 0;
+    if (g < a.G)
+      for (int c = s; c < per; c += lanes) {
+        const u64 v = keys[wave][g * per + c];
         second = umax64(second, min(best, v));
         best = umax64(best, v);
       }
-      const u64 m = wave_umax64(best);
-      u64 value = m;
-      if (a.sum2 && m) {
-        // one lane gives up its best; the rest keep theirs
-        const u64 at = __ballot(best == m);
-        const u64 s = wave_umax64(lane == __builtin_ctzll(at) ? second : best);
-        auto back = [](u64 v) { return __longlong_as_double((long long)((v >> 63) ? (v & 0x7fffffffffffffffull) : ~v)); };
-        value = sortable(back(m) + (s ? back(s) : 0.0));
-      }
-      if (lane == g) rank = value;
+    for (int o = 1; o < lanes; o <<= 1) {
+      const u64 ob = shfl_xor_u64(best, o), os = shfl_xor_u64(second, o);
+      second = umax64(umax64(second, os), min(best, ob));
+      best = umax64(best, ob);
     }
-    u64 taken = 0;                                     // a bit per group
-    for (int j = 0; j < a.top_group; ++j) {
-      const u64 m = wave_umax64(rank);
-      if (m == 0) break;
-      const int g = __builtin_ctzll(__ballot(rank == m));
-      taken |= 1ull << g;
-      if (lane == g) rank = 0;
+    auto back = [](u64 v) { return __longlong_as_double((long long)((v >> 63) ? (v & 0x7fffffffffffffffull) : ~v)); };
+    u64 rank = best;
+    if (a.sum2 && best && second) rank = sortable(back(best) + back(second));
+    // a group is taken if fewer than top_group are ahead of it
+    int ahead = 0;
+    for (int q = 0; q < a.G; ++q) {
+      const u64 other = ((u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(rank >> 32), q * lanes) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)rank, q * lanes);
+      ahead += other > rank || (other == rank && q < g);
     }
+    const u64 taken = __ballot(g < a.G && ahead < a.top_group);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (!(taken >> min((i * 64 + lane) / per, 63) & 1)) key[i] = 0;
+    for (int i = 0; i < N; ++i) {
+      const int mine = (i * 64 + lane) / per;
+      if (!(taken >> (min(mine, a.G - 1) * lanes) & 1)) key[i] = 0;
+    }
   }
   const int n_out = a.k + a.shared;
   int id = lane < a.k ? -1 : a.E + lane - a.k;         // lane j: the row's j-th id and weight
   double w = lane < a.k ? 0.0 : 1.0, total = 0.0;
   for (int j = 0; j < a.k; ++j) {
-    u64 best = key[0];
+    unsigned hi = (unsigned)(key[0] >> 32);
 #pragma unroll
-    for (int i = 1; i < N; ++i) best = umax64(best, key[i]);
-    const u64 m = wave_umax64(best);
-    if (m == 0) break;                                 // (scalar)
-    int e = -1;
+    for (int i = 1; i < N; ++i) hi = max(hi, (unsigned)(key[i] >> 32));
+    hi = wave_umax(hi);
+    if (hi == 0) break;                                // (scalar)
+    u64 at[N];
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { at[i] = __ballot((unsigned)(key[i] >> 32) == hi); n += __popcll(at[i]); }
+    if (n > 1) {                                       // (scalar)
+      unsigned lo = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) if ((unsigned)(key[i] >> 32) == hi) lo = max(lo, (unsigned)key[i]);
+      lo = wave_umax(lo);
+#pragma unroll
+      for (int i = 0; i < N; ++i) at[i] = __ballot((unsigned)(key[i] >> 32) == hi && (unsigned)key[i] == lo);
+    }
+    int e = -1, place = 0;
     double pe = 0.0;
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i) {                 // the lowest index of the largest
-      const u64 at = __ballot(key[i] == m);
-      if (at) { const int at_lane = __builtin_ctzll(at); e = i * 64 + at_lane; pe = read_lane(p[i], at_lane); }
-    }
+    for (int i = N - 1; i >= 0; --i)                   // the lowest index of the largest
+      if (at[i]) { place = __builtin_ctzll(at[i]); e = i * 64 + place; pe = read_lane(p[i], place); }
 #pragma unroll
     for (int i = 0; i < N; ++i) if (i * 64 + lane == e) key[i] = 0;
     if (lane == j) { id = e; w = pe; }
@@ -176,6 +274,13 @@ void launch_route(const sprinter_route_cfg& c, const float* logits, long long ld
                   hipStream_t s) {
   const RouteArgs a{logits, ld, bias, ids, weights, n_rows, c.n_expert, c.top_k, c.score == SPRINTER_SCORE_SIGMOID, c.n_group, c.top_group,
                     c.group_score == SPRINTER_GROUP_BEST_TWO, c.renormalize != 0, c.n_shared, c.scale};
+  if (!bias && c.n_group == 1 && c.n_expert <= 256 && c.top_k + c.n_shared <= 16) {
+    const dim3 grid((n_rows + 15) / 16), block(256);
+    if (c.n_expert <= 16) hipLaunchKernelGGL(k_route_plain<1>, grid, block, 0, s, a);
+    else if (c.n_expert <= 64) hipLaunchKernelGGL(k_route_plain<4>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(k_route_plain<16>, grid, block, 0, s, a);
+    return;
+  }
   const dim3 grid((n_rows + 3) / 4), block(256);
   if (c.n_expert <= 64) hipLaunchKernelGGL(k_route<1>, grid, block, 0, s, a);
   else if (c.n_expert <= 128) hipLaunchKernelGGL(k_route<2>, grid, block, 0, s, a);

@@ -30,32 +30,45 @@ class BlockNormCfgC(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "kind", "d")] + [("eps", C.c_float), ("scale", C.c_float)]
 
 
+# (the raw handle: a torch.cuda.Stream object takes longer to make than the smallest kernels run)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _call(name, device, *args):
     """One entry point on `device` and its current stream (the last argument of them all)."""
-    lib = load_library()
-    fn = getattr(lib, name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        rc = getattr(_lib or _load(), name)(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+            rc = getattr(_lib or _load(), name)(*args, _raw_stream(index))
     if rc != 0:
-        raise SprinterError(rc, lib.sprinter_last_error(None).decode())
+        raise SprinterError(rc, _lib.sprinter_last_error(None).decode())
+
+
+_lib = None
+
+
+def _load():
+    global _lib
+    _lib = load_library()
+    return _lib
 
 
 def _tensor(name, t, device, dtype, shape, contiguous=False):
     """Checks one argument: shape with None for any size; rows may lie apart unless contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
-    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    have = t.shape
+    if len(have) != len(shape) or any(w is not None and w != n for w, n in zip(shape, have)):
+        raise ValueError(f"{name}: shape {tuple(have)}, expected {shape}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: gradients are not computed here; detach it")
-    if contiguous:
-        if not t.is_contiguous():
+    if not t.is_contiguous():
+        if contiguous:
             raise ValueError(f"{name}: not contiguous")
-    elif t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: the elements of a row are not adjacent")
+        if have[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: the elements of a row are not adjacent")
 
 
 def _device(t, name):
