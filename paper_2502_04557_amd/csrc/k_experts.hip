@@ -127,52 +127,43 @@ __device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int la
   return at * 32 + __builtin_ctz(word);
 }
 
-// A workgroup: one expert's NTW column tiles of both matrices.  The 8 waves share K; each thread then finishes the elements of one row
-// and column in each tile.
-template <int NTW>
+// A workgroup: one expert's column tile of both matrices.  The 8 waves share K; 256 threads then finish an element each.  What bounds it: the
+// weights, at 6.0 - 6.4 TB/s (two column tiles per workgroup: 5.5; eight k tiles in flight per wave for four: as many or less).
 __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
-                                                        int T, int k, int E, int d, int ff, long long ldx, int x_type, int groups, uint4* hidden) {
+                                                        int T, int k, int E, int d, int ff, long long ldx, int x_type, int col_tiles, uint4* hidden) {
   constexpr int U = 4;
   __shared__ NamedExperts named;
-  __shared__ float red[8][NTW * 2][4][64], row_w[FEW_ROWS];
+  __shared__ float red[8][2][4][64], row_w[FEW_ROWS];
   __shared__ int row_hit[FEW_ROWS];
   const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
-  const int j = blockIdx.x / groups, nt0 = (blockIdx.x - j * groups) * NTW;
+  const int j = blockIdx.x / col_tiles, nt = blockIdx.x - j * col_tiles;
   name_experts(named, ids, T * k, E);
   const int e = named_expert(named, j, lane);
   if (e < 0) return;
   const int Kt = (d + 31) >> 5, Nt = (ff + 15) >> 4, row = lane & 15, oct = (lane >> 4) * 8;
-  const uint4* Wg = (const uint4*)wg + (size_t)e * Nt * Kt * 64 + lane;
-  const uint4* Wu = (const uint4*)wu + (size_t)e * Nt * Kt * 64 + lane;
+  const size_t tile = ((size_t)e * Nt + min(nt, Nt - 1)) * Kt * 64 + lane;      // (the column tile behind the last one of an odd count: zeros)
+  const uint4 *Wg = (const uint4*)wg + tile, *Wu = (const uint4*)wu + tile;
   const bf16_t* x = (const bf16_t*)x_ + (size_t)min(row, T - 1) * ldx;
-  f32x4 g[NTW], u[NTW];
-#pragma unroll
-  for (int n = 0; n < NTW; ++n) g[n] = u[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
   for (int kt = w; kt < Kt; kt += 8 * U) {
-    uint4 a[U][NTW], b[U][NTW], v[U];
+    uint4 a[U], b[U], v[U];
 #pragma unroll
     for (int q = 0; q < U; ++q) {
       const int kc = min(kt + q * 8, Kt - 1);
-#pragma unroll
-      for (int n = 0; n < NTW; ++n) {
-        const size_t at = ((size_t)min(nt0 + n, Nt - 1) * Kt + kc) * 64;
-        a[q][n] = Wg[at]; b[q][n] = Wu[at];
-      }
+      a[q] = Wg[(size_t)kc * 64]; b[q] = Wu[(size_t)kc * 64];
       v[q] = make_uint4(0u, 0u, 0u, 0u);
       if (row < T && kt + q * 8 < Kt && kc * 32 + oct < d) v[q] = *reinterpret_cast<const uint4*>(x + kc * 32 + oct);
     }
 #pragma unroll
     for (int q = 0; q < U; ++q) {
       const uint4 h = x_type == X_BF16 ? as_f16(v[q]) : v[q];
-#pragma unroll
-      for (int n = 0; n < NTW; ++n) { g[n] = mfma_f16(h, a[q][n], g[n]); u[n] = mfma_f16(h, b[q][n], u[n]); }
+      g = mfma_f16(h, a[q], g);
+      u = mfma_f16(h, b[q], u);
     }
   }
 #pragma unroll
-  for (int n = 0; n < NTW; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { red[w][2 * n][i][lane] = g[n][i]; red[w][2 * n + 1][i][lane] = u[n][i]; }
-  {                                                     // 32 threads to a row
+  for (int i = 0; i < 4; ++i) { red[w][0][i][lane] = g[i]; red[w][1][i][lane] = u[i]; }
+  {                                                     // the rows' weights for this expert: 32 threads to a row
     const int m = tid >> 5;
     float s = 0.f;
     int hit = 0;
@@ -184,14 +175,13 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
     if ((tid & 31) == 0) { row_w[m] = s; row_hit[m] = hit; }
   }
   __syncthreads();
-  bf16_t* out = (bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64);
-  for (int o = tid; o < NTW * 256; o += 512) {          // (row m, column c), in the order of the operand tile
-    const int m = (o >> 3) & 15, c = (o >> 7) * 8 + (o & 7), n = nt0 * 16 + c, i = m & 3, at = (m >> 2) * 16 + (c & 15);
-    float gs = 0.f, us = 0.f;
+  if (tid >= 256) return;
+  // (row m, column c), in the order of the operand tile
+  const int m = (tid >> 3) & 15, c = (tid >> 7) * 8 + (tid & 7), n = nt * 16 + c, i = m & 3, at = (m >> 2) * 16 + c;
+  float gs = 0.f, us = 0.f;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) { gs += red[q][2 * (c >> 4)][i][at]; us += red[q][2 * (c >> 4) + 1][i][at]; }
-    if (n < round_up(ff, 32)) act_store<bf16_t>(out, m, n, ff, row_hit[m] && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
-  }
+  for (int q = 0; q < 8; ++q) { gs += red[q][0][i][at]; us += red[q][1][i][at]; }
+  act_store<bf16_t>((bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64), m, n, ff, row_hit[m] && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
 }
 
 // A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.
@@ -264,38 +254,61 @@ __device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
   const f32x4 v = *reinterpret_cast<const f32x4*>(row + min(k, K - 4));
   return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
-constexpr int F32_BLOCK_ROWS = 16;
-
-// Sum of the four waves' accumulators
-__device__ __forceinline__ f32x4 join(f32x4 v, f32x4 (*red)[64], int w, int lane) {
-  red[w][lane] = v;
-  __syncthreads();
-  const f32x4 s = ((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane];
-  __syncthreads();
-  return s;
-}
-
-// A workgroup: one column tile (of col_tiles) of one row block.  Four waves share K.  up: out = silu(Wg x) * (Wu x) of the gathered rows.
-template <bool UP>
-__global__ __launch_bounds__(256) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out, int col_tiles) {
-  __shared__ f32x4 red[4][64];
+// A workgroup: one column tile (of col_tiles) of one row block of MT row tiles.  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
+// gathered rows.  MT = 4 from 17 rows an expert on: the weights are fetched once for 64 rows.
+template <bool UP, int MT>
+__global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out, int col_tiles) {
+  constexpr int U = MT == 1 ? 4 : 2, MATS = UP ? 2 : 1;
+  __shared__ f32x4 red[8][MT * MATS][64];
   const int lane = threadIdx.x & 63, w = wave_index(), id = blockIdx.x / col_tiles, nt = blockIdx.x - id * col_tiles;
   if (id >= *p.n_blocks) return;
   const Block b = p.blocks[id];
-  const int slot = b.slot + min(lane & 15, b.rows - 1);
-  const float* x = X + (UP ? p.row_of[slot] : slot) * ldx;
-  const size_t at = ((size_t)b.expert * N + min(nt * 16 + (lane & 15), N - 1)) * K;
-  f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
-  for (int kt = w; kt < (K + 15) >> 4; kt += 4) {
-    const int k = kt * 16 + (lane >> 4) * 4;
-    const f32x4 v = load4(x, k, K);
-    g = product(v, load4(W + at, k, K), g);
-    if (UP) u = product(v, load4(W2 + at, k, K), u);
+  const float* x[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int slot = b.slot + min(m * 16 + (lane & 15), b.rows - 1);
+    x[m] = X + (UP ? p.row_of[slot] : slot) * ldx;
   }
-  g = join(g, red, w, lane);
-  if (UP) u = join(u, red, w, lane);
-  const int n = nt * 16 + (lane & 15), m = (lane >> 4) * 4 + w;        // each wave finishes one of the four rows of a lane
-  if (m < b.rows && n < N) out[(size_t)(b.slot + m) * N + n] = UP ? silu(g[w]) * u[w] : g[w];
+  const size_t at = ((size_t)b.expert * N + min(nt * 16 + (lane & 15), N - 1)) * K;
+  f32x4 acc[MT][MATS];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int q = 0; q < MATS; ++q) acc[m][q] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int kt = w; kt < (K + 15) >> 4; kt += 8 * U) {
+    f32x4 wv[U][MATS], xv[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = (kt + u * 8) * 16 + (lane >> 4) * 4;               // (behind K: zeros)
+      wv[u][0] = load4(W + at, k, K);
+      if (UP) wv[u][MATS - 1] = load4(W2 + at, k, K);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xv[u][m] = load4(x[m], k, K);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int q = 0; q < MATS; ++q) acc[m][q] = product(xv[u][m], wv[u][q], acc[m][q]);
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int q = 0; q < MATS; ++q) red[w][m * MATS + q][lane] = acc[m][q];
+  __syncthreads();
+  // (row, column) of the block, one after the other; lane 16 (row / 4) + column holds four rows
+  for (int o = threadIdx.x; o < MT * 256; o += 512) {
+    const int m = o >> 4, n = nt * 16 + (o & 15), tile = (m >> 4) * MATS, from = ((m & 15) >> 2) * 16 + (o & 15), i = m & 3;
+    if (m >= b.rows || n >= N) continue;
+    float g = 0.f, u = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      g += red[q][tile][from][i];
+      if (UP) u += red[q][tile + MATS - 1][from][i];
+    }
+    out[(size_t)(b.slot + m) * N + n] = UP ? silu(g) * u : g;
+  }
 }
 
 // --------------------------------------------------------------------------------------------------------------- combine
@@ -323,8 +336,9 @@ void launch_pack_experts(const void* w, void* out, int E, int N, int K, hipStrea
 
 namespace {
 bool few(int dtype, long long T) { return dtype == SPRINTER_BF16 && T <= FEW_ROWS; }
-// Shares of the K of down_few: one workgroup per compute unit and more.
-int few_shares(int d) { return std::max(1, 512 / ((d + 15) / 16)); }
+// Shares of the K of down_few: a workgroup per compute unit.  us, 1 / 2 / 4 shares with the launch that joins them: 2 experts of 4096 x 14336
+// 42 / 45 / 45, 56 of 2048 x 1024 (half as many column tiles) 65 / 45 / 46.
+int few_shares(int d) { const int tiles = (d + 15) / 16; return (256 + tiles - 1) / tiles; }
 
 struct Space {
   Plan plan; int slots, blocks; void *rows, *hidden; float* out; size_t bytes;
@@ -361,17 +375,16 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   const Space w = space(workspace, a.dtype, a.E, a.d, a.ff, a.T, a.k);
   const int pairs = a.T * a.k, named = std::min(a.E, pairs);
   if (few(a.dtype, a.T)) {
-    constexpr int NTW = 2;
-    const int groups = ((a.ff + 15) / 16 + NTW - 1) / NTW, Nt = (a.d + 15) / 16, shares = few_shares(a.d);
-    hipLaunchKernelGGL(k_experts_up_few<NTW>, dim3(named * groups), dim3(512), 0, s, a.wg, a.wu, a.x, a.ids, a.weights, a.T, a.k, a.E, a.d, a.ff, a.ldx, a.x_type,
-                       groups, (uint4*)w.hidden);
+    const int up = (a.ff + 31) / 32 * 2, Nt = (a.d + 15) / 16, shares = few_shares(a.d);
+    hipLaunchKernelGGL(k_experts_up_few, dim3(named * up), dim3(512), 0, s, a.wg, a.wu, a.x, a.ids, a.weights, a.T, a.k, a.E, a.d, a.ff, a.ldx, a.x_type, up,
+                       (uint4*)w.hidden);
     hipLaunchKernelGGL(k_experts_down_few, dim3(Nt * shares), dim3(512), 0, s, a.w2, (const uint4*)w.hidden, a.ids, a.T, a.k, a.E, a.d, a.ff, shares, w.out, a.y, a.y_type, a.ldy);
     if (shares > 1)
       hipLaunchKernelGGL(k_experts_join, dim3(a.T * ((a.d + 255) / 256)), dim3(256), 0, s, w.out, shares, a.T, a.d, a.y, a.y_type, a.ldy);
     return;
   }
   const bool f32 = a.dtype == SPRINTER_F32, copy = !f32 && a.x_type != X_F16;
-  const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? F32_BLOCK_ROWS : expert_tile_rows(tile);
+  const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? (pairs > 16 * named ? 64 : 16) : expert_tile_rows(tile);
   const int blocks = pairs / block_rows + named, parts = (a.d / 4 + 255) / 256;
   const int share = std::max(1024, ((pairs + 15) / 16 + 1023) / 1024 * 1024), plans = (pairs + share - 1) / share;       // up to 16 workgroups
   const int copies = copy ? (int)std::min<long long>(1024, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
@@ -379,10 +392,13 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
                      (uint4*)w.rows, a.T, a.d);
   if (f32) {
     const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16;
-    hipLaunchKernelGGL(k_experts_f32<true>, dim3(up * blocks), dim3(256), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan,
-                       (float*)w.hidden, up);
-    hipLaunchKernelGGL(k_experts_f32<false>, dim3(down * blocks), dim3(256), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, w.plan,
-                       w.out, down);
+#define SPRINTER_EXPERTS_F32(MT) \
+    hipLaunchKernelGGL((k_experts_f32<true, MT>), dim3(up * blocks), dim3(512), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan, \
+                       (float*)w.hidden, up); \
+    hipLaunchKernelGGL((k_experts_f32<false, MT>), dim3(down * blocks), dim3(512), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, \
+                       w.plan, w.out, down)
+    if (block_rows == 16) { SPRINTER_EXPERTS_F32(1); } else { SPRINTER_EXPERTS_F32(4); }
+#undef SPRINTER_EXPERTS_F32
   } else {
     launch_expert_tiles(tile, ExpertTiles{w.plan, blocks, w.slots, a.E, a.d, a.ff, a.wg, a.wu, a.w2, copy ? w.rows : a.x,
                                           copy ? (long long)round_up(a.d, 32) * 2 : a.ldx * 2, w.hidden, w.out}, s);
