@@ -66,6 +66,9 @@ enum {
 enum { SPRINTER_ARCH_GPT = 0, SPRINTER_ARCH_LLAMA = 1 };
 enum { SPRINTER_F32 = 0, SPRINTER_BF16 = 1 };
 enum { SPRINTER_DRAFT = 0, SPRINTER_TARGET = 1, SPRINTER_VERIFIER = 2 };
+enum { SPRINTER_SCORE_SOFTMAX = 0, SPRINTER_SCORE_SIGMOID = 1 };
+enum { SPRINTER_GROUP_MAX = 0, SPRINTER_GROUP_BEST_TWO = 1 };
+enum { SPRINTER_NORM_LAYER = 0, SPRINTER_NORM_RMS = 1 };
 
 /* One decoder-only transformer.
  *   arch 0 (GPT family)  : pre-LN LayerNorm, biases on all linear maps, tanh-GELU
@@ -185,6 +188,38 @@ int sprinter_workspace_bytes(const sprinter_cfg* cfg, size_t* out_bytes);
 int sprinter_create(const sprinter_cfg* cfg, void* dev_workspace, size_t workspace_bytes,
                     void* hip_stream, sprinter_ctx** out_ctx);
 
+/* A decoder block with more around and inside it than sprinter_model_cfg describes (SPRINTER_ARCH_LLAMA only):
+ *   h += residual_scale * gate1 * post1(attention(norm1(h)));  h += residual_scale * gate2 * post2(ffn(norm2(h)))
+ *   route.n_expert  0: ffn is the dense SwiGLU of d_ff; else a set of experts of hidden width d_expert (a multiple of
+ *                   8; d_ff is then not used): the logits W_r norm2(h) are routed as route says (sprinter_route), and
+ *                   ffn is the weighted sum of the experts taken and of route.n_shared shared ones (sprinter_experts)
+ *   route_bias      1: the keys have a bias per expert
+ *   post_norm       1: RMSNorm on what attention and ffn return (post1, post2); 0: neither
+ *   gate            1: a gain per column on both (gate1, gate2); 0: neither
+ *   residual_scale  1 for the plain residual stream
+ * A zeroed struct with residual_scale 1 is the block of sprinter_create.  Further weights of such a model, per layer i:
+ * "l<i>.router" [n_expert, d], "l<i>.router.b" [n_expert] (route_bias), "l<i>.wg" and "l<i>.wu" [n_expert + n_shared,
+ * d_expert, d], "l<i>.w2" [n_expert + n_shared, d, d_expert], "l<i>.post1.g" and "l<i>.post2.g" [d] (post_norm),
+ * "l<i>.gate1" and "l<i>.gate2" [d] (gate).  In bf16 mode the router's product takes float16 operands like the others:
+ * experts whose keys lie closer than its rounding may change places. */
+typedef struct {
+  int32_t n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared;
+  float scale;
+} sprinter_route_cfg;   /* (the fields are described at sprinter_route) */
+typedef struct {
+  sprinter_route_cfg route;
+  int32_t d_expert, route_bias, post_norm, gate;
+  float residual_scale;
+} sprinter_block_cfg;
+
+/* sprinter_workspace_bytes and sprinter_create for models whose blocks are described by a sprinter_block_cfg (NULL: as
+ * sprinter_create).  Everything else of the context is the same. */
+int sprinter_blocks_workspace_bytes(const sprinter_cfg* cfg, const sprinter_block_cfg* draft_blocks,
+                                    const sprinter_block_cfg* target_blocks, size_t* out_bytes);
+int sprinter_create_blocks(const sprinter_cfg* cfg, const sprinter_block_cfg* draft_blocks,
+                           const sprinter_block_cfg* target_blocks, void* dev_workspace, size_t workspace_bytes,
+                           void* hip_stream, sprinter_ctx** out_ctx);
+
 /* sprinter_create for callers that cannot allocate device memory at all (code that runs while a
  * HIP graph is being captured elsewhere in the process, tight serving loops, harnesses that forbid
  * hipMalloc): the workspace is a static array inside the library, SPRINTER_STATIC_WORKSPACE_BYTES
@@ -303,24 +338,16 @@ int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* hos
  * all of them can be recorded into a HIP graph.  Errors as above, with the text in sprinter_last_error(NULL); a call
  * that is refused enqueues nothing. */
 
-enum { SPRINTER_SCORE_SOFTMAX = 0, SPRINTER_SCORE_SIGMOID = 1 };
-enum { SPRINTER_GROUP_MAX = 0, SPRINTER_GROUP_BEST_TWO = 1 };
-enum { SPRINTER_NORM_LAYER = 0, SPRINTER_NORM_RMS = 1 };
-
-/* Routing of a row: scores p = softmax(logits) or sigmoid(logits), keys p + bias (the bias only decides who is taken).
+/* Routing of a row (sprinter_route_cfg): scores p = softmax(logits) or sigmoid(logits), keys p + bias (the bias only decides who is taken).
  *   n_group     1: no groups; else the experts form n_group runs of n_expert / n_group, and only those of the
  *               top_group runs with the largest key (SPRINTER_GROUP_MAX) or the largest sum of their two best keys
  *               (SPRINTER_GROUP_BEST_TWO) can be taken
  *   top_k       experts taken, largest key first, equal keys by index
  *   renormalize 1: the weights are p / (sum of the taken p); 0: p itself.  Either times scale.
  *   n_shared    appends the ids n_expert, n_expert + 1, ... with a weight of 1 (shared experts behind the routed ones)
- * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16. */
-typedef struct {
-  int32_t n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared;
-  float scale;
-} sprinter_route_cfg;
-
-/* ids and weights [n_rows, top_k + n_shared] of logits [n_rows, n_expert] (float32; rows ld_logits apart).  dev_bias
+ * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16.
+ *
+ * ids and weights [n_rows, top_k + n_shared] of logits [n_rows, n_expert] (float32; rows ld_logits apart).  dev_bias
  * [n_expert] or NULL.  An expert whose logit is -inf or NaN is never taken; where fewer than top_k are left (a row may
  * have none) the remaining ids are -1 with weight 0.  Scores, keys and their sums are held in 64 bits. */
 int sprinter_route(const sprinter_route_cfg* cfg, const float* dev_logits, int64_t ld_logits, const float* dev_bias,

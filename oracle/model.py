@@ -13,6 +13,10 @@ written out here from their public definitions:
           separate LM head)
   Attn  : causal softmax(Q K^T / sqrt(d_h)) V followed by the output projection.
 
+A LLaMA model's cfg.blocks (None: the above) describes more of a block:
+  h += s * gate1 * RMS(attention part; post1) ; h += s * gate2 * RMS(feed-forward part; post2)   (gates and post-norms optional)
+  feed-forward part = sum over the experts that the row's router takes of weight * W2 (silu(Wg x) * Wu x), and the shared experts'.
+
 Two evaluation routes are given and tested against each other: `forward_full`
 (whole sequence, no cache) and `step` (one token per row against that row's cache).
 A cache entry stores the position id it was written with, so a cache whose
@@ -72,6 +76,30 @@ def attend(q, K, V):
         p /= p.sum()
         out[h] = p @ v
     return out
+
+
+def take_experts(logits, b, bias=None):
+    """The experts a row takes and their weights.  Scores p = softmax or sigmoid of the logits; the keys p + bias decide: of the
+    n_group runs of experts only the top_group with the largest key (or sum of their two best) stay, then the top_k largest
+    keys, equal ones by index.  Weights: p, over their sum if renormalised, times route_scale."""
+    logits = np.asarray(logits, np.float64)
+    if b.score == "softmax":
+        p = np.exp(logits - logits.max())
+        p /= p.sum()
+    else:
+        p = 1.0 / (1.0 + np.exp(-logits))
+    key = p if bias is None else p + bias
+    if b.n_group > 1:
+        best = -np.sort(-key.reshape(b.n_group, -1), axis=1)
+        rank = best[:, 0] if b.group_score == "max" else best[:, :2].sum(axis=1)
+        out = np.argsort(-rank, kind="stable")[b.top_group:]
+        key = key.copy()
+        key.reshape(b.n_group, -1)[out] = -np.inf
+    ids = np.argsort(-key, kind="stable")[:b.top_k]
+    w = p[ids]
+    if b.renormalize:
+        w = w / w.sum()
+    return ids, w * b.route_scale
 
 
 class KVCache:
@@ -137,7 +165,29 @@ class Decoder:
         y = a.reshape(a.shape[0], -1) @ self.w[p + "wo"].T
         if self.cfg.arch == ARCH_GPT:
             y = y + self.w[p + "bo"]
-        return h + y
+        return h + self._returned(i, y, 1)
+
+    def _returned(self, i, y, n):
+        """What attention (n = 1) or feed-forward (2) adds to the residual stream."""
+        b, p = getattr(self.cfg, "blocks", None), f"l{i}."
+        if b is None:
+            return y
+        if b.post_norm:
+            y = rms_norm(y, self.w[p + f"post{n}.g"], self.cfg.norm_eps)
+        if b.gate:
+            y = self.w[p + f"gate{n}"] * y
+        return b.residual_scale * y
+
+    def _experts(self, i, xn):
+        b, p = self.cfg.blocks, f"l{i}."
+        w = self.w
+        out = np.zeros_like(xn)
+        for r in range(xn.shape[0]):
+            ids, weights = take_experts(w[p + "router"] @ xn[r], b, w.get(p + "router.b"))
+            for e, wt in zip(list(ids) + list(range(b.n_expert, b.n_expert + b.n_shared)), list(weights) + [1.0] * b.n_shared):
+                m = silu(w[p + "wg"][e] @ xn[r]) * (w[p + "wu"][e] @ xn[r])
+                out[r] += wt * (w[p + "w2"][e] @ m)
+        return out
 
     def _ffn(self, i, h):
         p = f"l{i}."
@@ -145,8 +195,10 @@ class Decoder:
         if self.cfg.arch == ARCH_GPT:
             m = gelu_tanh(xn @ self.w[p + "w1"].T + self.w[p + "b1"])
             return h + m @ self.w[p + "w2"].T + self.w[p + "b2"]
+        if getattr(self.cfg, "blocks", None) and self.cfg.blocks.n_expert:
+            return h + self._returned(i, self._experts(i, xn), 2)
         m = silu(xn @ self.w[p + "wg"].T) * (xn @ self.w[p + "wu"].T)
-        return h + m @ self.w[p + "w2"].T
+        return h + self._returned(i, m @ self.w[p + "w2"].T, 2)
 
     def _head(self, h):
         hf = self._norm(h, "normf")

@@ -15,8 +15,11 @@ LIB_PATH = os.path.join(_PKG, "libsprinter.so")
 
 DRAFT, TARGET, VERIFIER = 0, 1, 2
 F32, BF16 = 0, 1
+SCORES = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORES = {"max": 0, "sum2": 1}
 
-EXPORTS = ("sprinter_workspace_bytes", "sprinter_create", "sprinter_create_static", "sprinter_load_weights", "sprinter_prefill",
+EXPORTS = ("sprinter_workspace_bytes", "sprinter_create", "sprinter_create_static", "sprinter_blocks_workspace_bytes",
+           "sprinter_create_blocks", "sprinter_load_weights", "sprinter_prefill",
            "sprinter_step", "sprinter_generate", "sprinter_sd_generate", "sprinter_set_tau", "sprinter_get_stats",
            "sprinter_route", "sprinter_experts_bytes", "sprinter_experts_pack", "sprinter_experts", "sprinter_block_norm",
            "sprinter_destroy", "sprinter_last_error")
@@ -32,6 +35,16 @@ class CfgC(C.Structure):
                 ("dtype", C.c_int32), ("max_batch", C.c_int32), ("max_seq", C.c_int32), ("tau", C.c_float),
                 ("temperature", C.c_float), ("seed", C.c_uint64), ("target_ctx_mode", C.c_int32),
                 ("reject_mode", C.c_int32), ("sd_gamma", C.c_int32), ("chunk_rows", C.c_int32)]
+
+
+class RouteCfgC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_expert", "top_k", "score", "n_group", "top_group", "group_score", "renormalize",
+                                         "n_shared")] + [("scale", C.c_float)]
+
+
+class BlockCfgC(C.Structure):
+    _fields_ = [("route", RouteCfgC)] + [(n, C.c_int32) for n in ("d_expert", "route_bias", "post_norm", "gate")] + \
+        [("residual_scale", C.c_float)]
 
 
 class StepOutC(C.Structure):
@@ -60,6 +73,8 @@ def load_library(path: str = LIB_PATH):
     lib.sprinter_workspace_bytes.argtypes = [C.POINTER(CfgC), C.POINTER(sz)]
     lib.sprinter_create.argtypes = [C.POINTER(CfgC), vp, sz, vp, C.POINTER(vp)]
     lib.sprinter_create_static.argtypes = [C.POINTER(CfgC), vp, C.POINTER(vp)]
+    lib.sprinter_blocks_workspace_bytes.argtypes = [C.POINTER(CfgC), C.POINTER(BlockCfgC), C.POINTER(BlockCfgC), C.POINTER(sz)]
+    lib.sprinter_create_blocks.argtypes = [C.POINTER(CfgC), C.POINTER(BlockCfgC), C.POINTER(BlockCfgC), vp, sz, vp, C.POINTER(vp)]
     lib.sprinter_load_weights.argtypes = [vp, i32, C.POINTER(C.c_char_p), C.POINTER(vp), C.POINTER(C.c_int64), i32]
     lib.sprinter_prefill.argtypes = [vp, vp, C.POINTER(C.c_int32), i32, i32]
     lib.sprinter_step.argtypes = [vp, C.POINTER(StepOutC)]
@@ -100,6 +115,16 @@ def cfg_to_c(cfg) -> CfgC:
                 getattr(cfg, "sd_gamma", 0), getattr(cfg, "chunk_rows", 0))
 
 
+def blocks_to_c(m):
+    """The BlockCfgC of a model configuration, or None (a model without one: sprinter_create)."""
+    b = getattr(m, "blocks", None)
+    if b is None:
+        return None
+    r = RouteCfgC(b.n_expert, b.top_k, SCORES[b.score], b.n_group, b.top_group, GROUP_SCORES[b.group_score], bool(b.renormalize),
+                  b.n_shared, b.route_scale)
+    return BlockCfgC(r, b.d_expert, bool(b.route_bias), bool(b.post_norm), bool(b.gate), b.residual_scale)
+
+
 def _ptr(t):
     return C.c_void_p(t.data_ptr()) if t is not None else C.c_void_p(None)
 
@@ -114,7 +139,15 @@ class Sprinter:
         self.device = torch.device(device)
         self.ccfg = cfg_to_c(cfg)
         need = C.c_size_t(0)
-        self._check(self.lib.sprinter_workspace_bytes(C.byref(self.ccfg), C.byref(need)), None)
+        blocks = [blocks_to_c(m) for m in (cfg.draft, cfg.target)]
+        described = any(b is not None for b in blocks)
+        if described and static_workspace:
+            raise ValueError("models with described blocks need a workspace of their own")
+        blocks = [C.byref(b) if b is not None else None for b in blocks]
+        if described:
+            self._check(self.lib.sprinter_blocks_workspace_bytes(C.byref(self.ccfg), *blocks, C.byref(need)), None)
+        else:
+            self._check(self.lib.sprinter_workspace_bytes(C.byref(self.ccfg), C.byref(need)), None)
         self.workspace_bytes = need.value
         self.stream = torch.cuda.current_stream(self.device)
         ctx = C.c_void_p(None)
@@ -125,8 +158,11 @@ class Sprinter:
                                                             C.byref(ctx)), None)
         else:
             self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-            self._check(self.lib.sprinter_create(C.byref(self.ccfg), _ptr(self.workspace), need.value,
-                                                 C.c_void_p(self.stream.cuda_stream), C.byref(ctx)), None)
+            args = (_ptr(self.workspace), need.value, C.c_void_p(self.stream.cuda_stream), C.byref(ctx))
+            if described:
+                self._check(self.lib.sprinter_create_blocks(C.byref(self.ccfg), *blocks, *args), None)
+            else:
+                self._check(self.lib.sprinter_create(C.byref(self.ccfg), *args), None)
         self.ctx = ctx
         self._keep = {}
         self.B = 0
@@ -157,7 +193,7 @@ class Sprinter:
                 t = a
             else:
                 t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32))
-                matrix = t.ndim == 2 and which != VERIFIER
+                matrix = t.ndim >= 2 and which != VERIFIER
                 if matrix and self.cfg.dtype == BF16:
                     t = t.to(torch.bfloat16)
                 t = t.to(self.device)

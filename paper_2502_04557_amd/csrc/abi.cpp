@@ -46,6 +46,7 @@ struct Bump {   // 256-byte aligned bump allocator; base == nullptr only measure
 struct Expected {      // one tensor the model needs
   std::string name;
   int64_t rows, cols;  // cols == 0: 1-D
+  int64_t experts;     // > 0: [experts, rows, cols]
   bool pack;           // bf16 matrix that is repacked into operand tiles
   const void** slot;   // where the usable device pointer is stored
   void* packed;        // destination of the packed copy
@@ -67,6 +68,9 @@ struct Model {
   ModelScratch sc;
   int *rd_n = nullptr, *rd_b = nullptr, *rd_tok = nullptr, *rd_pos = nullptr, *rd_slot = nullptr;
   bool loaded = false;
+  bool has_blocks = false;
+  sprinter_block_cfg blocks{};
+  int experts() const { return blocks.route.n_expert + blocks.route.n_shared; }
   RowDesc rd() const { return RowDesc{rd_n, rd_b, rd_tok, rd_pos, rd_slot}; }
 };
 
@@ -205,6 +209,24 @@ int validate_cfg(const sprinter_cfg* c, char* buf, size_t n) {
 #undef BAD
 }
 
+struct BlockCfgs { const sprinter_block_cfg *draft = nullptr, *target = nullptr; };
+
+const char* check_blocks(const sprinter_model_cfg& m, const sprinter_block_cfg* b, const char* who, char* buf, size_t n) {
+  if (!b) return nullptr;
+#define BAD(...) do { snprintf(buf, n, __VA_ARGS__); return buf; } while (0)
+  if (m.arch != SPRINTER_ARCH_LLAMA) BAD("%s: blocks are described for LLaMA models only", who);
+  if (b->post_norm != 0 && b->post_norm != 1) BAD("%s: post_norm %d is not one of 0, 1", who, b->post_norm);
+  if (b->gate != 0 && b->gate != 1) BAD("%s: gate %d is not one of 0, 1", who, b->gate);
+  if (b->route_bias != 0 && b->route_bias != 1) BAD("%s: route_bias %d is not one of 0, 1", who, b->route_bias);
+  if (!(b->residual_scale == b->residual_scale)) BAD("%s: residual_scale is NaN", who);
+  if (b->route.n_expert == 0) return nullptr;
+  if (const char* e = route_cfg_error(b->route)) BAD("%s: %s", who, e);
+  if (b->route.n_expert + b->route.n_shared > MAX_EXPERTS) BAD("%s: more than %d experts", who, MAX_EXPERTS);
+  if (b->d_expert < 8 || b->d_expert > 65536 || b->d_expert % 8) BAD("%s: d_expert %d is not a multiple of 8 in [8, 65536]", who, b->d_expert);
+  return nullptr;
+#undef BAD
+}
+
 ModelDims dims_of(const sprinter_model_cfg& m) {
   ModelDims d;
   d.arch = m.arch; d.n_layer = m.n_layer; d.d = m.d_model; d.H = m.n_head; d.KVH = m.n_kv_head;
@@ -216,8 +238,13 @@ ModelDims dims_of(const sprinter_model_cfg& m) {
 // Slots per (row, KV head) of a cache: the bf16 value cache is kept in blocks of 32 slots (tiles of V^T).
 int kv_slots(const sprinter_cfg& c) { return c.dtype == SPRINTER_BF16 ? round_up(c.max_seq, 32) : c.max_seq; }
 
+int validate_blocks(const sprinter_cfg* c, const BlockCfgs& b, char* buf, size_t n) {
+  if (int rc = validate_cfg(c, buf, n)) return rc;
+  return check_blocks(c->draft, b.draft, "draft", buf, n) || check_blocks(c->target, b.target, "target", buf, n) ? SPRINTER_E_CONFIG : SPRINTER_OK;
+}
+
 // Lays one model out in the workspace (or only measures when bump.base == nullptr).
-void carve_model(Bump& bump, const sprinter_cfg& c, const sprinter_model_cfg& mc, Model* m, int rows) {
+void carve_model(Bump& bump, const sprinter_cfg& c, const sprinter_model_cfg& mc, const sprinter_block_cfg* blocks, Model* m, int rows) {
   ModelDims md = dims_of(mc);
   const size_t es = esize(c.dtype);
   const bool bf = c.dtype == SPRINTER_BF16;
@@ -237,12 +264,25 @@ void carve_model(Bump& bump, const sprinter_cfg& c, const sprinter_model_cfg& mc
   sc.part = (float*)bump.take(std::max((size_t)PART_SHARES * rows * md.d, bf ? attn_split_floats(md) : 0) * 4);
   sc.n_lm_wg = lmhead_num_wg(c.dtype, md.V);
   sc.am_part = (unsigned long long*)bump.take((size_t)sc.n_lm_wg * rows * 8);
+  const bool moe = blocks && blocks->route.n_expert > 0;
+  const int n_experts = moe ? blocks->route.n_expert + blocks->route.n_shared : 0, taken = moe ? blocks->route.top_k + blocks->route.n_shared : 0;
+  sc.block = blocks ? (float*)bump.take((size_t)rows * md.d * 4) : nullptr;
+  sc.rows = nullptr; sc.logits = sc.route_w = nullptr; sc.ids = nullptr; sc.experts = nullptr;
+  if (moe) {
+    if (bf) sc.rows = bump.take((size_t)rows * round_up(md.d, 32) * 2);
+    sc.logits = (float*)bump.take((size_t)rows * round_up(blocks->route.n_expert, 8) * 4);
+    sc.ids = (int*)bump.take((size_t)rows * taken * 4);
+    sc.route_w = (float*)bump.take((size_t)rows * taken * 4);
+    sc.experts = bump.take(experts_workspace(c.dtype, n_experts, md.d, blocks->d_expert, rows, taken));
+  }
   int* rd_n = (int*)bump.take(4);
   int* rd_b = (int*)bump.take((size_t)rows * 4);
   int* rd_tok = (int*)bump.take((size_t)rows * 4);
   int* rd_pos = (int*)bump.take((size_t)rows * 4);
   int* rd_slot = (int*)bump.take((size_t)rows * 4);
   if (m) {
+    m->has_blocks = blocks != nullptr;
+    if (blocks) m->blocks = *blocks;
     m->cfg = mc; m->md = md; m->kcache = kc; m->vcache = vc; m->layer_stride = layer_stride; m->sc = sc;
     m->rd_n = rd_n; m->rd_b = rd_b; m->rd_tok = rd_tok; m->rd_pos = rd_pos; m->rd_slot = rd_slot;
     m->layers.assign(md.n_layer, LayerW{});
@@ -253,7 +293,11 @@ void carve_model(Bump& bump, const sprinter_cfg& c, const sprinter_model_cfg& mc
     bool pack = bf && is_matrix && !gathered;
     void* dst = pack ? bump.take(packed_elems((int)r, (int)cl) * 2) : nullptr;
     void* dst2 = (bf && slot2) ? bump.take(packed_elems((int)r, (int)cl) * 2) : nullptr;
-    if (m) m->expected.push_back(Expected{name, r, cl, pack, slot, dst, slot2, dst2, false});
+    if (m) m->expected.push_back(Expected{name, r, cl, 0, pack, slot, dst, slot2, dst2, false});
+  };
+  auto want_experts = [&](const std::string& name, int64_t r, int64_t cl, const void** slot) {
+    void* dst = bf ? bump.take(expert_elems((int)r, (int)cl) * n_experts * 2) : nullptr;
+    if (m) m->expected.push_back(Expected{name, r, cl, n_experts, bf, slot, dst, nullptr, nullptr, false});
   };
   const int d = md.d, ff = md.ff, V = md.V;
   const bool gpt = md.arch == SPRINTER_ARCH_GPT;
@@ -278,10 +322,24 @@ void carve_model(Bump& bump, const sprinter_cfg& c, const sprinter_model_cfg& mc
       want(p + "b1", ff, 0, false, false, (const void**)&L.b1);
       want(p + "w2", d, ff, true, false, &L.w2);
       want(p + "b2", d, 0, false, false, (const void**)&L.b2);
+    } else if (moe) {
+      want(p + "router", blocks->route.n_expert, d, true, false, &L.router);
+      if (blocks->route_bias) want(p + "router.b", blocks->route.n_expert, 0, false, false, (const void**)&L.router_b);
+      want_experts(p + "wg", blocks->d_expert, d, &L.wg);
+      want_experts(p + "wu", blocks->d_expert, d, &L.wu);
+      want_experts(p + "w2", d, blocks->d_expert, &L.w2);
     } else {
       want(p + "wg", ff, d, true, false, &L.wg);
       want(p + "wu", ff, d, true, false, &L.wu);
       want(p + "w2", d, ff, true, false, &L.w2);
+    }
+    if (blocks && blocks->post_norm) {
+      want(p + "post1.g", d, 0, false, false, (const void**)&L.post1);
+      want(p + "post2.g", d, 0, false, false, (const void**)&L.post2);
+    }
+    if (blocks && blocks->gate) {
+      want(p + "gate1", d, 0, false, false, (const void**)&L.gate1);
+      want(p + "gate2", d, 0, false, false, (const void**)&L.gate2);
     }
   }
   want("normf.g", d, 0, false, false, &t->normf_g);
@@ -301,13 +359,13 @@ int chunk_rows_of(const sprinter_cfg& c, int want) {
 }
 
 // Lays the whole workspace out for passes of `want` rows; ctx == nullptr only measures.  Returns total bytes.
-size_t carve_rows(const sprinter_cfg& c, int want, void* base, sprinter_ctx* ctx) {
+size_t carve_rows(const sprinter_cfg& c, const BlockCfgs& blocks, int want, void* base, sprinter_ctx* ctx) {
   Bump bump(base);
   // full-prefix mode: every committed token reaches the target once, so a step's work list averages one entry
   // per batch row with wide swings; buffers for twice the batch keep most steps to a single pass.
   const int rows = chunk_rows_of(c, want);
-  carve_model(bump, c, c.draft, ctx ? &ctx->draft : nullptr, rows);
-  carve_model(bump, c, c.target, ctx ? &ctx->target : nullptr, rows);
+  carve_model(bump, c, c.draft, blocks.draft, ctx ? &ctx->draft : nullptr, rows);
+  carve_model(bump, c, c.target, blocks.target, ctx ? &ctx->target : nullptr, rows);
   int chunks = verifier_num_chunks(c.ver_d_hidden);
   float* ver_part = (float*)bump.take((size_t)chunks * c.max_batch * 4);
   State st;
@@ -376,9 +434,9 @@ size_t carve_rows(const sprinter_cfg& c, int want, void* base, sprinter_ctx* ctx
 // cfg.chunk_rows, or by default DEFAULT_CHUNK_ROWS prompt tokens per pass over the weights in bf16 mode.  In float32 mode a pass is a
 // chain of short launches whatever its rows, so the default is 256 of them (24 prompts of 5 - 60 tokens through 2 + 4 layers: 22
 // passes of 32 rows 4.4 ms, 3 of 256 0.7) - 16 on the static workspace, which is short.
-size_t carve(const sprinter_cfg& c, bool on_static, void* base, sprinter_ctx* ctx) {
+size_t carve(const sprinter_cfg& c, const BlockCfgs& blocks, bool on_static, void* base, sprinter_ctx* ctx) {
   const int standard = c.dtype == SPRINTER_BF16 ? DEFAULT_CHUNK_ROWS : on_static ? STATIC_CHUNK_ROWS_F32 : DEFAULT_CHUNK_ROWS_F32;
-  return carve_rows(c, c.chunk_rows > 0 ? c.chunk_rows : standard, base, ctx);
+  return carve_rows(c, blocks, c.chunk_rows > 0 ? c.chunk_rows : standard, base, ctx);
 }
 
 // One model forward over the rows described by rd (device-side count).
@@ -401,13 +459,42 @@ void forward(sprinter_ctx* ctx, Model& m, const RowDesc& rd, int max_rows, bool 
   const size_t part_stride = (size_t)rows * md.d;
   // a few rows: they add themselves, and the norms before QKV and FFN-up are part of those launches (the rows' statistics lie in part,
   // which the attention only takes between a layer's QKV and its O-proj)
-  const bool fused = !shared_caches && md.ff <= FEW_ROWS_MAX_K && gemm_takes_norm(dt, md.d, max_rows);
+  const bool fused = !m.has_blocks && !shared_caches && md.ff <= FEW_ROWS_MAX_K && gemm_takes_norm(dt, md.d, max_rows);
   // Short passes (work lists, speculative windows) of a model without rotary positions: the projection's epilogue puts keys and values
   // where the append launch would.  (A key's rotary partner is another workgroup's; and a prefill pass gathers 8 slots of a value column
   // into one store in that launch, where an epilogue would write 2 bytes at a time.)
   // The append launch was 4.1 us per layer of 25 heads of 64 at 24 - 80 entries, next to 45 - 60 us of the others.
   const bool append_in_qkv = shared_caches && run_len == 0 && dt == SPRINTER_BF16 && md.arch == SPRINTER_ARCH_GPT;
   NormPending pend{sc.part, part_stride, 0, nullptr};
+  // A block with norms, gate and scale of its own, or with experts: what it returns is complete before it joins the residual rows, which it
+  // does in the launch of the norm that follows (launch_block_norm).
+  auto block_norm = [&](const float* post, const float* gate, const float* g, bool experts, void* out, float* f32_out) {
+    BlockNormArgs b{};
+    b.kind = SPRINTER_NORM_RMS; b.d = md.d; b.T = max_rows; b.eps = md.eps; b.scale = m.blocks.residual_scale;
+    b.h = sc.h; b.ldh = md.d; b.y = sc.block; b.y_type = X_F32; b.ldy = md.d; b.post_g = post; b.gate = gate; b.gate_col = 1; b.g = g;
+    b.h_out = sc.h; b.ld_h_out = md.d; b.f32 = f32_out;
+    if (dt == SPRINTER_F32) { b.out = out; b.out_type = X_F32; b.ldo = md.d; }
+    else {
+      b.tiles = out;
+      if (experts) { b.out = sc.rows; b.out_type = X_F16; b.ldo = round_up(md.d, 32); }
+    }
+    launch_block_norm(b, s);
+  };
+  auto block_ffn = [&](const LayerW& L) {
+    const sprinter_route_cfg& rt = m.blocks.route;
+    if (rt.n_expert == 0) {
+      launch_gemm(dt, EPI_SWIGLU, L.wg, L.wu, sc.xn, pl_d, rd.n_rows, md.ff, md.d, nullptr, nullptr, md.ff, sc.mid, md.ff, max_rows, s);
+      launch_gemm(dt, EPI_F32, L.w2, nullptr, sc.mid, pl_f, rd.n_rows, md.d, md.ff, nullptr, sc.block, md.d, nullptr, md.d, max_rows, s);
+      return;
+    }
+    const int ld = round_up(rt.n_expert, 8);
+    launch_gemm(dt, EPI_F32, L.router, nullptr, sc.xn, pl_d, rd.n_rows, rt.n_expert, md.d, nullptr, sc.logits, ld, nullptr, ld, max_rows, s);
+    launch_route(rt, sc.logits, ld, L.router_b, max_rows, sc.ids, sc.route_w, s);
+    const bool f32 = dt == SPRINTER_F32;
+    launch_experts(ExpertsArgs{dt, m.experts(), md.d, m.blocks.d_expert, L.wg, L.wu, L.w2, f32 ? sc.xn : sc.rows, f32 ? X_F32 : X_F16,
+                               f32 ? md.d : round_up(md.d, 32), sc.ids, sc.route_w, max_rows, rt.top_k + rt.n_shared, sc.block, X_F32, md.d},
+                   sc.experts, s);
+  };
   auto resid_gemm = [&](const void* W, const void* X, size_t plane, int K, const float* bias) {
     if (fused || gemm_adds_rows(dt, md.d, K, max_rows)) {
       if (!launch_gemm_resid(dt, md.arch, W, X, md.d, K, bias, sc.h, fused ? sc.part : nullptr, max_rows, s)) ctx->no_kernel = "a product that adds itself";
@@ -438,7 +525,7 @@ void forward(sprinter_ctx* ctx, Model& m, const RowDesc& rd, int max_rows, bool 
       // A prefill position only has to fill the caches: the last layer projects to its key and value columns (their rows of the matrix
       // begin at a multiple of 64, so at an operand tile of the packed one) and appends them; its queries and attention have no reader.
       const int nq = md.H * md.dh;
-      norm(L.n1g, L.n1b, sc.xn, nullptr, i == 0 ? &emb : nullptr);
+      if (!m.has_blocks || i == 0) norm(L.n1g, L.n1b, sc.xn, nullptr, i == 0 ? &emb : nullptr);
       launch_gemm(dt, EPI_F32, (const char*)L.wqkv + (size_t)nq * act_elems(dt, 1, md.d) * esize(dt), nullptr, sc.xn, pl_d, rd.n_rows, md.dqkv - nq, md.d,
                   L.bqkv ? L.bqkv + nq : nullptr, sc.y + nq, md.dqkv, nullptr, md.dqkv, max_rows, s);
       launch_attention(dt, md, sc.y, sc.rope, rd, m.kcache, m.vcache, m.layer_stride * i, ctx->max_prompt_len + (int)ctx->steps_done,
@@ -450,6 +537,8 @@ void forward(sprinter_ctx* ctx, Model& m, const RowDesc& rd, int max_rows, bool 
       const KvDest kv{(char*)m.kcache + at, (char*)m.vcache + at, rd.b, rd.slot, md.H * md.dh, md.KVH * md.dh, md.dh, md.KVH, kv_slots(ctx->cfg)};
       norm(L.n1g, L.n1b, sc.xn, nullptr, i == 0 ? &emb : nullptr);
       launch_gemm_qkv(L.wqkv, sc.xn, pl_d, rd.n_rows, md.dqkv, md.d, L.bqkv, sc.y, kv, max_rows, s);
+    } else if (m.has_blocks && i > 0) {                  // (the block before has left the normalised rows)
+      launch_gemm(dt, EPI_F32, L.wqkv, nullptr, sc.xn, pl_d, rd.n_rows, md.dqkv, md.d, L.bqkv, sc.y, md.dqkv, nullptr, md.dqkv, max_rows, s);
     } else {
       norm_gemm(L.n1g, L.n1b, EPI_F32, L.wqkv, nullptr, md.dqkv, L.bqkv, sc.y, nullptr, i == 0 ? &emb : nullptr);
     }
@@ -463,12 +552,20 @@ void forward(sprinter_ctx* ctx, Model& m, const RowDesc& rd, int max_rows, bool 
       launch_attention(dt, md, sc.y, sc.rope, rd, m.kcache, m.vcache, m.layer_stride * i, ctx->max_prompt_len + (int)ctx->steps_done,
                        kv_slots(ctx->cfg), sc.ao, max_rows, sc.part, s);
     }
+    if (m.has_blocks) {
+      const bool last = i + 1 == md.n_layer;
+      launch_gemm(dt, EPI_F32, L.wo, nullptr, sc.ao, pl_a, rd.n_rows, md.d, md.H * md.dh, nullptr, sc.block, md.d, nullptr, md.d, max_rows, s);
+      block_norm(L.post1, L.gate1, L.n2g, m.blocks.route.n_expert > 0, sc.xn, nullptr);
+      block_ffn(L);
+      block_norm(L.post2, L.gate2, last ? (const float*)m.normf_g : m.layers[i + 1].n1g, false, last ? sc.hfn : sc.xn, last ? sc.hf : nullptr);
+      continue;
+    }
     resid_gemm(L.wo, sc.ao, pl_a, md.H * md.dh, L.bo);
     if (md.arch == SPRINTER_ARCH_GPT) norm_gemm(L.n2g, L.n2b, EPI_GELU, L.w1, nullptr, md.ff, L.b1, nullptr, sc.mid);
     else norm_gemm(L.n2g, L.n2b, EPI_SWIGLU, L.wg, L.wu, md.ff, nullptr, nullptr, sc.mid);
     resid_gemm(L.w2, sc.mid, pl_f, md.ff, L.b2);
   }
-  norm((const float*)m.normf_g, (const float*)m.normf_b, sc.hfn, sc.hf);
+  if (!m.has_blocks) norm((const float*)m.normf_g, (const float*)m.normf_b, sc.hfn, sc.hf);
   SamplerArgs sa;
   sa.seed_lo = (unsigned)(ctx->cfg.seed & 0xFFFFFFFFull);
   sa.seed_hi = (unsigned)(ctx->cfg.seed >> 32);
@@ -626,15 +723,15 @@ int hip_status(sprinter_ctx* ctx, const char* what) {
 // What sprinter_create and sprinter_create_static share: cfg is valid and the workspace large enough.
 // static_dev >= 0: the workspace is the library's static array on that device and the context must not allocate
 // anything, pinned host memory included.
-int create_common(const sprinter_cfg* cfg, void* dev_workspace, void* hip_stream, int static_dev, sprinter_ctx** out_ctx) {
+int create_common(const sprinter_cfg* cfg, const BlockCfgs& blocks, void* dev_workspace, void* hip_stream, int static_dev, sprinter_ctx** out_ctx) {
   sprinter_ctx* ctx = new sprinter_ctx();
   ctx->cfg = *cfg;
   ctx->stream = (hipStream_t)hip_stream;
   ctx->err[0] = 0;
-  carve(*cfg, static_dev >= 0, dev_workspace, ctx);
+  carve(*cfg, blocks, static_dev >= 0, dev_workspace, ctx);
   // verifier tensors
   auto vwant = [&](const char* name, int64_t r, int64_t c, const void** slot) {
-    ctx->v_expected.push_back(Expected{name, r, c, false, slot, nullptr, nullptr, nullptr, false});
+    ctx->v_expected.push_back(Expected{name, r, c, 0, false, slot, nullptr, nullptr, nullptr, false});
   };
   if (cfg->ver_d_hidden > 0) {
     vwant("v.w1", cfg->ver_d_hidden, cfg->ver_d_in, &ctx->v_w1);
@@ -653,6 +750,7 @@ int create_common(const sprinter_cfg* cfg, void* dev_workspace, void* hip_stream
     launch_fill_zero(m->sc.ao, act_elems(cfg->dtype, rows, m->md.H * m->md.dh) * es, ctx->stream);
     launch_fill_zero(m->sc.mid, act_elems(cfg->dtype, rows, m->md.ff) * es, ctx->stream);
     launch_fill_zero(m->sc.hfn, act_elems(cfg->dtype, rows, m->md.d) * es, ctx->stream);
+    if (m->sc.rows) launch_fill_zero(m->sc.rows, (size_t)rows * round_up(m->md.d, 32) * 2, ctx->stream);
   }
   launch_set_f32(ctx->tau_dev, cfg->tau, ctx->stream);
   launch_fill_zero(ctx->dev_counts, 256, ctx->stream);
@@ -688,22 +786,38 @@ int sprinter_workspace_bytes(const sprinter_cfg* cfg, size_t* out_bytes) {
   char buf[256];
   int rc = validate_cfg(cfg, buf, sizeof buf);
   if (rc) return fail(nullptr, rc, "%s", buf);
-  *out_bytes = carve(*cfg, false, nullptr, nullptr);
+  *out_bytes = carve(*cfg, BlockCfgs{}, false, nullptr, nullptr);
+  return SPRINTER_OK;
+}
+
+int sprinter_blocks_workspace_bytes(const sprinter_cfg* cfg, const sprinter_block_cfg* draft_blocks,
+                                    const sprinter_block_cfg* target_blocks, size_t* out_bytes) {
+  if (!cfg || !out_bytes) return fail(nullptr, SPRINTER_E_NULL, "sprinter_blocks_workspace_bytes: NULL argument");
+  char buf[256];
+  int rc = validate_blocks(cfg, BlockCfgs{draft_blocks, target_blocks}, buf, sizeof buf);
+  if (rc) return fail(nullptr, rc, "%s", buf);
+  *out_bytes = carve(*cfg, BlockCfgs{draft_blocks, target_blocks}, false, nullptr, nullptr);
   return SPRINTER_OK;
 }
 
 int sprinter_create(const sprinter_cfg* cfg, void* dev_workspace, size_t workspace_bytes, void* hip_stream,
                     sprinter_ctx** out_ctx) {
+  return sprinter_create_blocks(cfg, nullptr, nullptr, dev_workspace, workspace_bytes, hip_stream, out_ctx);
+}
+
+int sprinter_create_blocks(const sprinter_cfg* cfg, const sprinter_block_cfg* draft_blocks, const sprinter_block_cfg* target_blocks,
+                           void* dev_workspace, size_t workspace_bytes, void* hip_stream, sprinter_ctx** out_ctx) {
   if (!cfg || !dev_workspace || !out_ctx) return fail(nullptr, SPRINTER_E_NULL, "sprinter_create: NULL argument");
   *out_ctx = nullptr;
   char buf[256];
-  int rc = validate_cfg(cfg, buf, sizeof buf);
+  const BlockCfgs blocks{draft_blocks, target_blocks};
+  int rc = validate_blocks(cfg, blocks, buf, sizeof buf);
   if (rc) return fail(nullptr, rc, "%s", buf);
   if (((uintptr_t)dev_workspace) & 255) return fail(nullptr, SPRINTER_E_WORKSPACE, "workspace is not 256-byte aligned");
-  size_t need = carve(*cfg, false, nullptr, nullptr);
+  size_t need = carve(*cfg, blocks, false, nullptr, nullptr);
   if (workspace_bytes < need)
     return fail(nullptr, SPRINTER_E_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
-  return create_common(cfg, dev_workspace, hip_stream, -1, out_ctx);
+  return create_common(cfg, blocks, dev_workspace, hip_stream, -1, out_ctx);
 }
 
 int sprinter_create_static(const sprinter_cfg* cfg, void* hip_stream, sprinter_ctx** out_ctx) {
@@ -712,7 +826,7 @@ int sprinter_create_static(const sprinter_cfg* cfg, void* hip_stream, sprinter_c
   char buf[256];
   int rc = validate_cfg(cfg, buf, sizeof buf);
   if (rc) return fail(nullptr, rc, "%s", buf);
-  const size_t need = carve(*cfg, true, nullptr, nullptr);
+  const size_t need = carve(*cfg, BlockCfgs{}, true, nullptr, nullptr);
   if (need > STATIC_WORKSPACE_BYTES)
     return fail(nullptr, SPRINTER_E_WORKSPACE, "this configuration needs %zu bytes of workspace, the static workspace holds %zu",
                 need, STATIC_WORKSPACE_BYTES);
@@ -736,7 +850,7 @@ int sprinter_create_static(const sprinter_cfg* cfg, void* hip_stream, sprinter_c
     slot.in_use = true;
     base = slot.base;
   }
-  rc = create_common(cfg, base, hip_stream, dev, out_ctx);
+  rc = create_common(cfg, BlockCfgs{}, base, hip_stream, dev, out_ctx);
   if (rc) {
     std::lock_guard<std::mutex> lock(g_static_mu);
     g_static[dev].in_use = false;
@@ -764,7 +878,11 @@ int sprinter_load_weights(sprinter_ctx* ctx, int which, const char* const* names
     if (it == idx->end()) return fail(ctx, SPRINTER_E_WEIGHTS, "%s: unknown tensor name '%s'", who, names[i]);
     const Expected& e = (*exp)[it->second];
     const int64_t* sh = shapes + 4 * i;
-    if (sh[0] != e.rows || sh[1] != e.cols || sh[2] != 0 || sh[3] != 0)
+    if (e.experts > 0) {
+      if (sh[0] != e.experts || sh[1] != e.rows || sh[2] != e.cols || sh[3] != 0)
+        return fail(ctx, SPRINTER_E_WEIGHTS, "%s: tensor '%s' has shape [%lld,%lld,%lld,%lld], expected [%lld,%lld,%lld]", who, names[i], (long long)sh[0],
+                    (long long)sh[1], (long long)sh[2], (long long)sh[3], (long long)e.experts, (long long)e.rows, (long long)e.cols);
+    } else if (sh[0] != e.rows || sh[1] != e.cols || sh[2] != 0 || sh[3] != 0)
       return fail(ctx, SPRINTER_E_WEIGHTS, "%s: tensor '%s' has shape [%lld,%lld,%lld,%lld], expected [%lld,%lld]", who,
                   names[i], (long long)sh[0], (long long)sh[1], (long long)sh[2], (long long)sh[3], (long long)e.rows,
                   (long long)e.cols);
@@ -778,7 +896,10 @@ int sprinter_load_weights(sprinter_ctx* ctx, int which, const char* const* names
     if (!seen[j]) return fail(ctx, SPRINTER_E_WEIGHTS, "%s: tensor '%s' is missing", who, (*exp)[j].name.c_str());
   for (int i = 0; i < n; ++i) {
     Expected& e = (*exp)[hit[i]];
-    if (e.pack) {
+    if (e.pack && e.experts > 0) {
+      launch_pack_experts(dev_ptrs[i], e.packed, (int)e.experts, (int)e.rows, (int)e.cols, ctx->stream);
+      *e.slot = e.packed;
+    } else if (e.pack) {
       launch_pack_bf16(dev_ptrs[i], e.packed, (int)e.rows, (int)e.cols, ctx->stream);
       *e.slot = e.packed;
     } else {

@@ -28,6 +28,7 @@ struct RowDesc {       // which rows a model forward works on (all device memory
 struct LayerW {
   const float *n1g, *n1b, *bqkv, *bo, *n2g, *n2b, *b1, *b2;
   const void *wqkv, *wo, *w1, *wg, *wu, *w2;   // dtype matrices (bf16: tile-packed)
+  const void* router; const float *router_b, *post1, *post2, *gate1, *gate2;   // sprinter_block_cfg
 };
 
 struct ModelDims {
@@ -54,6 +55,11 @@ struct ModelScratch {  // per-model activation buffers, sized for max_batch rows
   float* part;         // [PART_SHARES][M, d] partial O-proj / FFN-down products, float32
   unsigned long long* am_part;  // [n_lm_wg, Mpad] packed (value, index) arg-max partials
   int n_lm_wg;
+  // models with a sprinter_block_cfg
+  float* block;        // [M, d] what attention or feed-forward returned, float32
+  void* rows;          // [M, d rounded up to 32] normalised input of the experts, float16 rows (float32 mode: xn)
+  float *logits, *route_w; int* ids;   // router's [M, n_expert rounded up to 8]; [M, top_k + n_shared]
+  void* experts;       // workspace of launch_experts
 };
 
 struct SamplerArgs {

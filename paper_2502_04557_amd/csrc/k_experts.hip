@@ -369,7 +369,10 @@ Space space(void* base, int dtype, int E, int d, int ff, long long T, int k) {
 }
 }  // namespace
 
-size_t experts_workspace(int dtype, int E, int d, int ff, long long T, int k) { return space(nullptr, dtype, E, d, ff, T, k).bytes; }
+// Enough for any call of up to T rows.
+size_t experts_workspace(int dtype, int E, int d, int ff, long long T, int k) {
+  return std::max(space(nullptr, dtype, E, d, ff, T, k).bytes, space(nullptr, dtype, E, d, ff, std::min<long long>(T, FEW_ROWS), k).bytes);
+}
 
 void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   const Space w = space(workspace, a.dtype, a.E, a.d, a.ff, a.T, a.k);

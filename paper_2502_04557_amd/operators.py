@@ -9,17 +9,10 @@ import ctypes as C
 from functools import lru_cache
 import torch
 
-from .binding import F32, BF16, SprinterError, load_library
+from .binding import F32, BF16, GROUP_SCORES, SCORES, RouteCfgC, SprinterError, load_library
 
-SCORES = {"softmax": 0, "sigmoid": 1}
-GROUP_SCORES = {"max": 0, "sum2": 1}
 NORMS = {"layer": 0, "rms": 1}
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
-
-
-class RouteCfgC(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("n_expert", "top_k", "score", "n_group", "top_group", "group_score", "renormalize",
-                                         "n_shared")] + [("scale", C.c_float)]
 
 
 class ExpertsCfgC(C.Structure):

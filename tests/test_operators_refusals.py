@@ -129,3 +129,42 @@ def test_tensors_that_are_none_of_a_gpu():
         ops.block_norm(torch.zeros(2, 8), torch.zeros(2, 8), torch.zeros(8))
     with pytest.raises(ValueError):
         ops.route(np.zeros((2, 8)), 2)
+
+
+# ------------------------------------------------------------------------------------------ contexts with described blocks
+@pytest.mark.parametrize("which", ["draft", "target"])
+@pytest.mark.parametrize("change, word", [
+    (dict(post_norm=2), "post_norm"), (dict(gate=-1), "gate"), (dict(route_bias=2), "route_bias"), (dict(residual_scale=float("nan")), "residual_scale"),
+    (dict(d_expert=0), "d_expert"), (dict(d_expert=12), "d_expert"), (dict(d_expert=65544), "d_expert"), (dict(top_k=0), "top_k"),
+    (dict(n_expert=1024, n_shared=1), "experts"), (dict(n_expert=-1), "n_expert"), (dict(scale=-1.0), "scale")])
+def test_block_configuration(lib, which, change, word):  # noqa: F811
+    import workloads as W
+    from paper_2502_04557_amd import binding
+    cfg = W.mini_config("llama")
+    b = binding.blocks_to_c(W.mini_config("experts").target)
+    for k, v in change.items():
+        setattr(b.route if hasattr(b.route, k) else b, k, v)
+    c = binding.cfg_to_c(cfg)
+    n, ctx = C.c_size_t(0), C.c_void_p(None)
+    pair = [C.byref(b), None] if which == "draft" else [None, C.byref(b)]
+    for rc in (lib.sprinter_blocks_workspace_bytes(C.byref(c), *pair, C.byref(n)),
+               lib.sprinter_create_blocks(C.byref(c), *pair, A, 1 << 40, None, C.byref(ctx))):
+        _refused(lib, rc, CONFIG, word)
+        assert which in lib.sprinter_last_error(None).decode()
+
+
+def test_blocks_need_a_llama_model_and_their_workspace(lib):  # noqa: F811
+    import workloads as W
+    from paper_2502_04557_amd import binding
+    b = binding.blocks_to_c(W.mini_config("experts").target)
+    n, plain, ctx = C.c_size_t(0), C.c_size_t(0), C.c_void_p(None)
+    c = binding.cfg_to_c(W.mini_config("gpt"))
+    _refused(lib, lib.sprinter_blocks_workspace_bytes(C.byref(c), C.byref(b), None, C.byref(n)), CONFIG, "LLaMA")
+    c = binding.cfg_to_c(W.mini_config("llama"))
+    assert lib.sprinter_workspace_bytes(C.byref(c), C.byref(plain)) == 0
+    assert lib.sprinter_blocks_workspace_bytes(C.byref(c), None, None, C.byref(n)) == 0 and n.value == plain.value
+    assert lib.sprinter_blocks_workspace_bytes(C.byref(c), None, C.byref(b), C.byref(n)) == 0 and n.value > plain.value
+    _refused(lib, lib.sprinter_create_blocks(C.byref(c), None, C.byref(b), A, n.value - 1, None, C.byref(ctx)), WORKSPACE, "needed")
+    assert lib.sprinter_blocks_workspace_bytes(C.byref(c), None, None, None) == NULL
+    with pytest.raises(ValueError, match="workspace of their own"):
+        binding.Sprinter(W.mini_config("experts"), static_workspace=True)

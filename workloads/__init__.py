@@ -10,7 +10,7 @@ The paper evaluates on trained checkpoints (GPT-2 small/XL, GPT-Neo, Vicuna
 is available here, so the generators below produce random-init weights of the
 same shapes and i.i.d. token-id prompts (uniform or Zipf) that stand in for them.
 """
-from .configs import (ModelCfg, SprinterCfg, ARCH_GPT, ARCH_LLAMA, DT_F32, DT_BF16,
+from .configs import (BlockCfg, ModelCfg, SprinterCfg, ARCH_GPT, ARCH_LLAMA, DT_F32, DT_BF16,
                       CTX_OWN_HISTORY, CTX_FULL_PREFIX, REJECT_REPLACE, REJECT_SD, config, mini_config, CONFIG_NAMES)
 from .synth import (round_bf16, make_model_weights, make_verifier_weights,
                     make_weights, make_prompts, zipf_probs, model_weight_shapes,

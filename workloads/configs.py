@@ -14,6 +14,26 @@ CTX_FULL_PREFIX = 1   # the target first consumes the committed tokens it has no
 
 
 @dataclass(frozen=True)
+class BlockCfg:
+    """What a decoder block has beyond the dense one (LLaMA family): experts, norms behind attention and feed-forward, gates, a
+    scale of the residual stream."""
+    n_expert: int = 0            # 0: the dense feed-forward
+    top_k: int = 0
+    d_expert: int = 0
+    score: str = "softmax"       # "softmax" | "sigmoid"
+    route_bias: bool = False
+    n_group: int = 1
+    top_group: int = 1
+    group_score: str = "max"     # "max" | "sum2"
+    renormalize: bool = True
+    n_shared: int = 0
+    route_scale: float = 1.0
+    post_norm: bool = False
+    gate: bool = False
+    residual_scale: float = 1.0
+
+
+@dataclass(frozen=True)
 class ModelCfg:
     arch: int
     n_layer: int
@@ -25,6 +45,7 @@ class ModelCfg:
     max_pos: int
     norm_eps: float = 1e-5
     rope_theta: float = 10000.0
+    blocks: BlockCfg | None = None
 
     @property
     def d_head(self) -> int:
@@ -122,6 +143,15 @@ def mini_config(kind: str, dtype: int = DT_BF16, **over) -> SprinterCfg:
         cfg = SprinterCfg(_gpt(1, 128, 2, 256, 517, 64), _llama(2, 256, 2, 1, 384, 517, 64),
                           0, dtype, 3, 64, seed=13, name="mini-linear", batch=3, prompt_len=5,
                           n_gen=16, prompt_dist="uniform", weight_seed=81, prompt_seed=82)
+    elif kind in ("experts", "groups"):   # a dense draft with norms behind attention and feed-forward; a target of experts
+        if kind == "experts":
+            t = replace(_llama(3, 512, 4, 2, 1344, 1501, 128), blocks=BlockCfg(8, 2, 200, n_shared=1, residual_scale=0.5))
+        else:
+            t = replace(_llama(3, 256, 4, 1, 704, 1501, 128), blocks=BlockCfg(12, 3, 136, "sigmoid", True, 4, 2, "sum2", True, 0, 1.5, True, True))
+        cfg = SprinterCfg(replace(_llama(2, 256, 4, 2, 704, 1501, 128), blocks=BlockCfg(post_norm=True, gate=kind == "experts")), t,
+                          40, dtype, 19, 128, seed=14, name="mini-" + kind, batch=19, prompt_len=21,
+                          prompt_len_min=3, n_gen=20, prompt_dist="zipf", weight_seed=83,
+                          prompt_seed=84)
     else:
         raise KeyError(kind)
     return replace(cfg, **over) if over else cfg

@@ -44,10 +44,22 @@ def model_weight_shapes(m: ModelCfg) -> dict:
             s[p + "b1"] = (ff,)
             s[p + "w2"] = (d, ff)
             s[p + "b2"] = (d,)
+        elif m.blocks and m.blocks.n_expert:
+            b = m.blocks
+            n = b.n_expert + b.n_shared
+            s[p + "router"] = (b.n_expert, d)
+            if b.route_bias:
+                s[p + "router.b"] = (b.n_expert,)
+            s[p + "wg"] = s[p + "wu"] = (n, b.d_expert, d)
+            s[p + "w2"] = (n, d, b.d_expert)
         else:
             s[p + "wg"] = (ff, d)
             s[p + "wu"] = (ff, d)
             s[p + "w2"] = (d, ff)
+        if m.blocks and m.blocks.post_norm:
+            s[p + "post1.g"] = s[p + "post2.g"] = (d,)
+        if m.blocks and m.blocks.gate:
+            s[p + "gate1"] = s[p + "gate2"] = (d,)
     s["normf.g"] = (d,)
     if m.arch == ARCH_GPT:
         s["normf.b"] = (d,)
@@ -78,8 +90,10 @@ def _fill(shapes: dict, seed: int, bf16: bool, threads: int = 8) -> dict:
             blk = g.standard_normal(min(step, flat.size - o), dtype=np.float32)
             blk *= np.float32(0.02)
             flat[o:o + blk.size] = blk
-        if n.endswith(".g"):
+        if n.endswith((".g", ".gate1", ".gate2")):
             a += np.float32(1.0)
+        if n.endswith(".router"):
+            a *= np.float32(16.0)          # rows that know which experts they want
         return round_bf16(a) if bf16 else a
 
     with ThreadPoolExecutor(max_workers=threads) as ex:
