@@ -23,49 +23,58 @@ class BlockNormCfgC(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "kind", "d")] + [("eps", C.c_float), ("scale", C.c_float)]
 
 
-# (the raw handle: a torch.cuda.Stream object takes longer to make than the smallest kernels run)
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# The smallest kernels run for 2 - 4 us, so the host's side counts: raw handles instead of torch.cuda.Stream objects, no generators.
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_lib = None
+
+
+def _entry(name):
+    global _lib
+    if _lib is None:
+        _lib = load_library()
+    return getattr(_lib, name)
 
 
 def _call(name, device, *args):
     """One entry point on `device` and its current stream (the last argument of them all)."""
     index = device.index
-    if torch.cuda.current_device() == index:
-        rc = getattr(_lib or _load(), name)(*args, _raw_stream(index))
+    if _current_device() == index:
+        rc = _entry(name)(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            rc = getattr(_lib or _load(), name)(*args, _raw_stream(index))
+            rc = _entry(name)(*args, _raw_stream(index))
     if rc != 0:
         raise SprinterError(rc, _lib.sprinter_last_error(None).decode())
 
 
-_lib = None
-
-
-def _load():
-    global _lib
-    _lib = load_library()
-    return _lib
-
-
-def _tensor(name, t, device, dtype, shape, contiguous=False):
-    """Checks one argument: shape with None for any size; rows may lie apart unless contiguous."""
+def _tensor(name, t, device, dtype):
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
-    have = t.shape
-    if len(have) != len(shape) or any(w is not None and w != n for w, n in zip(shape, have)):
-        raise ValueError(f"{name}: shape {tuple(have)}, expected {shape}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: gradients are not computed here; detach it")
+
+
+def _rows(name, t, device, dtype, rows, cols):
+    """A matrix whose rows may lie apart; rows, cols: None for any."""
+    _tensor(name, t, device, dtype)
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected [{rows or 'any'}, {cols or 'any'}]")
+    if not t.is_contiguous() and shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row are not adjacent")
+
+
+def _whole(name, t, device, dtype, *shape):
+    """A contiguous array of this shape."""
+    _tensor(name, t, device, dtype)
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {list(shape)}")
     if not t.is_contiguous():
-        if contiguous:
-            raise ValueError(f"{name}: not contiguous")
-        if have[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{name}: the elements of a row are not adjacent")
+        raise ValueError(f"{name}: not contiguous")
 
 
 def _device(t, name):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a tensor on a GPU is needed")
     return t.device
 
@@ -86,10 +95,10 @@ def route(logits, top_k, *, score="softmax", bias=None, n_group=1, top_group=1, 
           n_shared=0):
     """logits [T, E] float32 -> (ids int32, weights float32), both [T, top_k + n_shared] (sprinter_route)."""
     dev = _device(logits, "logits")
-    _tensor("logits", logits, dev, torch.float32, (None, None))
+    _rows("logits", logits, dev, torch.float32, None, None)
     T, E = logits.shape
     if bias is not None:
-        _tensor("bias", bias, dev, torch.float32, (E,), True)
+        _whole("bias", bias, dev, torch.float32, E)
     cfg = _route_cfg(E, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale)
     n = max(0, top_k + n_shared)
     ids = torch.empty(T, n, dtype=torch.int32, device=dev)
@@ -109,7 +118,7 @@ class Experts:
             raise ValueError("gate: bfloat16 or float32 [n_expert, d_ff, d_model] is needed")
         E, ff, d = gate.shape
         for name, t, shape in (("gate", gate, (E, ff, d)), ("up", up, (E, ff, d)), ("down", down, (E, d, ff))):
-            _tensor(name, t, dev, gate.dtype, shape, True)
+            _whole(name, t, dev, gate.dtype, *shape)
         self.device, self.dtype = dev, gate.dtype
         self.n_expert, self.d_ff, self.d_model = E, ff, d
         self._cfg = ExpertsCfgC(DTYPES[gate.dtype], E, d, ff)
@@ -127,11 +136,10 @@ class Experts:
     def _bytes(self, rows, top_k):
         n = self._need.get((rows, top_k))
         if n is None:
-            lib = load_library()
             v = [C.c_size_t(0) for _ in range(3)]
-            rc = lib.sprinter_experts_bytes(self._ref, rows, top_k, *(C.byref(x) for x in v))
+            rc = _entry("sprinter_experts_bytes")(self._ref, rows, top_k, *(C.byref(x) for x in v))
             if rc:
-                raise SprinterError(rc, lib.sprinter_last_error(None).decode())
+                raise SprinterError(rc, _lib.sprinter_last_error(None).decode())
             if len(self._need) >= 4096:
                 self._need.clear()
             n = self._need[rows, top_k] = tuple(x.value for x in v)
@@ -140,15 +148,15 @@ class Experts:
     def __call__(self, x, ids, weights, out=None):
         """x [T, d_model] -> y [T, d_model] of its type; ids int32, weights float32 [T, top_k] as `route` gives them (sprinter_experts)."""
         dev = self.device
-        _tensor("x", x, dev, self.dtype, (None, self.d_model))
+        _rows("x", x, dev, self.dtype, None, self.d_model)
         T = x.shape[0]
-        _tensor("ids", ids, dev, torch.int32, (T, None), True)
-        k = ids.shape[1]
-        _tensor("weights", weights, dev, torch.float32, (T, k), True)
+        k = ids.shape[1] if isinstance(ids, torch.Tensor) and ids.dim() == 2 else 0
+        _whole("ids", ids, dev, torch.int32, T, k)
+        _whole("weights", weights, dev, torch.float32, T, k)
         if out is None:
             out = torch.empty(T, self.d_model, dtype=self.dtype, device=dev)
         else:
-            _tensor("out", out, dev, self.dtype, (T, self.d_model))
+            _rows("out", out, dev, self.dtype, T, self.d_model)
         need = self._bytes(T, k)[2]
         work = torch.empty(need, dtype=torch.uint8, device=dev)
         _call("sprinter_experts", dev, self._ref, *self._ptrs, x.data_ptr(), x.stride(0), ids.data_ptr(), weights.data_ptr(), T, k,
@@ -170,21 +178,22 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
     h [T, d] float32, y [T, d] bfloat16 or float32; gate float32 of any shape that broadcasts to [T, d].  h_out: where h' goes (h itself
     updates it in place); by default a new tensor."""
     dev = _device(h, "h")
-    _tensor("h", h, dev, torch.float32, (None, None))
+    _rows("h", h, dev, torch.float32, None, None)
     T, d = h.shape
     if not isinstance(y, torch.Tensor):
         raise ValueError("y: a tensor is needed")
     cfg = _norm_cfg(y.dtype, kind, d, eps, scale)
-    _tensor("y", y, dev, y.dtype, (T, d))
-    for name, t in (("gain", gain), ("offset", offset), ("post_gain", post_gain), ("post_offset", post_offset)):
-        if t is not None or name == "gain":
-            _tensor(name, t, dev, torch.float32, (d,), True)
+    _rows("y", y, dev, y.dtype, T, d)
+    _whole("gain", gain, dev, torch.float32, d)
+    if offset is not None:
+        _whole("offset", offset, dev, torch.float32, d)
+    if post_gain is not None:
+        _whole("post_gain", post_gain, dev, torch.float32, d)
+    if post_offset is not None:
+        _whole("post_offset", post_offset, dev, torch.float32, d)
     gate_row = gate_col = 0
     if gate is not None:
-        if not isinstance(gate, torch.Tensor) or gate.dtype != torch.float32 or gate.device != dev:
-            raise ValueError(f"gate: a float32 tensor on {dev} is needed")
-        if gate.requires_grad and torch.is_grad_enabled():
-            raise ValueError("gate: gradients are not computed here; detach it")
+        _tensor("gate", gate, dev, torch.float32)
         try:
             gate = gate.expand(T, d)
         except RuntimeError as e:
@@ -193,7 +202,7 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
     if h_out is None:
         h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
     else:
-        _tensor("h_out", h_out, dev, torch.float32, (T, d))
+        _rows("h_out", h_out, dev, torch.float32, T, d)
     out = torch.empty(T, d, dtype=y.dtype, device=dev)
     _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr(post_gain), _ptr(post_offset),
           _ptr(gate), gate_row, gate_col, gain.data_ptr(), _ptr(offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
