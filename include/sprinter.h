@@ -345,7 +345,7 @@ int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* hos
  *   top_k       experts taken, largest key first, equal keys by index
  *   renormalize 1: the weights are p / (sum of the taken p); 0: p itself.  Either times scale.
  *   n_shared    appends the ids n_expert, n_expert + 1, ... with a weight of 1 (shared experts behind the routed ones)
- * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16.
+ * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16, n_rows 2^23 (sprinter_block_norm too).
  *
  * ids and weights [n_rows, top_k + n_shared] of logits [n_rows, n_expert] (float32; rows ld_logits apart).  dev_bias
  * [n_expert] or NULL.  An expert whose logit is -inf or NaN is never taken; where fewer than top_k are left (a row may

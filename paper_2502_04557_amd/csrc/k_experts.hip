@@ -97,34 +97,29 @@ __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ i
 // -------------------------------------------------------------------------------------------------------------- few rows
 constexpr int FEW_ROWS = 16;
 
-// The set of experts that `pairs` ids name, as bits in LDS; then the j-th of them in rising order (every wave for itself; -1: there are
-// no more), and with a list the whole set.
-struct NamedExperts { unsigned bits[MAX_EXPERTS / 32]; };
-__device__ __forceinline__ void name_experts(NamedExperts& s, const int* __restrict__ ids, int pairs, int E) {
-  if (threadIdx.x < MAX_EXPERTS / 32) s.bits[threadIdx.x] = 0;
+// The rows that name each expert, as bits in LDS, from the ids [T, k]; experts that no row names have none.  named_expert: the j-th that is
+// named, in rising order, for every wave by itself (-1: there are no more).
+struct NamedExperts { unsigned rows[MAX_EXPERTS]; };
+__device__ __forceinline__ void name_experts(NamedExperts& s, const int* __restrict__ ids, int T, int k, int E) {
+  for (int e = threadIdx.x; e < E; e += blockDim.x) s.rows[e] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+  for (int i = threadIdx.x; i < T * k; i += blockDim.x) {
     const int e = ids[i];
-    if ((unsigned)e < (unsigned)E) atomicOr(&s.bits[e >> 5], 1u << (e & 31));
+    if ((unsigned)e < (unsigned)E) atomicOr(&s.rows[e], 1u << (i / k));
   }
   __syncthreads();
 }
-// Bits before word `lane` (lanes 0 - 31), and all of them
-__device__ __forceinline__ int named_before(unsigned word, int lane, int& all) {
-  int n = __popc(word);
-  for (int o = 1; o < 32; o <<= 1) { const int up = __shfl_up(n, o); if (lane >= o) n += up; }
-  all = __builtin_amdgcn_readlane(n, 31);
-  return n - __popc(word);
-}
-__device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int lane) {
-  unsigned word = lane < 32 ? s.bits[lane] : 0u;
-  int all;
-  const int before = named_before(word, lane, all);
-  if (j >= all) return -1;                              // (scalar)
-  const int at = __builtin_ctzll(__ballot(lane < 32 && before <= j && j < before + __popc(word)));
-  word = (unsigned)__builtin_amdgcn_readlane((int)word, at);
-  for (int i = __builtin_amdgcn_readlane(before, at); i < j; ++i) word &= word - 1;
-  return at * 32 + __builtin_ctz(word);
+__device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int E, int lane) {
+  for (int e0 = 0; e0 < E; e0 += 64) {                  // (scalar)
+    u64 named = __ballot(e0 + lane < E && s.rows[min(e0 + lane, E - 1)] != 0);
+    const int n = __popcll(named);
+    if (j < n) {
+      for (; j > 0; --j) named &= named - 1;
+      return e0 + __builtin_ctzll(named);
+    }
+    j -= n;
+  }
+  return -1;
 }
 
 // A workgroup: one expert's column tile of both matrices.  The 8 waves share K; 256 threads then finish an element each.  What bounds it: the
@@ -134,11 +129,10 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
   constexpr int U = 4;
   __shared__ NamedExperts named;
   __shared__ float red[8][2][4][64], row_w[FEW_ROWS];
-  __shared__ int row_hit[FEW_ROWS];
   const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
   const int j = blockIdx.x / col_tiles, nt = blockIdx.x - j * col_tiles;
-  name_experts(named, ids, T * k, E);
-  const int e = named_expert(named, j, lane);
+  name_experts(named, ids, T, k, E);
+  const int e = named_expert(named, j, E, lane);
   if (e < 0) return;
   const int Kt = (d + 31) >> 5, Nt = (ff + 15) >> 4, row = lane & 15, oct = (lane >> 4) * 8;
   const size_t tile = ((size_t)e * Nt + min(nt, Nt - 1)) * Kt * 64 + lane;      // (the column tile behind the last one of an odd count: zeros)
@@ -166,13 +160,12 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
   {                                                     // the rows' weights for this expert: 32 threads to a row
     const int m = tid >> 5;
     float s = 0.f;
-    int hit = 0;
     if (m < T)
       for (int i = tid & 31; i < k; i += 32)
-        if (ids[m * k + i] == e) { s += weights[m * k + i]; hit = 1; }
+        if (ids[m * k + i] == e) s += weights[m * k + i];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { s += __shfl_xor(s, o); hit |= __shfl_xor(hit, o); }
-    if ((tid & 31) == 0) { row_w[m] = s; row_hit[m] = hit; }
+    for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
+    if ((tid & 31) == 0) row_w[m] = s;
   }
   __syncthreads();
   if (tid >= 256) return;
@@ -181,44 +174,57 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
   float gs = 0.f, us = 0.f;
 #pragma unroll
   for (int q = 0; q < 8; ++q) { gs += red[q][0][i][at]; us += red[q][1][i][at]; }
-  act_store<bf16_t>((bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64), m, n, ff, row_hit[m] && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
+  act_store<bf16_t>((bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64), m, n, ff, (named.rows[e] >> m & 1) && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
 }
 
-// A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.
+// A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.  A row takes nothing from an expert that it does
+// not name, not even 0 times an infinite weight: each expert's sum joins the rows that name it.
 __global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const int* __restrict__ ids, int T, int k, int E, int d,
                                                           int ff, int shares, float* part, void* y, int y_type, long long ldy) {
   constexpr int U = 8;
   __shared__ NamedExperts named;
   __shared__ unsigned short list[MAX_EXPERTS];
   __shared__ float red[8][4][64];
+  __shared__ int n_named;
   const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
   const int Nt = (d + 15) >> 4, Kt = (ff + 31) >> 5, nt = blockIdx.x % Nt, share = blockIdx.x / Nt;
-  name_experts(named, ids, T * k, E);
-  int all;
-  {
-    unsigned word = lane < 32 ? named.bits[lane] : 0u;
-    int at = named_before(word, lane, all);
-    if (w == 0 && lane < 32)
-      for (; word; word &= word - 1) list[at++] = (unsigned short)(lane * 32 + __builtin_ctz(word));
+  name_experts(named, ids, T, k, E);
+  if (w == 0) {
+    int n = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+      const bool on = e0 + lane < E && named.rows[min(e0 + lane, E - 1)] != 0;
+      const u64 at = __ballot(on);
+      if (on) list[n + __popcll(at & ((1ull << lane) - 1))] = (unsigned short)(e0 + lane);
+      n += __popcll(at);
+    }
+    if (lane == 0) n_named = n;
   }
   __syncthreads();
-  const int total = all * Kt, parts = shares * 8, me = share * 8 + w;
+  const int total = n_named * Kt, parts = shares * 8, me = share * 8 + w;
   const int q0 = (int)((long long)total * me / parts), q1 = (int)((long long)total * (me + 1) / parts);
   const bool live = (lane & 15) < T;
   f32x4 c = (f32x4){0.f, 0.f, 0.f, 0.f};
-  const uint4* W = (const uint4*)w2 + lane;
-  const uint4* H = hidden + lane;
-  for (int q = q0; q < q1; q += U) {
-    uint4 a[U], h[U];
+  for (int j = q0 / Kt, q = q0; q < q1; ++j) {          // expert by expert
+    const int e = __builtin_amdgcn_readfirstlane((int)list[j]), end = min(q1, (j + 1) * Kt);
+    const unsigned rows = named.rows[e];
+    const uint4* W = (const uint4*)w2 + (((size_t)e * Nt + nt) * Kt - (size_t)j * Kt) * 64 + lane;
+    const uint4* H = hidden + lane;
+    f32x4 p = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (; q < end; q += U) {
+      uint4 a[U], h[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int qc = min(q + i, q1 - 1), j = qc / Kt, e = __builtin_amdgcn_readfirstlane((int)list[j]);
-      a[i] = W[(((size_t)e * Nt + nt) * Kt + (qc - j * Kt)) * 64];
-      h[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (live && q + i < q1) h[i] = H[(size_t)qc * 64];
+      for (int i = 0; i < U; ++i) {
+        const int qc = min(q + i, end - 1);
+        a[i] = W[(size_t)qc * 64];
+        h[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && q + i < end) h[i] = H[(size_t)qc * 64];
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) p = mfma_f16(h[i], a[i], p);
     }
+    q = end;
 #pragma unroll
-    for (int i = 0; i < U; ++i) c = mfma_f16(h[i], a[i], c);
+    for (int i = 0; i < 4; ++i) c[i] += rows >> ((lane >> 4) * 4 + i) & 1 ? p[i] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) red[w][i][lane] = c[i];
@@ -254,15 +260,15 @@ __device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
   const f32x4 v = *reinterpret_cast<const f32x4*>(row + min(k, K - 4));
   return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
-// A workgroup: one column tile (of col_tiles) of one row block of MT row tiles.  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
+// A workgroup: one column tile (blockIdx.x) of one row block (blockIdx.y) of MT row tiles.  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
 // gathered rows.  MT = 4 from 17 rows an expert on: the weights are fetched once for 64 rows.
 template <bool UP, int MT>
-__global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out, int col_tiles) {
+__global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out) {
   constexpr int U = MT == 1 ? 4 : 2, MATS = UP ? 2 : 1;
   __shared__ f32x4 red[8][MT * MATS][64];
-  const int lane = threadIdx.x & 63, w = wave_index(), id = blockIdx.x / col_tiles, nt = blockIdx.x - id * col_tiles;
-  if (id >= *p.n_blocks) return;
-  const Block b = p.blocks[id];
+  const int lane = threadIdx.x & 63, w = wave_index(), nt = blockIdx.x;
+  if ((int)blockIdx.y >= *p.n_blocks) return;
+  const Block b = p.blocks[blockIdx.y];
   const float* x[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
@@ -396,10 +402,10 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   if (f32) {
     const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16;
 #define SPRINTER_EXPERTS_F32(MT) \
-    hipLaunchKernelGGL((k_experts_f32<true, MT>), dim3(up * blocks), dim3(512), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan, \
-                       (float*)w.hidden, up); \
-    hipLaunchKernelGGL((k_experts_f32<false, MT>), dim3(down * blocks), dim3(512), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, \
-                       w.plan, w.out, down)
+    hipLaunchKernelGGL((k_experts_f32<true, MT>), dim3(up, blocks), dim3(512), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan, \
+                       (float*)w.hidden); \
+    hipLaunchKernelGGL((k_experts_f32<false, MT>), dim3(down, blocks), dim3(512), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, \
+                       w.plan, w.out)
     if (block_rows == 16) { SPRINTER_EXPERTS_F32(1); } else { SPRINTER_EXPERTS_F32(4); }
 #undef SPRINTER_EXPERTS_F32
   } else {

@@ -5,7 +5,7 @@ using namespace sprinter;
 
 namespace {
 
-constexpr int MAX_EXPERT_PAIRS = 1 << 20;
+constexpr int MAX_EXPERT_PAIRS = 1 << 20, MAX_ROWS = 1 << 23;      // (a grid has fewer than 2^32 threads)
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 size_t element(int dtype) { return dtype == SPRINTER_F32 ? 4 : 2; }
@@ -41,7 +41,7 @@ int sprinter_route(const sprinter_route_cfg* cfg, const float* dev_logits, int64
                    int32_t* dev_ids, float* dev_weights, void* hip_stream) {
   if (!cfg) return op_fail(SPRINTER_E_NULL, "sprinter_route: NULL configuration");
   if (const char* e = route_cfg_error(*cfg)) return op_fail(SPRINTER_E_CONFIG, "sprinter_route: %s", e);
-  if (n_rows < 0) return op_fail(SPRINTER_E_RANGE, "sprinter_route: %d rows", n_rows);
+  if (n_rows < 0 || n_rows > MAX_ROWS) return op_fail(SPRINTER_E_RANGE, "sprinter_route: %d rows are not in [0, %d]", n_rows, MAX_ROWS);
   if (n_rows == 0) return SPRINTER_OK;
   if (!dev_logits || !dev_ids || !dev_weights) return op_fail(SPRINTER_E_NULL, "sprinter_route: NULL array");
   if (n_rows > 1 && ld_logits < cfg->n_expert)
@@ -111,7 +111,7 @@ int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, 
     return op_fail(SPRINTER_E_CONFIG, "sprinter_block_norm: kind %d is neither a layer norm nor an RMS norm", cfg->kind);
   if (cfg->d < 1 || cfg->d > MAX_BLOCK_COLS) return op_fail(SPRINTER_E_CONFIG, "sprinter_block_norm: d %d outside [1, %d]", cfg->d, MAX_BLOCK_COLS);
   if (!(cfg->eps >= 0.f) || !(cfg->scale == cfg->scale)) return op_fail(SPRINTER_E_CONFIG, "sprinter_block_norm: eps is negative or scale is NaN");
-  if (n_rows < 0) return op_fail(SPRINTER_E_RANGE, "sprinter_block_norm: %d rows", n_rows);
+  if (n_rows < 0 || n_rows > MAX_ROWS) return op_fail(SPRINTER_E_RANGE, "sprinter_block_norm: %d rows are not in [0, %d]", n_rows, MAX_ROWS);
   if (n_rows == 0) return SPRINTER_OK;
   if (!dev_h || !dev_y || !dev_gain || !dev_h_out || !dev_out) return op_fail(SPRINTER_E_NULL, "sprinter_block_norm: NULL array");
   if (dev_post_offset && !dev_post_gain) return op_fail(SPRINTER_E_NULL, "sprinter_block_norm: post_offset without post_gain");

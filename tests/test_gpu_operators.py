@@ -165,6 +165,39 @@ def test_experts_rows_do_not_meet(T, dtype):
     assert (room == 7.0).all()
 
 
+def _poison():
+    """Memory that later allocations take holds NaN."""
+    t = torch.full((1 << 28,), float("nan"), device=DEV)
+    del t
+
+
+@pytest.mark.parametrize("T, E, k, d, ff", [(3, 20, 6, 72, 40), (2100, 4, 2, 1032, 5480), (700, 4, 2, 520, 1352), (90, 4, 1, 264, 200)])
+def test_experts_odd_columns_in_every_tile(T, E, k, d, ff):
+    """Columns behind d and d_ff in the last k tile, on a workspace full of NaN: few rows, 256 x 256, 128 x 128, 64 x 128."""
+    wg, wu, w2, normal, g = _weights(E, d, ff, BF, T)
+    x = normal(T, d)
+    ids, w = _ops().route(normal(T, E, dt=FP), k)
+    experts = _ops().Experts(wg, wu, w2)
+    _poison()
+    _check_experts(experts(x, ids, w), x, ids, w, (wg, wu, w2))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("T", [4, 16, 50, 600])
+def test_experts_broken_expert(T, dtype):
+    """What an expert's weights hold reaches the rows that name it, and no other."""
+    E, k, d, ff = 6, 2, 128, 96
+    wg, wu, w2, normal, g = _weights(E, d, ff, dtype, T)
+    x = normal(T, d)
+    ids, w = _ops().route(normal(T, E, dt=FP), k)
+    clean = _ops().Experts(wg, wu, w2)(x, ids, w)
+    w2[2, 5], wu[3, 7] = float("inf"), float("nan")
+    y = _ops().Experts(wg, wu, w2)(x, ids, w)
+    touched = ((ids == 2) | (ids == 3)).any(1)
+    assert torch.equal(y[~touched], clean[~touched])
+    assert not torch.isfinite(y[touched]).all(1).any()
+
+
 @pytest.mark.parametrize("T", [1, 30, 500])
 def test_experts_again_and_beside_other_rows(T):
     """The same rows give the same bits on every run, and in another order of the batch."""

@@ -37,6 +37,7 @@ def test_route_arguments(lib):  # noqa: F811
     for args in ((None, 8, None, 1, A, A), (A, 8, None, 1, None, A), (A, 8, None, 1, A, None)):
         _refused(lib, lib.sprinter_route(c, *args, None), NULL, "NULL array")
     _refused(lib, lib.sprinter_route(c, A, 8, None, -1, A, A, None), RANGE, "-1 rows")
+    _refused(lib, lib.sprinter_route(c, A, 8, None, (1 << 23) + 1, A, A, None), RANGE, "rows")
     _refused(lib, lib.sprinter_route(c, A, 7, None, 2, A, A, None), RANGE, "8 logits")
     _refused(lib, lib.sprinter_route(c, A + 2, 8, None, 2, A, A, None), RANGE, "aligned")
     assert lib.sprinter_route(c, None, 0, None, 0, None, None, None) == 0
@@ -117,6 +118,7 @@ def test_block_norm_arguments(lib):  # noqa: F811
     _refused(lib, call(h=A + 2), RANGE, "aligned")
     _refused(lib, call(y=A + 1), RANGE, "aligned")
     _refused(lib, call(rows=-3), RANGE, "rows")
+    _refused(lib, call(rows=(1 << 23) + 1), RANGE, "rows")
     assert call(rows=0, h=None) == 0
 
 
