@@ -33,6 +33,7 @@ struct GemmTile {                                       // WM x WN waves, MT x N
 using TileL = GemmTile<2, 2, 8, 8, 4>;                  // 256 x 256, 128 KiB: one workgroup per compute unit
 using TileH = GemmTile<2, 2, 8, 4, 4>;                  // 256 x 128, for the last round of the one above
 using TileT = GemmTile<2, 2, 4, 8, 4>;                  // 128 x 256, for row blocks of at most 128 rows among those of the first one
+using TileQ = GemmTile<2, 2, 2, 8, 4>;                  // 64 x 256, of at most 64
 using TileG = GemmTile<4, 2, 4, 8, 4>;                  // 256 x 256 of eight waves, for GELU
 using TileM = GemmTile<2, 2, 4, 4, 5>;                  // 128 x 128, 80 KiB: two
 using TileS = GemmTile<2, 2, 2, 4, 6>;                  // 64 x 128, 72 KiB: two

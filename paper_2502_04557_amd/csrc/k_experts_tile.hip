@@ -34,8 +34,11 @@ __global__ __launch_bounds__(T::waves * 64, T::pinned ? 1 : 2) void k_expert_til
   a.Kt = t.Kt; a.N = t.N; a.n_tiles = (t.N + 15) >> 4; a.out_f32 = (float*)t.out; a.out_act = t.out; a.ldo = a.out_K = t.ldo;
   if constexpr (T::pinned) {
     if (id >= whole) { expert_tile<TileH, EPI>(a, t, b, 2 * bn + (halves & 1), lds); return; }
+    if (b.rows <= 64) { expert_tile<TileQ, EPI>(a, t, b, bn, lds); return; }
     if (b.rows <= 128) { expert_tile<TileT, EPI>(a, t, b, bn, lds); return; }
   }
+  if constexpr (std::is_same_v<T, TileM>)
+    if (b.rows <= 64) { expert_tile<TileS, EPI>(a, t, b, bn, lds); return; }
   expert_tile<T, EPI>(a, t, b, bn, lds);
 }
 
@@ -65,17 +68,17 @@ void launch_expert_tiles(int tile, const ExpertTiles& a, hipStream_t s) {
 }
 
 // Which tile, by the rows r that an expert has in the mean.  Whole calls, us, 256 x 256 / 128 x 128 / 64 x 128 / 32 x 64:
-//   8 experts of 4096 x 14336    r = 8: - / 497 / 477 / 489   24: 654 / 513 / 497 / 565   96: 723 / 757 / 803 / 1035   1024: 2599 / 3437 / 4399 / -
-//   64 of 2048 x 1024            r = 8: - / 151 / 148 / 149   24: 181 / 168 / 161 / 171   96: 249 / 231 / 225 / 307    128: 267 / 255 / 269 / 373   256: 342 / 383 / 439 / -
-//   16 of 1024 x 2816            r = 12: - / 70 / 64 / 57     32: 121 / 78 / 70 / 68      128: 141 / 100 / 113 / 152   512: 238 / 239 / 279 / -     1024: 397 / 419 / 488 / -
-//   4 of 2048 x 8192             r = 16: - / 128 / 115 / 96   32: 218 / 131 / 115 / 106   192: 233 / 172 / 177 / 271   512: 327 / 316 / 378 / -     1024: 482 / 554 / 661 / -
-//   32 of 512 x 1344             r = 8: - / 45 / 40 / 37      96: 85 / 57 / 52 / 63       256: 112 / 83 / 88 / -       1024: 271 / 240 / 281 / -
-// The largest tile has one workgroup per compute unit, so it needs three rounds of them and a K that hides its first loads and its
-// epilogue; the second narrowest one fills its two places per compute unit from 512 workgroups on.
+//   8 experts of 4096 x 14336    r = 8: - / 497 / 477 / 489   24: - / 513 / 497 / 565     64: 695 / 698 / 658 / 838    96: 723 / 765 / 749 / -      1024: 2599 / 3437 / 4399 / -
+//   64 of 2048 x 1024            r = 8: - / 151 / 148 / 149   24: - / 168 / 161 / 171     96: 237 / 226 / 234 / 307    192: 313 / 299 / 341 / -     224: 327 / 339 / 382 / -      512: 555 / 646 / 759 / -
+//   16 of 1024 x 2816            r = 12: - / 70 / 64 / 57     32: - / 78 / 70 / 68        128: 138 / 101 / 116 / -     384: 194 / 176 / 217 / -     512: 220 / 226 / 266 / -
+//   4 of 2048 x 8192             r = 16: - / 128 / 115 / 96   32: - / 131 / 115 / 106     192: 266 / 178 / 180 / -     512: 323 / 310 / 373 / -     768: 391 / 410 / 505 / -
+//   32 of 512 x 1344             r = 8: - / 45 / 40 / 37      96: 84 / 55 / 51 / 63       256: 114 / 82 / 86 / -       1024: 271 / 240 / 281 / -
+// The largest tile has one workgroup per compute unit, so it needs most of three rounds of them and a K that hides its first loads and
+// its epilogue; the narrowest one is ahead while 64 x 128 leaves compute units empty.
 int expert_tile_choice(int E, long long pairs, int d, int ff) {
-  const long long used = std::min<long long>(E, pairs), r = pairs / used;
-  const long long large = (pairs / 256 + (used + 1) / 2) * ((ff + 127) / 128);         // (an expert's last row block is half empty in the mean)
-  if (r >= 80 && d >= 1024 && std::max(large, used * ((ff + 127) / 128)) >= 768) return 0;
+  const long long used = std::min<long long>(E, pairs), r = pairs / used, cols = (ff + 127) / 128;
+  const long long large = std::max((pairs / 256 + (used + 1) / 2) * cols, used * cols);         // (an expert's last row block is half empty in the mean)
+  if (r >= 80 && d >= 1024 && large >= (d >= 2048 ? 683 : 768)) return 0;
   if (r > 112) return 1;
   return r <= 12 || (r <= 32 && used * ((ff + 63) / 64) <= 512) ? 3 : 2;
 }

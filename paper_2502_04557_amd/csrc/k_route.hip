@@ -31,11 +31,6 @@ __device__ __forceinline__ unsigned wave_umax(unsigned v) {
   v = dpp_max<0x142, 0xA>(v); v = dpp_max<0x143, 0xC>(v);
   return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
-__device__ __forceinline__ double read_lane(double v, int lane) {
-  const u64 u = (u64)__double_as_longlong(v);
-  const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
-  return __longlong_as_double((long long)(((u64)hi << 32) | lo));
-}
 __device__ __forceinline__ double shfl_xor_f64(double v, int o) { return __longlong_as_double((long long)shfl_xor_u64((u64)__double_as_longlong(v), o)); }
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
@@ -184,7 +179,7 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   }
   if (a.G > 1) {                                       // (uniform)
     // 64 / (G rounded up to a power of two) lanes per group find its two best keys
-    const int per = a.E / a.G, wide = a.G == 1 ? 1 : 1 << (32 - __clz(a.G - 1)), lanes = 64 / wide, g = lane / lanes, s = lane % lanes;
+    const int per = a.E / a.G, wide = 1 << (32 - __clz(a.G - 1)), lanes = 64 / wide, g = lane / lanes, s = lane % lanes;
 #pragma unroll
     for (int i = 0; i < N; ++i) keys[wave][i * 64 + lane] = key[i];
     __builtin_amdgcn_wave_barrier();                   // (LDS operations of one wave complete in order)
@@ -216,41 +211,48 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       if (!(taken >> (min(mine, a.G - 1) * lanes) & 1)) key[i] = 0;
     }
   }
-  const int n_out = a.k + a.shared;
-  int id = lane < a.k ? -1 : a.E + lane - a.k;         // lane j: the row's j-th id and weight
-  double w = lane < a.k ? 0.0 : 1.0, total = 0.0;
-  for (int j = 0; j < a.k; ++j) {
-    unsigned hi = (unsigned)(key[0] >> 32);
+  double* scores = reinterpret_cast<double*>(keys[wave]);
+  __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 1; i < N; ++i) hi = max(hi, (unsigned)(key[i] >> 32));
-    hi = wave_umax(hi);
-    if (hi == 0) break;                                // (scalar)
+  for (int i = 0; i < N; ++i) scores[i * 64 + lane] = p[i];
+  __builtin_amdgcn_wave_barrier();
+  unsigned hi[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) hi[i] = (unsigned)(key[i] >> 32);
+  int id = -1;                                         // lane j: the row's j-th
+  for (int j = 0; j < a.k; ++j) {
+    unsigned most = hi[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) most = max(most, hi[i]);
+    most = wave_umax(most);
+    if (most == 0) break;                              // (scalar)
     u64 at[N];
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) { at[i] = __ballot((unsigned)(key[i] >> 32) == hi); n += __popcll(at[i]); }
+    for (int i = 0; i < N; ++i) { at[i] = __ballot(hi[i] == most); n += __popcll(at[i]); }
     if (n > 1) {                                       // (scalar)
       unsigned lo = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) if ((unsigned)(key[i] >> 32) == hi) lo = max(lo, (unsigned)key[i]);
+      for (int i = 0; i < N; ++i) lo = hi[i] == most ? max(lo, (unsigned)key[i]) : lo;
       lo = wave_umax(lo);
 #pragma unroll
-      for (int i = 0; i < N; ++i) at[i] = __ballot((unsigned)(key[i] >> 32) == hi && (unsigned)key[i] == lo);
+      for (int i = 0; i < N; ++i) at[i] = __ballot(hi[i] == most && (unsigned)key[i] == lo);
     }
-    int e = -1, place = 0;
-    double pe = 0.0;
+    int e = 0;
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i)                   // the lowest index of the largest
-      if (at[i]) { place = __builtin_ctzll(at[i]); e = i * 64 + place; pe = read_lane(p[i], place); }
+    for (int i = N - 1; i >= 0; --i) e = at[i] ? i * 64 + __builtin_ctzll(at[i]) : e;       // the lowest index of the largest (scalar)
 #pragma unroll
-    for (int i = 0; i < N; ++i) if (i * 64 + lane == e) key[i] = 0;
-    if (lane == j) { id = e; w = pe; }
-    total += pe;
+    for (int i = 0; i < N; ++i) hi[i] = i * 64 + lane == e ? 0 : hi[i];
+    if (lane == j) id = e;
   }
-  if (lane < a.k) {
-    if (a.renorm) w = total > 0.0 ? w / total : 0.0;
-    w *= (double)a.scale;
+  double w = id >= 0 ? scores[id] : 0.0;
+  if (a.renorm) {
+    const double total = wave_sum64(w);
+    w = total > 0.0 ? w / total : 0.0;
   }
+  w *= (double)a.scale;
+  const int n_out = a.k + a.shared;
+  if (lane >= a.k) { id = a.E + lane - a.k; w = 1.0; }
   if (lane < n_out) {
     a.ids[row * n_out + lane] = id;
     a.weights[row * n_out + lane] = (float)w;

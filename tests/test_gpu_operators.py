@@ -165,6 +165,21 @@ def test_experts_rows_do_not_meet(T, dtype):
     assert (room == 7.0).all()
 
 
+@pytest.mark.parametrize("d, ff, T", [(1032, 5480, 1200), (264, 200, 1200)])
+def test_experts_short_blocks(d, ff, T):
+    """One row, and 20 and 100 rows, of an expert among row blocks of 256 and of 128."""
+    wg, wu, w2, normal, g = _weights(6, d, ff, BF, T)
+    x = normal(T, d)
+    ids = torch.randint(0, 3, (T, 4), generator=g, device=DEV, dtype=torch.int32)
+    ids[7, 0] = 3
+    ids[100:120, 1] = 4
+    ids[200:300, 2] = 5
+    w = torch.rand(T, 4, generator=g, device=DEV)
+    experts = _ops().Experts(wg, wu, w2)
+    _poison()
+    _check_experts(experts(x, ids, w), x, ids, w, (wg, wu, w2))
+
+
 def _poison():
     """Memory that later allocations take holds NaN."""
     t = torch.full((1 << 28,), float("nan"), device=DEV)
