@@ -49,7 +49,7 @@ __device__ __forceinline__ int xcd_run(int id, int n_blk) {
 // Row blocks of grouped products: the operand tiles from row tile tile0 on, rows up to `end`; or, with RowsGathered, row i is row
 // row_of[i] of a row-major float16 matrix (rows row_bytes apart, whole k tiles).  Four lanes next to each other fetch the 64 bytes of a
 // row's k tile (in the lane order of the operand they would be 16 lanes apart, which cost the 256 x 256 tile a fifth of its rate); in LDS
-// a row's octets are exchanged by row / 4, so that the fragment reads stay free of bank conflicts.
+// a row's octets are exchanged by row / 2 % 4, so that the fragment reads stay free of bank conflicts.
 struct RowsOfTiles { int tile0, end; };
 struct RowsGathered { int tile0, end; const int* row_of; long long row_bytes; };
 
@@ -80,7 +80,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, int x_tiles, int bm
     int tile;
     if (l < TMT) {
       if constexpr (GATHER) {
-        src[i] = (const char*)a.X + (long long)rows.row_of[min((row0 + l) * 16 + (lane >> 2), rows.end - 1)] * rows.row_bytes + ((lane & 3) ^ (lane >> 4)) * 16;
+        src[i] = (const char*)a.X + (long long)rows.row_of[min((row0 + l) * 16 + (lane >> 2), rows.end - 1)] * rows.row_bytes + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
         continue;
       }
       base = a.X;
@@ -109,7 +109,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, int x_tiles, int bm
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
   // this lane's 16 bytes of an activation tile in LDS, relative to its own of a weight tile
-  const int x_at = GATHER ? (lane & 15) * 4 + ((lane >> 4) ^ ((lane >> 2) & 3)) - lane : 0;
+  const int x_at = GATHER ? (lane & 15) * 4 + ((lane >> 4) ^ ((lane >> 1) & 3)) - lane : 0;
   struct Frag { u32x4 x[MT], w[NT]; };
   auto read = [&](Frag& f, int kt) {
     const u32x4* s = &ring[(kt - k0) % S][0][lane];
