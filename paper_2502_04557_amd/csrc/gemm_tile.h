@@ -48,7 +48,7 @@ __device__ __forceinline__ int xcd_run(int id, int n_blk) {
 
 // Row blocks of grouped products: the operand tiles from row tile tile0 on, rows up to `end`; or, with RowsGathered, row i is row
 // row_of[i] of a row-major float16 matrix (rows row_bytes apart, whole k tiles).  Four lanes next to each other fetch the 64 bytes of a
-// row's k tile (in the lane order of the operand they would be 16 lanes apart, which cost the 256 x 256 tile a fifth of its rate); in LDS
+// row's k tile (in the lane order of the operand they would be 16 lanes apart: 2002 for 1876 us at 8192 rows of 2 x 14336 x 4096); in LDS
 // a row's octets are exchanged by row / 2 % 4, so that the fragment reads stay free of bank conflicts.
 struct RowsOfTiles { int tile0, end; };
 struct RowsGathered { int tile0, end; const int* row_of; long long row_bytes; };

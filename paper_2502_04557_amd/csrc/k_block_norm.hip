@@ -6,8 +6,8 @@
 
 namespace sprinter {
 
-// u = norm(y; post) or y;  h' = h + scale gate u;  out = norm(h'; gain), one row per workgroup; the row stays in LDS between the steps.
-// Statistics are two-pass float32: the mean first, then the squares of what lies around it.
+// u = norm(y; post) or y;  h' = h + scale gate u;  out = norm(h'; gain).  Statistics are two-pass float32: the mean first, then the
+// squares of what lies around it.  k_block_norm takes any width and alignment, one row per workgroup, which stays in LDS between the steps.
 template <int YT> struct RowType { using type = float; };
 template <> struct RowType<X_BF16> { using type = bf16_t; };
 
@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256) void k_block_norm(BlockNormArgs a) {
 }
 
 // The same where rows, gains and gate lie at 16-byte addresses: a row in registers, 8 NI columns of 256 threads' chunks of 8 each, requested together
-// while the row before is worked on.  A workgroup takes rows gridDim.x apart.
+// while the row before is worked on.  A workgroup takes rows `stride` apart.  What bounds it: HBM; 4096 x 4096 with both norms and a gain per
+// column 37 us, 201 MB at 5.4 TB/s (through LDS, an element at a time: 62), one row 3.5 (12.4).
 template <int YT, int NI>
 __global__ __launch_bounds__(256) void k_block_norm_rows(BlockNormArgs a, int stride) {
   using Y = typename RowType<YT>::type;

@@ -15,6 +15,8 @@ namespace sprinter {
 //   plan       slots of the pairs, the rows of the slots, the list of row blocks; beside it the rows as float16
 //   up, down   hidden[slot], product[slot] (k_experts_tile.hip; float32 mode: here)
 //   combine    y[t] = sum over j
+// us of the launches: 4096 rows, 2 of 8 experts of 4096 x 14336: 13 + 1711 + 825 + 28; 1789 rows, 8 of 64 of 2048 x 1024: 9 + 196 + 107 + 19;
+// 61 rows, 2 of 8 of 4096 x 14336: 5 + 315 + 153 + 5 (2.8 GB at 6.0 TB/s); 1 row of them: 78 + 41 (0.7 GB at 5.9); 16 rows, 8 of 64: 73 + 39 + 4.
 
 // ------------------------------------------------------------------------------------------------------------------ plan
 // 8 elements of a row as float16
@@ -27,7 +29,7 @@ __device__ __forceinline__ uint4 as_f16(uint4 v) {
 
 // A counter per expert in LDS gives each pair its place among its expert's; the counts' prefix sums (rounded up to 16) are the experts'
 // first slots.  Every workgroup counts all pairs, those before its own share apart, and writes the slots of its share: the scattered
-// stores of one workgroup alone took 18 us for 14312 pairs.  The workgroups behind the `plans` of them copy x as float16 rows of whole k tiles.
+// stores of one workgroup alone took 18 us for 14312 pairs, now 9.  The workgroups behind the `plans` of them copy x as float16 rows of whole k tiles.
 __global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, int share, Plan p, int plans,
                                                        const bf16_t* __restrict__ x, long long ldx, uint4* __restrict__ rows, int T, int d) {
   __shared__ int count[MAX_EXPERTS], before[MAX_EXPERTS], slots[16], blocks[16];
@@ -261,7 +263,8 @@ __device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
   return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
 // A workgroup: one column tile (blockIdx.x) of one row block (blockIdx.y) of MT row tiles.  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
-// gathered rows.  MT = 4 from 17 rows an expert on: the weights are fetched once for 64 rows.
+// gathered rows.  MT = 4 from 17 rows an expert on: the weights are fetched once for 64 rows.  What bounds it: the weights, 67 MB of 8 experts of
+// 512 x 2048 in 15 us and 34 MB in 9.3 (four waves and a k tile at a time: 13.5 and 16.3).
 template <bool UP, int MT>
 __global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out) {
   constexpr int U = MT == 1 ? 4 : 2, MATS = UP ? 2 : 1;
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float
 }
 
 // --------------------------------------------------------------------------------------------------------------- combine
-// One thread per 4 columns of a row.
+// One thread per 4 columns of a row.  It reads what the product has just written: 117 MB in 19 us.
 __global__ __launch_bounds__(256) void k_experts_combine(const int* __restrict__ slot_of, const float* __restrict__ weights, const float* __restrict__ out, int k, int d,
                                                          int parts, void* y, int y_type, long long ldy) {
   const int t = blockIdx.x / parts, c = ((blockIdx.x - t * parts) * 256 + threadIdx.x) * 4;

@@ -77,7 +77,8 @@ __device__ __forceinline__ void take16(K (&key)[N], int k, int lane, K& mine, in
 // The scores rise with the logits, so the logits themselves are the keys, and only what is taken needs its exponential (and, unless the
 // weights are renormalised, the sum of the softmax all of them).  Where float64 scores meet although their logits do not - under- and
 // overflow - the wave takes the scores for keys, as the definition does.
-// What bounds it: the instructions of the selection rounds, about 45 for four rows (a row per wave: 50 for one).
+// What bounds it: the instructions of the selection rounds, about 45 for four rows (a row per wave: 50 for one).  16381 rows of 64 experts, 8
+// taken: 6.3 us (a row per wave 14.6; their 5 MB take 1.1 at the rate of a copy); one row 2.2.
 template <int N>
 __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
   const int lane = threadIdx.x & 15;
@@ -134,7 +135,8 @@ __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
 }
 
 // Every other case: one wave per row; lane l holds experts l, 64 + l, ...  A selection round looks at the keys' upper words, and at the
-// lower ones where more than one key has the largest upper word.
+// lower ones where more than one key has the largest upper word.  What bounds it: instructions, of which the exponentials and divisions in
+// 64 bits are a third.  4096 rows of 256 sigmoid scores in 8 groups, 8 taken: 11 us (groups one after the other: 17.5; 4.5 MB take 0.9).
 template <int N>
 __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   __shared__ u64 keys[4][N * 64];

@@ -289,6 +289,96 @@ def test_block_norm_rows_do_not_meet():
         assert torch.equal(hn[r], hn2[r]) and torch.equal(out[r], out2[r])
 
 
+# ------------------------------------------------------------------------------------------------------------- limits, refusals
+@pytest.mark.parametrize("T, E, k, d, ff", [(16, 1024, 8, 64, 24), (40, 600, 48, 64, 40), (3, 70, 60, 64, 16), (1, 1024, 64, 72, 8),
+                                            (16, 64, 64, 64, 32), (17, 1024, 1, 64, 64), (2000, 1024, 4, 64, 64)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_experts_many_experts(T, E, k, d, ff, dtype):
+    wg, wu, w2, normal, g = _weights(E, d, ff, dtype, E + k)
+    x = normal(T, d)
+    ids = torch.rand(T, E, generator=g, device=DEV).argsort(1)[:, :k].to(torch.int32).contiguous()
+    w = torch.rand(T, k, generator=g, device=DEV)
+    _check_experts(_ops().Experts(wg, wu, w2)(x, ids, w), x, ids, w, (wg, wu, w2))
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_experts_weights_beyond_32_bits(T):
+    E, d, ff = 40, 4096, 14336                           # 4.7 GB a matrix
+    wg, wu, w2, normal, g = _weights(E, d, ff, BF, T)
+    x = normal(T, d)
+    ids = torch.full((T, 2), E - 1, dtype=torch.int32, device=DEV)
+    ids[:, 1] = 36
+    w = torch.rand(T, 2, generator=g, device=DEV)
+    y = _ops().Experts(wg, wu, w2)(x, ids, w)
+    _check_experts(y, x, torch.where(ids == 36, 0, 1), w, tuple(m[[36, E - 1]] for m in (wg, wu, w2)))
+
+
+def test_rows_beyond_32_bits():
+    T, d = 530000, 4096                                  # 2.2e9 elements
+    h = torch.zeros(T, d, device=DEV)
+    y = torch.zeros(T, d, dtype=BF, device=DEV)
+    g = _rng(9)
+    last = g.standard_normal((5, d)).astype(np.float32)
+    h[-5:] = torch.from_numpy(last).to(DEV)
+    y[-5:] = torch.from_numpy(last[::-1].copy()).to(DEV).to(BF)
+    gain = torch.ones(d, device=DEV)
+    hn, out = _ops().block_norm(h, y, gain, post_gain=gain)
+    rh, bh, ro, bo = M.block_norm(last.astype(np.float64), y[-5:].cpu().double().numpy(), np.ones(d), post_gain=np.ones(d),
+                                  eps=float(np.float32(1e-5)), half=True)
+    assert (np.abs(hn[-5:].cpu().double().numpy() - rh) <= bh).all() and (np.abs(out[-5:].cpu().double().numpy() - ro) <= bo).all()
+    assert (hn[:-5:1000] == 0).all() and (out[:-5:1000] == 0).all()
+    del h, y, hn, out
+    T, E = 1 << 23, 264                                  # the most rows
+    logits = torch.zeros(T, E, device=DEV)
+    logits[-3:] = torch.from_numpy(g.standard_normal((3, E)).astype(np.float32)).to(DEV)
+    for bias in (None, np.zeros(E, np.float32)):
+        ids, w = _ops().route(logits, 3, bias=None if bias is None else torch.from_numpy(bias).to(DEV))
+        rid, _ = M.route(logits[-3:].cpu().numpy(), 3, bias=bias)
+        assert np.array_equal(ids[-3:].cpu().numpy(), rid) and (ids[:-3:4096].cpu() == torch.arange(3)).all()
+
+
+def test_wrong_tensors_are_refused():
+    from paper_2502_04557_amd.binding import SprinterError
+    ops = _ops()
+    f = lambda *s, dt=FP: torch.zeros(*s, dtype=dt, device=DEV)  # noqa: E731
+    for bad in (f(4, 8, dt=BF), f(8), f(8, 4).t(), f(4, 8).requires_grad_()):
+        with pytest.raises(ValueError):
+            ops.route(bad, 2)
+    with pytest.raises(ValueError):
+        ops.route(f(4, 8), 2, bias=f(7))
+    with pytest.raises(ValueError):
+        ops.route(f(4, 8), 2, bias=torch.zeros(8))
+    with pytest.raises(ValueError):
+        ops.route(f(4, 8), 2, score="linear")
+    with pytest.raises(SprinterError, match="top_k"):
+        ops.route(f(4, 8), 9)
+    with torch.no_grad():
+        ops.route(f(4, 8).requires_grad_(), 2)
+    e = ops.Experts(f(4, 16, 8, dt=BF), f(4, 16, 8, dt=BF), f(4, 8, 16, dt=BF))
+    ids, w = torch.zeros(3, 2, dtype=torch.int32, device=DEV), f(3, 2)
+    with pytest.raises(ValueError):
+        ops.Experts(f(4, 16, 8, dt=BF), f(4, 16, 8, dt=BF), f(4, 16, 8, dt=BF))
+    for x, i, ww in ((f(3, 8), ids, w), (f(3, 16, dt=BF), ids, w), (f(3, 8, dt=BF), ids.long(), w), (f(3, 8, dt=BF), ids[:2], w),
+                     (f(3, 8, dt=BF), ids, w.to(BF)), (f(3, 8, dt=BF), ids.t().contiguous().t(), w), (f(3, 8, dt=BF), None, w)):
+        with pytest.raises(ValueError):
+            e(x, i, ww)
+    with pytest.raises(SprinterError, match="16-byte"):
+        e(f(3, 12, dt=BF)[:, 2:10], ids, w)
+    with pytest.raises(SprinterError, match="columns"):
+        e(f(1, 8, dt=BF).expand(3, 8), ids, w)
+    assert e(f(0, 8, dt=BF), ids[:0], w[:0]).shape == (0, 8)
+    h, y, g = f(3, 8), f(3, 8, dt=BF), f(8)
+    for kw in (dict(gain=f(7)), dict(gain=g, gate=f(2, 8)), dict(gain=g, gate=f(8, dt=BF)), dict(gain=g, kind="batch"), dict(gain=g, h_out=f(3, 7)),
+               dict(gain=g, offset=f(8, dt=BF)), dict(gain=g.requires_grad_())):
+        with pytest.raises(ValueError):
+            ops.block_norm(h, y, **kw)
+    with pytest.raises(ValueError):
+        ops.block_norm(h, y.to(torch.float16), g)
+    with pytest.raises(SprinterError, match="post_offset"):
+        ops.block_norm(h, y, f(8), post_offset=f(8))
+    assert ops.block_norm(h[:0], y[:0], f(8))[1].shape == (0, 8)
+
+
 # ------------------------------------------------------------------------------------------------------------- run together
 def _block(E=8, d=256, ff=320, k=2, shared=1, seed=3, dtype=BF):
     wg, wu, w2, normal, g = _weights(E + shared, d, ff, dtype, seed)
