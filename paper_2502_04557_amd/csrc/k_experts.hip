@@ -8,9 +8,10 @@ namespace sprinter {
 // y[t] = sum_j w[t,j] W2[e] (silu(Wg[e] x_t) * (Wu[e] x_t)), e = ids[t,j].
 //
 // bf16 mode, up to 16 rows: they are one row tile of the matrix instruction, whoever names an expert.
-//   up_few     hidden[e][t] = w (silu(Wg x_t) * (Wu x_t)) for every expert that some row names, w = the sum of the row's weights for e,
-//              0 for rows that do not name it
-//   down_few   y[t] = sum over e of W2[e] hidden[e][t]: one product with a K of (experts named) x ff, no sum afterwards
+//   up_few     hidden[e][t] = silu(Wg x_t) * (Wu x_t) for every expert that some row names (0 for rows that do not name it), and the
+//              rows' weights for it
+//   down_few   y[t] = sum over e of w W2[e] hidden[e][t]: one launch over a K of (experts named) x ff, an expert's sum joining the rows that
+//              name it.  (The weight could ride in hidden, but small ones would push it below float16's normal numbers.)
 // Else:
 //   plan       slots of the pairs, the rows of the slots, the list of row blocks; beside it the rows as float16
 //   up, down   hidden[slot], product[slot] (k_experts_tile.hip; float32 mode: here)
@@ -127,10 +128,11 @@ __device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int E,
 // A workgroup: one expert's column tile of both matrices.  The 8 waves share K; 256 threads then finish an element each.  What bounds it: the
 // weights, at 6.0 - 6.4 TB/s (two column tiles per workgroup: 5.5; eight k tiles in flight per wave for four: as many or less).
 __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
-                                                        int T, int k, int E, int d, int ff, long long ldx, int x_type, int col_tiles, uint4* hidden) {
+                                                        int T, int k, int E, int d, int ff, long long ldx, int x_type, int col_tiles, uint4* hidden,
+                                                        float* row_weights) {
   constexpr int U = 4;
   __shared__ NamedExperts named;
-  __shared__ float red[8][2][4][64], row_w[FEW_ROWS];
+  __shared__ float red[8][2][4][64];
   const int tid = threadIdx.x, lane = tid & 63, w = wave_index();
   const int j = blockIdx.x / col_tiles, nt = blockIdx.x - j * col_tiles;
   name_experts(named, ids, T, k, E);
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) { red[w][0][i][lane] = g[i]; red[w][1][i][lane] = u[i]; }
-  {                                                     // the rows' weights for this expert: 32 threads to a row
+  if (nt == 0) {                                        // the rows' weights for this expert: 32 threads to a row
     const int m = tid >> 5;
     float s = 0.f;
     if (m < T)
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
         if (ids[m * k + i] == e) s += weights[m * k + i];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
-    if ((tid & 31) == 0) row_w[m] = s;
+    if ((tid & 31) == 0) row_weights[j * FEW_ROWS + m] = s;
   }
   __syncthreads();
   if (tid >= 256) return;
@@ -176,12 +178,12 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
   float gs = 0.f, us = 0.f;
 #pragma unroll
   for (int q = 0; q < 8; ++q) { gs += red[q][0][i][at]; us += red[q][1][i][at]; }
-  act_store<bf16_t>((bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64), m, n, ff, (named.rows[e] >> m & 1) && n < ff ? row_w[m] * (silu(gs) * us) : 0.f);
+  act_store<bf16_t>((bf16_t*)(hidden + (size_t)j * ((ff + 31) >> 5) * 64), m, n, ff, (named.rows[e] >> m & 1) && n < ff ? silu(gs) * us : 0.f);
 }
 
 // A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.  A row takes nothing from an expert that it does
 // not name, not even 0 times an infinite weight: each expert's sum joins the rows that name it.
-__global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const int* __restrict__ ids, int T, int k, int E, int d,
+__global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const float* __restrict__ row_weights, const int* __restrict__ ids, int T, int k, int E, int d,
                                                           int ff, int shares, float* part, void* y, int y_type, long long ldy) {
   constexpr int U = 8;
   __shared__ NamedExperts named;
@@ -209,6 +211,7 @@ __global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const 
   for (int j = q0 / Kt, q = q0; q < q1; ++j) {          // expert by expert
     const int e = __builtin_amdgcn_readfirstlane((int)list[j]), end = min(q1, (j + 1) * Kt);
     const unsigned rows = named.rows[e];
+    const float4 weight = *reinterpret_cast<const float4*>(row_weights + j * FEW_ROWS + (lane >> 4) * 4);
     const uint4* W = (const uint4*)w2 + (((size_t)e * Nt + nt) * Kt - (size_t)j * Kt) * 64 + lane;
     const uint4* H = hidden + lane;
     f32x4 p = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const 
     }
     q = end;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] += rows >> ((lane >> 4) * 4 + i) & 1 ? p[i] : 0.f;
+    for (int i = 0; i < 4; ++i) c[i] += rows >> ((lane >> 4) * 4 + i) & 1 ? (&weight.x)[i] * p[i] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) red[w][i][lane] = c[i];
@@ -350,7 +353,7 @@ bool few(int dtype, long long T) { return dtype == SPRINTER_BF16 && T <= FEW_ROW
 int few_shares(int d) { const int tiles = (d + 15) / 16; return (256 + tiles - 1) / tiles; }
 
 struct Space {
-  Plan plan; int slots, blocks; void *rows, *hidden; float* out; size_t bytes;
+  Plan plan; int slots, blocks; void *rows, *hidden; float *out, *row_weights; size_t bytes;
 };
 // pairs and experts bound the slots: every expert named rounds its own up to 16.
 Space space(void* base, int dtype, int E, int d, int ff, long long T, int k) {
@@ -361,6 +364,7 @@ Space space(void* base, int dtype, int E, int d, int ff, long long T, int k) {
   Space s{};
   if (few(dtype, T)) {
     s.hidden = take((size_t)named * FEW_ROWS * round_up(ff, 32) * 2);
+    s.row_weights = (float*)take((size_t)named * FEW_ROWS * 4);
     s.out = (float*)take((size_t)few_shares(d) * FEW_ROWS * d * 4);
   } else {
     s.slots = (int)((pairs + 15 * named + 15) / 16 * 16);
@@ -389,8 +393,8 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   if (few(a.dtype, a.T)) {
     const int up = (a.ff + 31) / 32 * 2, Nt = (a.d + 15) / 16, shares = few_shares(a.d);
     hipLaunchKernelGGL(k_experts_up_few, dim3(named * up), dim3(512), 0, s, a.wg, a.wu, a.x, a.ids, a.weights, a.T, a.k, a.E, a.d, a.ff, a.ldx, a.x_type, up,
-                       (uint4*)w.hidden);
-    hipLaunchKernelGGL(k_experts_down_few, dim3(Nt * shares), dim3(512), 0, s, a.w2, (const uint4*)w.hidden, a.ids, a.T, a.k, a.E, a.d, a.ff, shares, w.out, a.y, a.y_type, a.ldy);
+                       (uint4*)w.hidden, w.row_weights);
+    hipLaunchKernelGGL(k_experts_down_few, dim3(Nt * shares), dim3(512), 0, s, a.w2, (const uint4*)w.hidden, w.row_weights, a.ids, a.T, a.k, a.E, a.d, a.ff, shares, w.out, a.y, a.y_type, a.ldy);
     if (shares > 1)
       hipLaunchKernelGGL(k_experts_join, dim3(a.T * ((a.d + 255) / 256)), dim3(256), 0, s, w.out, shares, a.T, a.d, a.y, a.y_type, a.ldy);
     return;

@@ -64,7 +64,7 @@ def experts(x, ids, weights, wg, wu, w2, half):
         hid = s * u
         dh = 1.1 * dg * (u.abs() + du) + s.abs() * du + 8 * F32 * hid.abs()       # |silu'| < 1.1
         if half:
-            dh = dh * (1 + H16) + H16 * hid.abs() + TINY16 * (1 + 1 / w.abs().clamp_min(1e-3))     # (the weight may ride in it)
+            dh = dh * (1 + H16) + H16 * hid.abs() + TINY16
         a = w2[e].abs()
         out = hid @ w2[e].T
         do = dh @ a.T + (ff + 2) * F32 * ((hid.abs() + dh) @ a.T) + low * (hid.abs().sum(1, keepdim=True) + a.sum(1)) + 2 * H16 * low

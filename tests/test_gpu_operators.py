@@ -180,6 +180,16 @@ def test_experts_short_blocks(d, ff, T):
     _check_experts(experts(x, ids, w), x, ids, w, (wg, wu, w2))
 
 
+@pytest.mark.parametrize("T", [1, 16, 17, 600])
+@pytest.mark.parametrize("scale", [1e-6, 1e4])
+def test_experts_small_and_large_weights(T, scale):
+    """A row's weights scale its result and nothing else."""
+    wg, wu, w2, normal, g = _weights(5, 128, 96, BF, T)
+    x = normal(T, 128)
+    ids, w = _ops().route(normal(T, 5, dt=FP), 2, scale=scale)
+    _check_experts(_ops().Experts(wg, wu, w2)(x, ids, w), x, ids, w, (wg, wu, w2))
+
+
 def _poison():
     """Memory that later allocations take holds NaN."""
     t = torch.full((1 << 28,), float("nan"), device=DEV)
