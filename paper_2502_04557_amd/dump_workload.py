@@ -38,6 +38,8 @@ def main():
     args = ap.parse_args()
     base = W.config(args.config)
     cfg = replace(base, max_seq=max(base.max_seq, base.prompt_len + args.steps + args.warmup))
+    if cfg.draft.blocks or cfg.target.blocks:
+        raise SystemExit("the file format has no place for described blocks")
     weights = W.make_weights(cfg)
     prompts, plen = W.make_prompts(cfg)
     blobs, lines = [], ["SPRW1"]
