@@ -159,6 +159,18 @@ def test_speculative_rounds(dtype):
     p.close()
 
 
+@pytest.mark.parametrize("layers", [1, 2])
+def test_a_draft_of_experts_and_few_layers(layers):
+    from parity_util import compare_replay
+    cfg = W.mini_config("groups", W.DT_F32, batch=7, n_gen=8)
+    cfg = replace(cfg, draft=replace(cfg.draft, n_layer=layers, blocks=W.BlockCfg(4, 1, 72, "sigmoid", n_shared=2, gate=True, residual_scale=0.7)),
+                  target=replace(cfg.target, n_layer=layers))
+    p = _pair(cfg, ver_scale=8.0)
+    g, _ = p.gpu_generate(8)
+    print(compare_replay(cfg, g, p.oracle(8, forced=dict(tok=g["tok"], accept=g["accept"]))), flush=True)
+    p.close()
+
+
 def test_a_block_without_anything_is_the_dense_one():
     """A BlockCfg that describes nothing runs through other launches than a model without one, and agrees with the same oracle."""
     from parity_util import compare_replay
