@@ -265,62 +265,145 @@ __device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
   const f32x4 v = *reinterpret_cast<const f32x4*>(row + min(k, K - 4));
   return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
-// A workgroup: one column tile (blockIdx.x) of one row block (blockIdx.y) of MT row tiles.  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
-// gathered rows.  MT = 4 from 17 rows an expert on: the weights are fetched once for 64 rows.  What bounds it: the weights, 67 MB of 8 experts of
-// 512 x 2048 in 15 us and 34 MB in 9.3 (four waves and a k tile at a time: 13.5 and 16.3).
-template <bool UP, int MT>
+// A workgroup: one column tile (blockIdx.x) of one row block of 16 rows (blockIdx.y).  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
+// gathered rows.  What bounds it: the weights, 67 MB of 8 experts of 512 x 2048 in 15 us and 34 MB in 9.3 (four waves and a k tile at a
+// time: 13.5 and 16.3).
+template <bool UP>
 __global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out) {
-  constexpr int U = MT == 1 ? 4 : 2, MATS = UP ? 2 : 1;
-  __shared__ f32x4 red[8][MT * MATS][64];
+  constexpr int U = 4, MATS = UP ? 2 : 1;
+  __shared__ f32x4 red[8][MATS][64];
   const int lane = threadIdx.x & 63, w = wave_index(), nt = blockIdx.x;
   if ((int)blockIdx.y >= *p.n_blocks) return;
   const Block b = p.blocks[blockIdx.y];
-  const float* x[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int slot = b.slot + min(m * 16 + (lane & 15), b.rows - 1);
-    x[m] = X + (UP ? p.row_of[slot] : slot) * ldx;
-  }
+  const int slot = b.slot + min(lane & 15, b.rows - 1);
+  const float* x = X + (UP ? p.row_of[slot] : slot) * ldx;
   const size_t at = ((size_t)b.expert * N + min(nt * 16 + (lane & 15), N - 1)) * K;
-  f32x4 acc[MT][MATS];
+  f32x4 acc[MATS];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int q = 0; q < MATS; ++q) acc[m][q] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int q = 0; q < MATS; ++q) acc[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
   for (int kt = w; kt < (K + 15) >> 4; kt += 8 * U) {
-    f32x4 wv[U][MATS], xv[U][MT];
+    f32x4 wv[U][MATS], xv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = (kt + u * 8) * 16 + (lane >> 4) * 4;               // (behind K: zeros)
       wv[u][0] = load4(W + at, k, K);
       if (UP) wv[u][MATS - 1] = load4(W2 + at, k, K);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) xv[u][m] = load4(x[m], k, K);
+      xv[u] = load4(x, k, K);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int q = 0; q < MATS; ++q) acc[m][q] = product(xv[u][m], wv[u][q], acc[m][q]);
+      for (int q = 0; q < MATS; ++q) acc[q] = product(xv[u], wv[u][q], acc[q]);
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int q = 0; q < MATS; ++q) red[w][m * MATS + q][lane] = acc[m][q];
+  for (int q = 0; q < MATS; ++q) red[w][q][lane] = acc[q];
   __syncthreads();
-  // (row, column) of the block, one after the other; lane 16 (row / 4) + column holds four rows
-  for (int o = threadIdx.x; o < MT * 256; o += 512) {
-    const int m = o >> 4, n = nt * 16 + (o & 15), tile = (m >> 4) * MATS, from = ((m & 15) >> 2) * 16 + (o & 15), i = m & 3;
-    if (m >= b.rows || n >= N) continue;
-    float g = 0.f, u = 0.f;
+  if (threadIdx.x >= 256) return;
+  // lane 16 (row / 4) + column of an accumulator holds four rows
+  const int m = threadIdx.x >> 4, n = nt * 16 + (threadIdx.x & 15), from = (m >> 2) * 16 + (threadIdx.x & 15), i = m & 3;
+  if (m >= b.rows || n >= N) return;
+  float g = 0.f, u = 0.f;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      g += red[q][tile][from][i];
-      if (UP) u += red[q][tile + MATS - 1][from][i];
-    }
-    out[(size_t)(b.slot + m) * N + n] = UP ? silu(g) * u : g;
+  for (int q = 0; q < 8; ++q) {
+    g += red[q][0][from][i];
+    if (UP) u += red[q][MATS - 1][from][i];
   }
+  out[(size_t)(b.slot + m) * N + n] = UP ? silu(g) * u : g;
+}
+
+// The same for many rows: 64 rows x 64 columns (up: 32 of each matrix) per workgroup, both operands through LDS.  A stage is 32 k, 128 bytes
+// of 64 rows of each operand; eight lanes next to each other fetch a row's 128 bytes (one cache line), whose 16-byte units lie exchanged
+// by row % 8 in LDS, so that the fragment reads - 16 bytes of 16 rows - are free of bank conflicts.  A ring of four stages: at the top of
+// stage kc the wave waits for its own loads of it, the barrier makes that true for every wave and says that nobody reads stage kc - 1 any
+// more, whose place takes the loads of kc + 3.
+// KS = 2: half the columns, and two of the waves take the other 16 k of a stage, for outputs whose workgroups would not fill the chip.
+template <bool UP, int KS>
+__global__ __launch_bounds__(256, 2) void k_experts_f32_tile(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out) {
+  constexpr int S = 4, WR = 64 / KS, COLS = UP ? WR / 2 : WR, PER = (64 + WR) / 32;
+  __shared__ __attribute__((aligned(1024))) f32x4 ring[S][64 + WR][8]; // rows 0 - 63: x; then the weights (up: half of them of each matrix)
+  if ((int)blockIdx.y >= *p.n_blocks) return;
+  const Block b = p.blocks[blockIdx.y];
+  const int lane = threadIdx.x & 63, w = wave_index(), n0 = blockIdx.x * COLS, stages = (K + 31) >> 5;
+  const int unit = (lane & 7) ^ (lane >> 3);            // what this lane fetches of its rows' stage
+  const float* src[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = (w * PER + i) * 8 + (lane >> 3);
+    if ((w * PER + i) * 8 < 64) {                       // (scalar)
+      const int slot = b.slot + min(r, b.rows - 1);
+      src[i] = X + (UP ? p.row_of[slot] : slot) * ldx;
+    } else {
+      const int c = r - 64, n = min(n0 + c % COLS, N - 1);
+      src[i] = (UP && c >= COLS ? W2 : W) + ((size_t)b.expert * N + n) * K;
+    }
+  }
+  auto issue = [&](int kc) {                            // (units behind K: its last one again; stages behind the last one: never read)
+    const int k = min(min(kc, stages - 1) * 32 + unit * 4, K - 4);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[i] + k),
+                                       (__attribute__((address_space(3))) void*)&ring[kc % S][(w * PER + i) * 8][0], 16, 0, 0);
+  };
+  const int l16 = lane & 15, q4 = lane >> 4, wm = (w & 1) * 32, wn = KS == 1 ? w >> 1 : 0, half = w >> 1;
+  const int wr[2] = {64 + wn * (UP ? 16 : 32), UP ? 64 + COLS + wn * 16 : 80 + wn * 32};     // this wave's two weight tiles
+  f32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) acc[i][0] = acc[i][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i) issue(i);
+  for (int kc = 0; kc < stages; ++kc) {
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 2) * PER) : "memory");
+    issue(kc + S - 1);
+    const auto& st = ring[kc % S];
+    const bool tail = kc * 32 + 32 > K;                 // (scalar)
+#pragma unroll
+    for (int h = 0; h < 2 / KS; ++h) {
+      const int u = (KS == 1 ? h : half) * 4 + q4, at = u ^ (l16 & 7);
+      f32x4 xv[2], wv[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { xv[i] = st[wm + i * 16 + l16][at]; wv[i] = st[wr[i] + l16][at]; }
+      if (tail && kc * 32 + u * 4 >= K) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xv[i] = wv[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv[i][e], wv[j][e], acc[i][j], 0, 0, 0);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the last stages' loads still write to LDS
+  if constexpr (KS == 2) {                              // the halves of K: the first two waves add the others' to theirs
+    __syncthreads();
+    f32x4(*other)[4][64] = reinterpret_cast<f32x4(*)[4][64]>(&ring[0][0][0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (half) other[w & 1][i][lane] = acc[i >> 1][i & 1];
+    __syncthreads();
+    if (half) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] += other[w][i][lane];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int m = wm + i * 16 + q4 * 4 + v;
+      if (m >= b.rows) continue;
+      float* row = out + (size_t)(b.slot + m) * N;
+      if (UP) {
+        const int n = n0 + wn * 16 + l16;
+        if (n < N) row[n] = silu(acc[i][0][v]) * acc[i][1][v];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int n = n0 + wn * 32 + j * 16 + l16;
+          if (n < N) row[n] = acc[i][j][v];
+        }
+      }
+    }
 }
 
 // --------------------------------------------------------------------------------------------------------------- combine
@@ -347,6 +430,9 @@ void launch_pack_experts(const void* w, void* out, int E, int N, int K, hipStrea
 }
 
 namespace {
+// Float32: rows of a block, by the rows r that an expert has in the mean.  us of up + down, 16 / 64: 8 experts of 512 x 2048 at r = 12 20 + 16 /
+// 28 + 31, 24 28 + 18 / 29 + 31, 50 49 + 32 / 28 + 31; 16 of 1024 x 2048 at r = 16 86 + 48 / 96 + 50, 32 129 + 76 / 97 + 51, 128 418 + 248 / 236 + 142.
+int f32_block_rows(int r) { return r > 24 ? 64 : 16; }
 bool few(int dtype, long long T) { return dtype == SPRINTER_BF16 && T <= FEW_ROWS; }
 // Shares of the K of down_few: a workgroup per compute unit.  us, 1 / 2 / 4 shares with the launch that joins them: 2 experts of 4096 x 14336
 // 42 / 45 / 45, 56 of 2048 x 1024 (half as many column tiles) 65 / 45 / 46.
@@ -400,21 +486,26 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
     return;
   }
   const bool f32 = a.dtype == SPRINTER_F32, copy = !f32 && a.x_type != X_F16;
-  const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? (pairs > 16 * named ? 64 : 16) : expert_tile_rows(tile);
+  const int tile = f32 ? 0 : expert_tile_choice(a.E, pairs, a.d, a.ff), block_rows = f32 ? f32_block_rows(pairs / named) : expert_tile_rows(tile);
   const int blocks = pairs / block_rows + named, parts = (a.d / 4 + 255) / 256;
   const int share = std::max(1024, ((pairs + 15) / 16 + 1023) / 1024 * 1024), plans = (pairs + share - 1) / share;       // up to 16 workgroups
   const int copies = copy ? (int)std::min<long long>(1024, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
   hipLaunchKernelGGL(k_experts_plan, dim3(plans + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, share, w.plan, plans, (const bf16_t*)a.x, a.ldx,
                      (uint4*)w.rows, a.T, a.d);
   if (f32) {
-    const int up = (a.ff + 15) / 16, down = (a.d + 15) / 16;
-#define SPRINTER_EXPERTS_F32(MT) \
-    hipLaunchKernelGGL((k_experts_f32<true, MT>), dim3(up, blocks), dim3(512), 0, s, (const float*)a.wg, (const float*)a.wu, (const float*)a.x, a.ldx, a.ff, a.d, w.plan, \
-                       (float*)w.hidden); \
-    hipLaunchKernelGGL((k_experts_f32<false, MT>), dim3(down, blocks), dim3(512), 0, s, (const float*)a.w2, nullptr, (const float*)w.hidden, (long long)a.ff, a.d, a.ff, \
-                       w.plan, w.out)
-    if (block_rows == 16) { SPRINTER_EXPERTS_F32(1); } else { SPRINTER_EXPERTS_F32(4); }
-#undef SPRINTER_EXPERTS_F32
+    const float *x = (const float*)a.x, *hidden = (const float*)w.hidden;
+    if (block_rows == 64) {
+      // in halves where whole columns would give a compute unit less than two workgroups
+      const int up = (a.ff + 31) / 32, down = (a.d + 63) / 64, live = pairs / 64 + (named + 1) / 2;
+      if (up * live >= 512) hipLaunchKernelGGL((k_experts_f32_tile<true, 1>), dim3(up, blocks), dim3(256), 0, s, (const float*)a.wg, (const float*)a.wu, x, a.ldx, a.ff, a.d, w.plan, (float*)w.hidden);
+      else hipLaunchKernelGGL((k_experts_f32_tile<true, 2>), dim3((a.ff + 15) / 16, blocks), dim3(256), 0, s, (const float*)a.wg, (const float*)a.wu, x, a.ldx, a.ff, a.d, w.plan, (float*)w.hidden);
+      if (down * live >= 512) hipLaunchKernelGGL((k_experts_f32_tile<false, 1>), dim3(down, blocks), dim3(256), 0, s, (const float*)a.w2, nullptr, hidden, (long long)a.ff, a.d, a.ff, w.plan, w.out);
+      else hipLaunchKernelGGL((k_experts_f32_tile<false, 2>), dim3((a.d + 31) / 32, blocks), dim3(256), 0, s, (const float*)a.w2, nullptr, hidden, (long long)a.ff, a.d, a.ff, w.plan, w.out);
+    } else {
+      hipLaunchKernelGGL(k_experts_f32<true>, dim3((a.ff + 15) / 16, blocks), dim3(512), 0, s, (const float*)a.wg, (const float*)a.wu, x, a.ldx, a.ff, a.d, w.plan,
+                         (float*)w.hidden);
+      hipLaunchKernelGGL(k_experts_f32<false>, dim3((a.d + 15) / 16, blocks), dim3(512), 0, s, (const float*)a.w2, nullptr, hidden, (long long)a.ff, a.d, a.ff, w.plan, w.out);
+    }
   } else {
     launch_expert_tiles(tile, ExpertTiles{w.plan, blocks, w.slots, a.E, a.d, a.ff, a.wg, a.wu, a.w2, copy ? w.rows : a.x,
                                           copy ? (long long)round_up(a.d, 32) * 2 : a.ldx * 2, w.hidden, w.out}, s);

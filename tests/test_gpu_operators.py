@@ -108,7 +108,7 @@ BF, FP = torch.bfloat16, torch.float32
 @pytest.mark.parametrize("T, E, k, d, ff", [
     (1, 1, 1, 8, 8), (1, 8, 2, 256, 704), (2, 4, 4, 40, 24), (7, 8, 2, 512, 1344), (16, 64, 8, 128, 72), (16, 3, 1, 264, 520),
     (17, 8, 2, 256, 704), (31, 5, 3, 200, 136), (64, 16, 4, 320, 200), (100, 8, 2, 768, 1088), (257, 9, 2, 136, 264), (400, 4, 1, 256, 256),
-    (900, 6, 3, 328, 712), (2100, 4, 2, 256, 384)])
+    (900, 6, 3, 328, 712), (2100, 4, 2, 256, 384), (1500, 5, 4, 520, 264)])
 def test_experts(T, E, k, d, ff, dtype):
     wg, wu, w2, normal, g = _weights(E, d, ff, dtype, T * 1000 + E)
     x = normal(T, d)
