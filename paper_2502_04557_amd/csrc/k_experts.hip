@@ -314,7 +314,7 @@ __global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float
 // The same for many rows: 64 rows x 64 columns (up: 32 of each matrix) per workgroup, both operands through LDS.  A stage is 32 k, 128 bytes
 // of 64 rows of each operand; eight lanes next to each other fetch a row's 128 bytes (one cache line), whose 16-byte units lie exchanged
 // by row % 8 in LDS, so that the fragment reads - 16 bytes of 16 rows - are free of bank conflicts.  A ring of four stages: at the top of
-// stage kc the wave waits for its own loads of it, the barrier makes that true for every wave and says that nobody reads stage kc - 1 any
+// stage kc the wave waits for its own loads of it and its own reads of kc - 1, the barrier makes that true for every wave and says that nobody reads stage kc - 1 any
 // more, whose place takes the loads of kc + 3.
 // KS = 2: half the columns, and two of the waves take the other 16 k of a stage, for outputs whose workgroups would not fill the chip.
 template <bool UP, int KS>
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void k_experts_f32_tile(const float* W, con
 #pragma unroll
   for (int i = 0; i < S - 1; ++i) issue(i);
   for (int kc = 0; kc < stages; ++kc) {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 2) * PER) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * PER) : "memory");
     issue(kc + S - 1);
     const auto& st = ring[kc % S];
     const bool tail = kc * 32 + 32 > K;                 // (scalar)
