@@ -346,9 +346,9 @@ __global__ __launch_bounds__(256, 2) void k_experts_f32_tile(const float* W, con
   };
   const int l16 = lane & 15, q4 = lane >> 4, wm = (w & 1) * 32, wn = KS == 1 ? w >> 1 : 0, half = w >> 1;
   const int wr[2] = {64 + wn * (UP ? 16 : 32), UP ? 64 + COLS + wn * 16 : 80 + wn * 32};     // this wave's two weight tiles
-  f32x4 acc[2][2];
+  f32x4 sum[2 / KS][2][2];                              // a sum for each 16 k of a stage: half as long, half the roundings in a row
 #pragma unroll
-  for (int i = 0; i < 2; ++i) acc[i][0] = acc[i][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < 8 / KS; ++i) sum[i >> 2][i >> 1 & 1][i & 1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < S - 1; ++i) issue(i);
   for (int kc = 0; kc < stages; ++kc) {
@@ -371,10 +371,16 @@ __global__ __launch_bounds__(256, 2) void k_experts_f32_tile(const float* W, con
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv[i][e], wv[j][e], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < 2; ++j) sum[h][i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv[i][e], wv[j][e], sum[h][i][j], 0, 0, 0);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the last stages' loads still write to LDS
+  f32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    acc[i >> 1][i & 1] = sum[0][i >> 1][i & 1];
+    if constexpr (KS == 1) acc[i >> 1][i & 1] += sum[1][i >> 1][i & 1];
+  }
   if constexpr (KS == 2) {                              // the halves of K: the first two waves add the others' to theirs
     __syncthreads();
     f32x4(*other)[4][64] = reinterpret_cast<f32x4(*)[4][64]>(&ring[0][0][0]);
