@@ -31,14 +31,14 @@ __device__ __forceinline__ uint4 as_f16(uint4 v) {
 // A counter per expert in LDS gives each pair its place among its expert's; the counts' prefix sums (rounded up to 16) are the experts'
 // first slots.  Every workgroup counts all pairs, those before its own share apart, and writes the slots of its share: the scattered
 // stores of one workgroup alone took 18 us for 14312 pairs, now 9.  The workgroups behind the `plans` of them copy x as float16 rows of whole k tiles.
-__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, int share, Plan p, int plans,
+__global__ __launch_bounds__(1024) void k_experts_plan(const int* __restrict__ ids, int pairs, int k, int E, int block_rows, int share, Plan p, int plans, int copies,
                                                        const bf16_t* __restrict__ x, long long ldx, uint4* __restrict__ rows, int T, int d) {
   __shared__ int count[MAX_EXPERTS], before[MAX_EXPERTS], slots[16], blocks[16];
   constexpr int N = 8;                                  // ids of a thread that are requested together
   const int tid = threadIdx.x, lane = tid & 63, p0 = blockIdx.x * share, p1 = min(p0 + share, pairs);
   if ((int)blockIdx.x >= plans) {
     const int octets = round_up(d, 32) >> 3;
-    const long long n = (long long)T * octets, step = (long long)(gridDim.x - plans) * 1024;
+    const long long n = (long long)T * octets, step = (long long)copies * 1024;
     for (long long i = (long long)(blockIdx.x - plans) * 1024 + tid; i < n; i += step) {
       const int t = (int)(i / octets), c = (int)(i - (long long)t * octets) * 8;
       rows[i] = c < d ? as_f16(*reinterpret_cast<const uint4*>(x + t * ldx + c)) : make_uint4(0u, 0u, 0u, 0u);
@@ -103,10 +103,11 @@ constexpr int FEW_ROWS = 16;
 // The rows that name each expert, as bits in LDS, from the ids [T, k]; experts that no row names have none.  named_expert: the j-th that is
 // named, in rising order, for every wave by itself (-1: there are no more).
 struct NamedExperts { unsigned rows[MAX_EXPERTS]; };
+constexpr int FEW_THREADS = 512;                        // (no kernel here asks for its block's or grid's size, which would bring hidden arguments)
 __device__ __forceinline__ void name_experts(NamedExperts& s, const int* __restrict__ ids, int T, int k, int E) {
-  for (int e = threadIdx.x; e < E; e += blockDim.x) s.rows[e] = 0;
+  for (int e = threadIdx.x; e < E; e += FEW_THREADS) s.rows[e] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < T * k; i += blockDim.x) {
+  for (int i = threadIdx.x; i < T * k; i += FEW_THREADS) {
     const int e = ids[i];
     if ((unsigned)e < (unsigned)E) atomicOr(&s.rows[e], 1u << (i / k));
   }
@@ -127,7 +128,7 @@ __device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int E,
 
 // A workgroup: one expert's column tile of both matrices.  The 8 waves share K; 256 threads then finish an element each.  What bounds it: the
 // weights, at 6.0 - 6.4 TB/s (two column tiles per workgroup: 5.5; eight k tiles in flight per wave for four: as many or less).
-__global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
+__global__ __launch_bounds__(FEW_THREADS) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
                                                         int T, int k, int E, int d, int ff, long long ldx, int x_type, int col_tiles, uint4* hidden,
                                                         float* row_weights) {
   constexpr int U = 4;
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(512) void k_experts_up_few(const void* wg, const vo
 
 // A workgroup: one column tile of y and one of `shares` shares of K = (experts named) x ff.  A row takes nothing from an expert that it does
 // not name, not even 0 times an infinite weight: each expert's sum joins the rows that name it.
-__global__ __launch_bounds__(512) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const float* __restrict__ row_weights, const int* __restrict__ ids, int T, int k, int E, int d,
+__global__ __launch_bounds__(FEW_THREADS) void k_experts_down_few(const void* w2, const uint4* __restrict__ hidden, const float* __restrict__ row_weights, const int* __restrict__ ids, int T, int k, int E, int d,
                                                           int ff, int shares, float* part, void* y, int y_type, long long ldy) {
   constexpr int U = 8;
   __shared__ NamedExperts named;
@@ -496,7 +497,7 @@ void launch_experts(const ExpertsArgs& a, void* workspace, hipStream_t s) {
   const int blocks = pairs / block_rows + named, parts = (a.d / 4 + 255) / 256;
   const int share = std::max(1024, ((pairs + 15) / 16 + 1023) / 1024 * 1024), plans = (pairs + share - 1) / share;       // up to 16 workgroups
   const int copies = copy ? (int)std::min<long long>(1024, ((long long)a.T * round_up(a.d, 32) / 8 + 1023) / 1024) : 0;
-  hipLaunchKernelGGL(k_experts_plan, dim3(plans + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, share, w.plan, plans, (const bf16_t*)a.x, a.ldx,
+  hipLaunchKernelGGL(k_experts_plan, dim3(plans + copies), dim3(1024), 0, s, a.ids, pairs, a.k, a.E, block_rows, share, w.plan, plans, copies, (const bf16_t*)a.x, a.ldx,
                      (uint4*)w.rows, a.T, a.d);
   if (f32) {
     const float *x = (const float*)a.x, *hidden = (const float*)w.hidden;
