@@ -7,6 +7,7 @@ right type, shape or device ValueError.  There are no gradients: a tensor that a
 from __future__ import annotations
 import ctypes as C
 from functools import lru_cache
+from numbers import Integral
 import torch
 
 from .binding import F32, BF16, GROUP_SCORES, SCORES, RouteCfgC, SprinterError, load_library
@@ -60,6 +61,8 @@ def _rows(name, t, device, dtype, rows, cols):
     shape = t.shape
     if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError(f"{name}: shape {tuple(shape)}, expected [{rows or 'any'}, {cols or 'any'}]")
+    if shape[0] >= 2 ** 31:
+        raise ValueError(f"{name}: {shape[0]} rows are more than 32 bits hold")
     if not t.is_contiguous() and shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row are not adjacent")
 
@@ -79,6 +82,13 @@ def _device(t, name):
     return t.device
 
 
+def _int32(name, v):
+    """A whole number that the library's 32 bits hold (ctypes would cut others off and pass what is left)."""
+    if not isinstance(v, Integral) or not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name}: {v!r} is no whole number of 32 bits")
+    return v
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -87,6 +97,8 @@ def _ptr(t):
 def _route_cfg(n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale):
     if score not in SCORES or group_score not in GROUP_SCORES:
         raise ValueError(f"score is one of {tuple(SCORES)}, group_score one of {tuple(GROUP_SCORES)}")
+    for name, v in (("logits' columns", n_expert), ("top_k", top_k), ("n_group", n_group), ("top_group", top_group), ("n_shared", n_shared)):
+        _int32(name, v)
     c = RouteCfgC(n_expert, top_k, SCORES[score], n_group, top_group, GROUP_SCORES[group_score], bool(renormalize), n_shared, scale)
     return c, C.byref(c)
 
@@ -121,7 +133,7 @@ class Experts:
             _whole(name, t, dev, gate.dtype, *shape)
         self.device, self.dtype = dev, gate.dtype
         self.n_expert, self.d_ff, self.d_model = E, ff, d
-        self._cfg = ExpertsCfgC(DTYPES[gate.dtype], E, d, ff)
+        self._cfg = ExpertsCfgC(DTYPES[gate.dtype], _int32("n_expert", E), _int32("d_model", d), _int32("d_ff", ff))
         self._ref = C.byref(self._cfg)
         self._need = {}
         n_up, n_down, _ = self._bytes(0, 1)
@@ -136,6 +148,8 @@ class Experts:
     def _bytes(self, rows, top_k):
         n = self._need.get((rows, top_k))
         if n is None:
+            _int32("rows", rows)
+            _int32("ids' columns", top_k)
             v = [C.c_size_t(0) for _ in range(3)]
             rc = _entry("sprinter_experts_bytes")(self._ref, rows, top_k, *(C.byref(x) for x in v))
             if rc:
@@ -168,7 +182,7 @@ class Experts:
 def _norm_cfg(dtype, kind, d, eps, scale):
     if dtype not in DTYPES or kind not in NORMS:
         raise ValueError(f"y is bfloat16 or float32, kind one of {tuple(NORMS)}")
-    c = BlockNormCfgC(DTYPES[dtype], NORMS[kind], d, eps, scale)
+    c = BlockNormCfgC(DTYPES[dtype], NORMS[kind], _int32("d", d), eps, scale)
     return c, C.byref(c)
 
 
