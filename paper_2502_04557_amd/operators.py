@@ -7,7 +7,7 @@ right type, shape or device ValueError.  There are no gradients: a tensor that a
 from __future__ import annotations
 import ctypes as C
 from functools import lru_cache
-from numbers import Integral
+from numbers import Integral, Real
 import torch
 
 from .binding import F32, BF16, GROUP_SCORES, SCORES, RouteCfgC, SprinterError, load_library
@@ -89,6 +89,13 @@ def _int32(name, v):
     return v
 
 
+def _number(name, v):
+    """A plain number: the configurations are kept by their values, and a tensor's can change while it stays the same key."""
+    if not isinstance(v, Real):
+        raise ValueError(f"{name}: {type(v).__name__} is no plain number")
+    return v
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -97,9 +104,10 @@ def _ptr(t):
 def _route_cfg(n_expert, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale):
     if score not in SCORES or group_score not in GROUP_SCORES:
         raise ValueError(f"score is one of {tuple(SCORES)}, group_score one of {tuple(GROUP_SCORES)}")
-    for name, v in (("logits' columns", n_expert), ("top_k", top_k), ("n_group", n_group), ("top_group", top_group), ("n_shared", n_shared)):
+    for name, v in (("logits' columns", n_expert), ("top_k", top_k), ("n_group", n_group), ("top_group", top_group), ("n_shared", n_shared),
+                    ("renormalize", renormalize)):
         _int32(name, v)
-    c = RouteCfgC(n_expert, top_k, SCORES[score], n_group, top_group, GROUP_SCORES[group_score], bool(renormalize), n_shared, scale)
+    c = RouteCfgC(n_expert, top_k, SCORES[score], n_group, top_group, GROUP_SCORES[group_score], bool(renormalize), n_shared, _number("scale", scale))
     return c, C.byref(c)
 
 
@@ -182,7 +190,7 @@ class Experts:
 def _norm_cfg(dtype, kind, d, eps, scale):
     if dtype not in DTYPES or kind not in NORMS:
         raise ValueError(f"y is bfloat16 or float32, kind one of {tuple(NORMS)}")
-    c = BlockNormCfgC(DTYPES[dtype], NORMS[kind], _int32("d", d), eps, scale)
+    c = BlockNormCfgC(DTYPES[dtype], NORMS[kind], _int32("d", d), _number("eps", eps), _number("scale", scale))
     return c, C.byref(c)
 
 

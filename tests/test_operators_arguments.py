@@ -32,3 +32,23 @@ def test_shapes_beyond_32_bits_are_refused(lib):  # noqa: F811
         with pytest.raises(ValueError, match="32 bits"):
             e._bytes(rows, k)
     assert e._bytes(4, 2)[2] > 0
+
+
+# ------------------------------------------------------------------------------------------- numbers that can change in place
+@pytest.mark.parametrize("change", [dict(scale=torch.tensor(2.5)), dict(scale=torch.nn.Parameter(torch.tensor(2.5))), dict(renormalize=torch.tensor(True)),
+                                    dict(top_k=torch.tensor(2)), dict(scale="2.5"), dict(scale=None)])
+def test_an_option_of_a_route_is_a_plain_number(change):
+    """A tensor is the same key of the kept configurations after its value has changed, so the old value would be used again."""
+    with pytest.raises(ValueError):
+        ops._route_cfg(*{**ROUTE, **change}.values())
+
+
+def test_an_option_of_a_norm_is_a_plain_number():
+    scale = torch.tensor(0.5)
+    for eps, s in ((1e-5, scale), (torch.tensor(1e-5), 1.0)):
+        with pytest.raises(ValueError, match="plain number"):
+            ops._norm_cfg(torch.float32, "rms", 64, eps, s)
+    import numpy as np
+    assert ops._norm_cfg(torch.float32, "rms", 64, np.float32(1e-5), float(scale))[0].scale == 0.5
+    assert ops._route_cfg(*{**ROUTE, "top_k": np.int64(2), "scale": np.float64(2.5)}.values())[0].scale == 2.5
+    assert ops._route_cfg(*{**ROUTE, "renormalize": False}.values())[0].renormalize == 0
