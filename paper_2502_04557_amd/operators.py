@@ -2,13 +2,15 @@
 
 Argument marshalling only; every call runs the library's HIP kernels on the device and the current stream of its tensors, allocates its
 outputs (and workspace) through torch and waits for nothing.  What the library refuses raises SprinterError, what is no tensor of the
-right type, shape or device ValueError.  There are no gradients: a tensor that asks for one is refused.
+right type, shape or device ValueError.  There are no gradients: a tensor that asks for one, or that carries a tangent of forward mode,
+is refused.
 """
 from __future__ import annotations
 import ctypes as C
 from functools import lru_cache
 from numbers import Integral, Real
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from .binding import F32, BF16, GROUP_SCORES, SCORES, RouteCfgC, SprinterError, load_library
 
@@ -53,6 +55,8 @@ def _tensor(name, t, device, dtype):
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: gradients are not computed here; detach it")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name}: tangents are not computed here; unpack it")
 
 
 def _rows(name, t, device, dtype, rows, cols):

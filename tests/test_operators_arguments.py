@@ -52,3 +52,37 @@ def test_an_option_of_a_norm_is_a_plain_number():
     assert ops._norm_cfg(torch.float32, "rms", 64, np.float32(1e-5), float(scale))[0].scale == 0.5
     assert ops._route_cfg(*{**ROUTE, "top_k": np.int64(2), "scale": np.float64(2.5)}.values())[0].scale == 2.5
     assert ops._route_cfg(*{**ROUTE, "renormalize": False}.values())[0].renormalize == 0
+
+
+# ------------------------------------------------------------------------------------------------------- gradients, versions
+CPU = torch.device("cpu")
+
+
+@pytest.fixture
+def no_device(monkeypatch):
+    """The entry points up to the library's own call, on tensors of the CPU."""
+    calls = []
+    monkeypatch.setattr(ops, "_device", lambda t, name: t.device)
+    monkeypatch.setattr(ops, "_call", lambda name, *args: calls.append(name))
+    return calls
+
+
+def _experts():
+    return ops.Experts(torch.ones(4, 16, 8), torch.ones(4, 16, 8), torch.ones(4, 8, 16))
+
+
+def test_tangents_are_refused(no_device, lib):  # noqa: F811
+    import torch.autograd.forward_ad as fwd
+    f = lambda *s: torch.ones(*s)  # noqa: E731
+    ids, e = torch.zeros(3, 2, dtype=torch.int32), _experts()
+    with fwd.dual_level():
+        dual = lambda *s: fwd.make_dual(f(*s), f(*s))  # noqa: E731
+        for call in (lambda: ops.route(dual(3, 8), 2), lambda: ops.route(f(3, 8), 2, bias=dual(8)), lambda: e(dual(3, 8), ids, f(3, 2)),
+                     lambda: e(f(3, 8), ids, dual(3, 2)), lambda: ops.Experts(dual(4, 16, 8), f(4, 16, 8), f(4, 8, 16)),
+                     lambda: ops.block_norm(dual(3, 8), f(3, 8), f(8)), lambda: ops.block_norm(f(3, 8), dual(3, 8), f(8)),
+                     lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), gate=dual(8))):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        ops.route(f(3, 8), 2)                            # plain tensors pass beside dual ones
+        ops.route(fwd.unpack_dual(dual(3, 8)).primal, 2)
+    assert no_device == ["sprinter_route"] * 2
