@@ -100,6 +100,9 @@ def _number(name, v):
     return v
 
 
+_written = torch.autograd.graph.increment_version          # what autograd has kept of a tensor that is written in place is out of date
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -179,14 +182,17 @@ class Experts:
         k = ids.shape[1] if isinstance(ids, torch.Tensor) and ids.dim() == 2 else 0
         _whole("ids", ids, dev, torch.int32, T, k)
         _whole("weights", weights, dev, torch.float32, T, k)
-        if out is None:
-            out = torch.empty(T, self.d_model, dtype=self.dtype, device=dev)
-        else:
+        given = out is not None
+        if given:
             _rows("out", out, dev, self.dtype, T, self.d_model)
+        else:
+            out = torch.empty(T, self.d_model, dtype=self.dtype, device=dev)
         need = self._bytes(T, k)[2]
         work = torch.empty(need, dtype=torch.uint8, device=dev)
         _call("sprinter_experts", dev, self._ref, *self._ptrs, x.data_ptr(), x.stride(0), ids.data_ptr(), weights.data_ptr(), T, k,
               out.data_ptr(), out.stride(0), work.data_ptr(), need)
+        if given:
+            _written(out)
         return out
 
 
@@ -225,11 +231,14 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
         except RuntimeError as e:
             raise ValueError(f"gate: shape {tuple(gate.shape)} does not broadcast to {(T, d)}") from e
         gate_row, gate_col = gate.stride()
-    if h_out is None:
-        h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
-    else:
+    given = h_out is not None
+    if given:
         _rows("h_out", h_out, dev, torch.float32, T, d)
+    else:
+        h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
     out = torch.empty(T, d, dtype=y.dtype, device=dev)
     _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr(post_gain), _ptr(post_offset),
           _ptr(gate), gate_row, gate_col, gain.data_ptr(), _ptr(offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
+    if given:
+        _written(h_out)
     return h_out, out

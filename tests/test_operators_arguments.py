@@ -86,3 +86,16 @@ def test_tangents_are_refused(no_device, lib):  # noqa: F811
         ops.route(f(3, 8), 2)                            # plain tensors pass beside dual ones
         ops.route(fwd.unpack_dual(dual(3, 8)).primal, 2)
     assert no_device == ["sprinter_route"] * 2
+
+
+def test_a_tensor_written_in_place_is_known_to_autograd(no_device, lib):  # noqa: F811
+    """What autograd has saved for a backward pass and is then written by out= or h_out= makes that pass an error, not a wrong gradient."""
+    ids, w, e = torch.zeros(3, 2, dtype=torch.int32), torch.ones(3, 2), _experts()
+    for write in (lambda t: e(torch.ones(3, 8), ids, w, out=t), lambda t: ops.block_norm(t, torch.ones(3, 8), torch.ones(8), h_out=t),
+                  lambda t: ops.block_norm(torch.ones(3, 8), torch.ones(3, 8), torch.ones(8), h_out=t)):
+        leaf, t = torch.ones(3, 8, requires_grad=True), torch.ones(3, 8)
+        loss = (leaf * t).sum()
+        assert write(t)[0].shape[-1] == 8 and t._version == 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    assert ops.block_norm(torch.ones(3, 8), torch.ones(3, 8), torch.ones(8))[0]._version == 0
