@@ -75,8 +75,11 @@ __device__ __forceinline__ void take16(K (&key)[N], int k, int lane, K& mine, in
 
 // Without bias and groups, up to 256 experts and 16 of them: four rows per wave, 16 lanes each; lane l of a row holds experts l, 16 + l, ...
 // The scores rise with the logits, so the logits themselves are the keys, and only what is taken needs its exponential (and, unless the
-// weights are renormalised, the sum of the softmax all of them).  Where float64 scores meet although their logits do not - under- and
-// overflow - the wave takes the scores for keys, as the definition does.
+// weights are renormalised, the sum of the softmax all of them).  Float64 scores of different logits can meet: by under- and overflow, and
+// next to zero, where a float32 is finer than 1 + e^-l or l - max l in 64 bits.  There the wave takes the scores for keys, as the definition does.
+// Elsewhere neither order can differ from the other, so that a row's ids depend neither on the rows beside it nor on which kernel takes
+// it: logits are 0 or of magnitude 2^-20 and more, so differ by 2^-43 and more; l - max l (below 2^10) is then exact, and e^(l - max l) and
+// 1 / (1 + e^-l) differ by 2^-44 of their value and more (p (1 - p) dl: 1 - p > 2^-24 below l = 16, where dl is 2^-20), roundings being a few 2^-53.
 // What bounds it: the instructions of the selection rounds, about 45 for four rows (a row per wave: 50 for one).  16381 rows of 64 experts, 8
 // taken: 6.3 us (a row per wave 14.6; their 5 MB take 1.1 at the rate of a copy); one row 2.2.
 template <int N>
@@ -90,8 +93,10 @@ __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = l[min(i * 16 + lane, a.E - 1)];
   float low = INFINITY;
+  unsigned tiny = ~0u;                                 // least magnitude but 0, as bits, less 1
 #pragma unroll
   for (int i = 0; i < N; ++i) {
+    tiny = min(tiny, (__float_as_uint(x[i]) & 0x7fffffffu) - 1u);
     key[i] = i * 16 + lane < a.E ? sortable(x[i]) : 0;
     top = max(top, key[i]);
     low = key[i] ? fminf(low, x[i]) : low;
@@ -101,10 +106,19 @@ __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
   auto score = [&](float v) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : v == most ? 1.0 : exp((double)v - (double)most); };
   float mine;
   int id;
-  if (__ballot(top && (a.sigmoid ? most > 16.f || low < -700.f : !(most - low < 700.f)))) {
+  const bool meet = tiny < __float_as_uint(0x1p-20f) - 1u || (a.sigmoid ? most > 16.f || low < -700.f : !(most - low < 700.f));
+  if (__ballot(top && meet)) {
     u64 wide[N], value;
+    double p[N], part[4] = {0.0, 0.0, 0.0, 0.0}, sum = 1.0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) wide[i] = key[i] ? sortable(score(x[i])) : 0;
+    for (int i = 0; i < N; ++i) { p[i] = key[i] ? score(x[i]) : 0.0; part[i & 3] += p[i]; }
+    if (!a.sigmoid) {                                  // (in k_route's order: experts q 16 + lane + 64 i together)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) part[q] = sum16(part[q]);
+      sum = (part[0] + part[1]) + (part[2] + part[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) wide[i] = key[i] ? sortable(p[i] / sum) : 0;
     take16(wide, a.k, lane, value, id);
     mine = l[max(id, 0)];
   } else {
