@@ -336,7 +336,7 @@ int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* hos
  * configurations are host memory), dtype is SPRINTER_F32 or SPRINTER_BF16, a row stride (ld_*) counts elements.
  * No call keeps anything between calls, so two calls may run at once when their outputs and workspaces differ, and
  * all of them can be recorded into a HIP graph.  Errors as above, with the text in sprinter_last_error(NULL); a call
- * that is refused enqueues nothing. */
+ * that is refused enqueues nothing.  An error that HIP still holds for the thread from before a call is dropped by it. */
 
 /* Routing of a row (sprinter_route_cfg): scores p = softmax(logits) or sigmoid(logits), keys p + bias (the bias only decides who is taken).
  *   n_group     1: no groups; else the experts form n_group runs of n_expert / n_group, and only those of the

@@ -10,6 +10,8 @@ constexpr int MAX_EXPERT_PAIRS = 1 << 20, MAX_ROWS = 1 << 23;      // (a grid ha
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 size_t element(int dtype) { return dtype == SPRINTER_F32 ? 4 : 2; }
 
+// Around a call's launches.  An error that other code of the thread has left is not this call's: it is dropped before them.
+void launching() { (void)hipGetLastError(); }
 int launched(const char* what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SPRINTER_OK : op_fail(SPRINTER_E_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -48,6 +50,7 @@ int sprinter_route(const sprinter_route_cfg* cfg, const float* dev_logits, int64
     return op_fail(SPRINTER_E_RANGE, "sprinter_route: rows %lld apart hold no %d logits", (long long)ld_logits, cfg->n_expert);
   if (!aligned(dev_logits, 4) || !aligned(dev_bias, 4) || !aligned(dev_ids, 4) || !aligned(dev_weights, 4))
     return op_fail(SPRINTER_E_RANGE, "sprinter_route: an array is not aligned to its elements");
+  launching();
   launch_route(*cfg, dev_logits, ld_logits, dev_bias, n_rows, dev_ids, dev_weights, (hipStream_t)hip_stream);
   return launched("sprinter_route");
 }
@@ -70,6 +73,7 @@ int sprinter_experts_pack(const sprinter_experts_cfg* cfg, int down, const void*
   if (!dev_weights || !dev_packed) return op_fail(SPRINTER_E_NULL, "sprinter_experts_pack: NULL array");
   if (!aligned(dev_weights, 16) || !aligned(dev_packed, 16))
     return op_fail(SPRINTER_E_RANGE, "sprinter_experts_pack: an array is not 16-byte aligned");
+  launching();
   launch_pack_experts(dev_weights, dev_packed, cfg->n_expert, down ? cfg->d_model : cfg->d_ff, down ? cfg->d_ff : cfg->d_model,
                       (hipStream_t)hip_stream);
   return launched("sprinter_experts_pack");
@@ -97,6 +101,7 @@ int sprinter_experts(const sprinter_experts_cfg* cfg, const void* dev_gate, cons
   const int type = cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16;
   const ExpertsArgs a{cfg->dtype, cfg->n_expert, cfg->d_model, cfg->d_ff, dev_gate, dev_up, dev_down, dev_x, type, ld_x, dev_ids,
                       dev_route_weights, n_rows, top_k, dev_y, type, ld_y};
+  launching();
   launch_experts(a, dev_workspace, (hipStream_t)hip_stream);
   return launched("sprinter_experts");
 }
@@ -128,6 +133,7 @@ int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, 
   a.h = dev_h; a.ldh = ld_h; a.y = dev_y; a.y_type = type; a.ldy = ld_y; a.post_g = dev_post_gain; a.post_b = dev_post_offset;
   a.gate = dev_gate; a.gate_row = gate_row; a.gate_col = gate_col; a.g = dev_gain; a.b = dev_offset;
   a.h_out = dev_h_out; a.ld_h_out = ld_h_out; a.out = dev_out; a.out_type = type; a.ldo = ld_out;
+  launching();
   launch_block_norm(a, (hipStream_t)hip_stream);
   return launched("sprinter_block_norm");
 }
