@@ -227,10 +227,9 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       if (!(taken >> (min(mine, a.G - 1) * lanes) & 1)) key[i] = 0;
     }
   }
-  double* scores = reinterpret_cast<double*>(keys[wave]);
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int i = 0; i < N; ++i) scores[i * 64 + lane] = p[i];
+  for (int i = 0; i < N; ++i) keys[wave][i * 64 + lane] = (u64)__double_as_longlong(p[i]);       // the scores, in the keys' place and type
   __builtin_amdgcn_wave_barrier();
   unsigned hi[N];
 #pragma unroll
@@ -261,7 +260,7 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     for (int i = 0; i < N; ++i) hi[i] = i * 64 + lane == e ? 0 : hi[i];
     if (lane == j) id = e;
   }
-  double w = id >= 0 ? scores[id] : 0.0;
+  double w = id >= 0 ? __longlong_as_double((long long)keys[wave][id]) : 0.0;
   if (a.renorm) {
     const double total = wave_sum64(w);
     w = total > 0.0 ? w / total : 0.0;
