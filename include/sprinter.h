@@ -191,8 +191,8 @@ int sprinter_create(const sprinter_cfg* cfg, void* dev_workspace, size_t workspa
 /* A decoder block with more around and inside it than sprinter_model_cfg describes (SPRINTER_ARCH_LLAMA only):
  *   h += residual_scale * gate1 * post1(attention(norm1(h)));  h += residual_scale * gate2 * post2(ffn(norm2(h)))
  *   route.n_expert  0: ffn is the dense SwiGLU of d_ff; else a set of experts of hidden width d_expert (a multiple of
- *                   8; d_ff is then not used): the logits W_r norm2(h) are routed as route says (sprinter_route), and
- *                   ffn is the weighted sum of the experts taken and of route.n_shared shared ones (sprinter_experts)
+ *                   8; d_ff then has to be a valid one, but no weights have it): the logits W_r norm2(h) are routed as
+ *                   route says (sprinter_route), and ffn is the weighted sum of the experts taken and of route.n_shared shared ones (sprinter_experts)
  *   route_bias      1: the keys have a bias per expert
  *   post_norm       1: RMSNorm on what attention and ffn return (post1, post2); 0: neither
  *   gate            1: a gain per column on both (gate1, gate2); 0: neither
@@ -334,6 +334,7 @@ int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* hos
  * arrays and a stream; a context made by sprinter_create_blocks runs the same kernels inside its forward passes.
  * They enqueue work on hip_stream of the current device and wait for nothing; pointers are device memory (the
  * configurations are host memory), dtype is SPRINTER_F32 or SPRINTER_BF16, a row stride (ld_*) counts elements.
+ * Outputs and workspaces overlap neither each other nor an input unless it is said below.
  * No call keeps anything between calls, so two calls may run at once when their outputs and workspaces differ, and
  * all of them can be recorded into a HIP graph.  Errors as above, with the text in sprinter_last_error(NULL); a call
  * that is refused enqueues nothing.  An error that HIP still holds for the thread from before a call is dropped by it. */
@@ -348,7 +349,7 @@ int sprinter_get_stats(sprinter_ctx* ctx, sprinter_stats* host_out, int64_t* hos
  * Limits: n_expert 1024, top_k 48, n_group 64, n_shared 16, n_rows 2^23 (sprinter_block_norm too).
  *
  * ids and weights [n_rows, top_k + n_shared] of logits [n_rows, n_expert] (float32; rows ld_logits apart).  dev_bias
- * [n_expert] or NULL.  An expert whose logit is -inf or NaN is never taken; where fewer than top_k are left (a row may
+ * [n_expert] or NULL.  An expert whose logit or key is -inf or NaN is never taken; where fewer than top_k are left (a row may
  * have none) the remaining ids are -1 with weight 0.  Scores, keys and their sums are held in 64 bits. */
 int sprinter_route(const sprinter_route_cfg* cfg, const float* dev_logits, int64_t ld_logits, const float* dev_bias,
                    int n_rows, int32_t* dev_ids, float* dev_weights, void* hip_stream);

@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void k_block_norm(BlockNormArgs a) {
 
 // The same where rows, gains and gate lie at 16-byte addresses: a row in registers, 8 NI columns of 256 threads' chunks of 8 each, requested together
 // while the row before is worked on.  A workgroup takes rows `stride` apart.  What bounds it: HBM; 4096 x 4096 with both norms and a gain per
-// column 37 us, 201 MB at 5.4 TB/s (through LDS, an element at a time: 62), one row 3.5 (12.4).
+// column 42 us, 201 MB at 4.8 TB/s, of inputs that change from call to call (37 of the same ones, which the cache behind L2 keeps in part; 4095
+// columns through LDS, an element at a time: 96), one row 3.4 (12.4 through LDS).
 template <int YT, int NI>
 __global__ __launch_bounds__(256) void k_block_norm_rows(BlockNormArgs a, int stride) {
   using Y = typename RowType<YT>::type;

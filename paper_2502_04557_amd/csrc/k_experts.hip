@@ -16,8 +16,9 @@ namespace sprinter {
 //   plan       slots of the pairs, the rows of the slots, the list of row blocks; beside it the rows as float16
 //   up, down   hidden[slot], product[slot] (k_experts_tile.hip; float32 mode: here)
 //   combine    y[t] = sum over j
-// us of the launches: 4096 rows, 2 of 8 experts of 4096 x 14336: 13 + 1711 + 825 + 28; 1789 rows, 8 of 64 of 2048 x 1024: 9 + 196 + 107 + 19;
-// 61 rows, 2 of 8 of 4096 x 14336: 5 + 315 + 153 + 5 (2.8 GB at 6.0 TB/s); 1 row of them: 78 + 41 (0.7 GB at 5.9); 16 rows, 8 of 64: 73 + 39 + 4.
+// us of the launches, inputs and weights changing from call to call: 4096 rows, 2 of 8 experts of 4096 x 14336: 14 + 1730 + 857 + 28; 1789 rows,
+// 8 of 64 of 2048 x 1024: 11 + 211 + 111 + 20; 61 rows, 2 of 8 of 4096 x 14336: 5 + 322 + 154 + 5 (2.8 GB at 5.9 TB/s); 1 row of them: 80 + 41
+// (0.7 GB at 5.9); 16 rows, 8 of 64: 71 + 38 + 5 (49 experts are named: 0.63 GB at 5.7).
 
 // ------------------------------------------------------------------------------------------------------------------ plan
 // 8 elements of a row as float16
@@ -127,7 +128,7 @@ __device__ __forceinline__ int named_expert(const NamedExperts& s, int j, int E,
 }
 
 // A workgroup: one expert's column tile of both matrices.  The 8 waves share K; 256 threads then finish an element each.  What bounds it: the
-// weights, at 6.0 - 6.4 TB/s (two column tiles per workgroup: 5.5; eight k tiles in flight per wave for four: as many or less).
+// weights, at 5.7 - 5.9 TB/s (two column tiles per workgroup: 5.5; eight k tiles in flight per wave for four: as many or less).
 __global__ __launch_bounds__(FEW_THREADS) void k_experts_up_few(const void* wg, const void* wu, const void* x_, const int* __restrict__ ids, const float* __restrict__ weights,
                                                         int T, int k, int E, int d, int ff, long long ldx, int x_type, int col_tiles, uint4* hidden,
                                                         float* row_weights) {
@@ -267,8 +268,8 @@ __device__ __forceinline__ f32x4 load4(const float* row, int k, int K) {
   return k < K ? v : (f32x4){0.f, 0.f, 0.f, 0.f};
 }
 // A workgroup: one column tile (blockIdx.x) of one row block of 16 rows (blockIdx.y).  Eight waves share K.  up: out = silu(Wg x) * (Wu x) of the
-// gathered rows.  What bounds it: the weights, 67 MB of 8 experts of 512 x 2048 in 15 us and 34 MB in 9.3 (four waves and a k tile at a
-// time: 13.5 and 16.3).
+// gathered rows.  What bounds it: the weights, 67 MB of 8 experts of 512 x 2048 in 16.7 us and 34 MB in 10.9, 4.0 and 3.1 TB/s: streams this
+// short do not reach the rate of long ones.
 template <bool UP>
 __global__ __launch_bounds__(512) void k_experts_f32(const float* W, const float* W2, const float* X, long long ldx, int N, int K, Plan p, float* out) {
   constexpr int U = 4, MATS = UP ? 2 : 1;
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(256, 2) void k_experts_f32_tile(const float* W, con
 }
 
 // --------------------------------------------------------------------------------------------------------------- combine
-// One thread per 4 columns of a row.  It reads what the product has just written: 117 MB in 19 us.
+// One thread per 4 columns of a row.  It reads what the product has just written: 117 MB in 20 us.
 __global__ __launch_bounds__(256) void k_experts_combine(const int* __restrict__ slot_of, const float* __restrict__ weights, const float* __restrict__ out, int k, int d,
                                                          int parts, void* y, int y_type, long long ldy) {
   const int t = blockIdx.x / parts, c = ((blockIdx.x - t * parts) * 256 + threadIdx.x) * 4;
@@ -442,7 +443,9 @@ namespace {
 int f32_block_rows(int r) { return r > 24 ? 64 : 16; }
 bool few(int dtype, long long T) { return dtype == SPRINTER_BF16 && T <= FEW_ROWS; }
 // Shares of the K of down_few: a workgroup per compute unit.  us, 1 / 2 / 4 shares with the launch that joins them: 2 experts of 4096 x 14336
-// 42 / 45 / 45, 56 of 2048 x 1024 (half as many column tiles) 65 / 45 / 46.
+// 42 / 45 / 45, 56 of 2048 x 1024 (half as many column tiles) 65 / 45 / 46.  Fewer columns, whole calls of 16 rows and of 1, one share / this
+// rule: 8 experts of 256 x 704 11.1 / 10.3 and 7.3 / 8.6 (16 shares), 8 of 512 x 1344 16.3 / 13.1 and 8.0 / 9.1, 64 of them 82 / 50 and 13.6 / 11.5 (8),
+// 16 of 1024 x 2048 45 / 37 and 14.4 / 15.1 (4).
 int few_shares(int d) { const int tiles = (d + 15) / 16; return (256 + tiles - 1) / tiles; }
 
 struct Space {

@@ -8,9 +8,9 @@ namespace sprinter {
 // up: hidden[slot] = silu(Wg x) * (Wu x) of the gathered rows, float16 operand tiles; down: out[slot] = W2 hidden[slot], float32.  The
 // tiles and the loop are those of the dense products (gemm_tile.h); a row block's weights are its expert's.  How many blocks there are
 // is only known on the device, so the grid is the most there can be; the workgroups behind them end at once.
-// What bounds them: 8192 pairs, 8 experts of 4096 x 14336: 1711 and 825 us, 1.12 and 1.17 PFLOP/s of useful work (a library product of
+// What bounds them: 8192 pairs, 8 experts of 4096 x 14336: 1730 and 857 us, 1.11 and 1.12 PFLOP/s of useful work (a library product of
 // 8192 x 8192 x 8192: 1.22); the matrix instructions are busy 58 % of the cycles, the clock is 1.9 GHz, 7 % of the products are padding of
-// row blocks, and the last round is half empty.  14312 pairs, 64 experts of 2048 x 1024: 196 and 107 us for 537 and 268 MB of weights and 0.18
+// row blocks, and the last round is half empty.  14312 pairs, 64 experts of 2048 x 1024: 211 and 111 us for 537 and 268 MB of weights and 0.18
 // TFLOP: neither HBM nor the products are at their rate, the first loads and the epilogue of a tile are a fifth of its 64 k tiles.
 // Measured and dropped: rows gathered into operand tiles ahead (up 4 % faster, the gathering 22 - 31 us); a stage more in the ring (equal);
 // columns dealt out to the XCDs in turn, long row blocks first (5 % slower: the short ones, which wait for weights, no longer run beside
@@ -82,6 +82,8 @@ void launch_expert_tiles(int tile, const ExpertTiles& a, hipStream_t s) {
 //   32 of 512 x 1344             r = 8: - / 45 / 40 / 37      96: 84 / 55 / 51 / 63       256: 114 / 82 / 86 / -       1024: 271 / 240 / 281 / -
 // The largest tile has one workgroup per compute unit, so it needs most of three rounds of them and a K that hides its first loads and
 // its epilogue; the narrowest one is ahead while 64 x 128 leaves compute units empty.
+// r counts ids without an expert too, since only the device knows them: where a row's experts mostly lie on other devices the mean is too high by
+// the number of devices, and the tile that is taken for it the slower one (never a wrong one: row blocks follow the plan).
 int expert_tile_choice(int E, long long pairs, int d, int ff) {
   const long long used = std::min<long long>(E, pairs), r = pairs / used, cols = (ff + 127) / 128;
   const long long large = std::max((pairs / 256 + (used + 1) / 2) * cols, used * cols);         // (an expert's last row block is half empty in the mean)

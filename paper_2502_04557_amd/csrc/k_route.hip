@@ -81,7 +81,7 @@ __device__ __forceinline__ void take16(K (&key)[N], int k, int lane, K& mine, in
 // it: logits are 0 or of magnitude 2^-20 and more, so differ by 2^-43 and more; l - max l (below 2^10) is then exact, and e^(l - max l) and
 // 1 / (1 + e^-l) differ by 2^-44 of their value and more (p (1 - p) dl: 1 - p > 2^-24 below l = 16, where dl is 2^-20), roundings being a few 2^-53.
 // What bounds it: the instructions of the selection rounds, about 45 for four rows (a row per wave: 50 for one).  16381 rows of 64 experts, 8
-// taken: 6.3 us (a row per wave 14.6; their 5 MB take 1.1 at the rate of a copy); one row 2.2.
+// taken: 6.8 us by itself, 5.9 in a row of launches (a row per wave 14.6; their 5 MB take 1.1 at the rate of a copy); one row 2.2.
 template <int N>
 __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
   const int lane = threadIdx.x & 15;
@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256) void k_route_plain(RouteArgs a) {
 
 // Every other case: one wave per row; lane l holds experts l, 64 + l, ...  A selection round looks at the keys' upper words, and at the
 // lower ones where more than one key has the largest upper word.  What bounds it: instructions, of which the exponentials and divisions in
-// 64 bits are a third.  4096 rows of 256 sigmoid scores in 8 groups, 8 taken: 11 us (groups one after the other: 17.5; 4.5 MB take 0.9).
+// 64 bits are a third.  4096 rows of 256 sigmoid scores in 8 groups, 8 taken: 11.5 us by itself, 10.3 in a row of launches (groups one after the
+// other: 17.5; 4.5 MB take 0.9).
 template <int N>
 __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   __shared__ u64 keys[4][N * 64];

@@ -137,7 +137,11 @@ def route(logits, top_k, *, score="softmax", bias=None, n_group=1, top_group=1, 
 class Experts:
     """A set of experts on one device: gate, up [E, d_ff, d_model], down [E, d_model, d_ff], bfloat16 or float32.
 
-    bfloat16 weights are laid out once here (on the current stream) and may go afterwards; float32 ones are kept and read as they are."""
+    bfloat16 weights are laid out once here (on the current stream) and may go afterwards; float32 ones are kept and read as they are.
+
+    Arithmetic of bfloat16: the framework's for its bfloat16 models, matrix products of float16 operands with float32 sums.  Weights below 2^-14 lose
+    bits (below 2^-25: all), rows and hidden values silu(Wg x) * (Wu x) above 65504 become infinite, and hidden values are rounded to
+    2^-11, which adds less than 1 % to the mean distance of the result, a bfloat16, from 64 bits.  float32: float32 throughout."""
 
     def __init__(self, gate, up, down):
         dev = _device(gate, "gate")
