@@ -1,9 +1,9 @@
 """The operators of include/sprinter.h on torch tensors: routing to experts, the experts' products, the norms around a block.
 
 Argument marshalling only; every call runs the library's HIP kernels on the device and the current stream of its tensors, allocates its
-outputs (and workspace) through torch and waits for nothing.  What the library refuses raises SprinterError, what is no tensor of the
-right type, shape or device ValueError.  There are no gradients: a tensor that asks for one, or that carries a tangent of forward mode,
-is refused.
+outputs (and workspace) through torch and waits for nothing.  Options are plain numbers, no tensors.  What the library refuses raises
+SprinterError, what is no tensor of the right type, shape or device, or no such number, ValueError.  There are no gradients: a tensor that
+asks for one, or that carries a tangent of forward mode, is refused.
 """
 from __future__ import annotations
 import ctypes as C
@@ -126,6 +126,8 @@ def route(logits, top_k, *, score="softmax", bias=None, n_group=1, top_group=1, 
     T, E = logits.shape
     if bias is not None:
         _whole("bias", bias, dev, torch.float32, E)
+    if type(renormalize) is not bool and not isinstance(renormalize, torch.Tensor):
+        renormalize = bool(renormalize)                  # (numpy's, which is no Integral)
     cfg = _route_cfg(E, top_k, score, n_group, top_group, group_score, renormalize, n_shared, scale)
     n = max(0, top_k + n_shared)
     ids = torch.empty(T, n, dtype=torch.int32, device=dev)

@@ -99,3 +99,15 @@ def test_a_tensor_written_in_place_is_known_to_autograd(no_device, lib):  # noqa
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             loss.backward()
     assert ops.block_norm(torch.ones(3, 8), torch.ones(3, 8), torch.ones(8))[0]._version == 0
+
+
+def test_truth_values_of_numpy(no_device, monkeypatch):
+    import numpy as np
+    seen = []
+    monkeypatch.setattr(ops, "_call", lambda name, dev, cfg, *args: seen.append(cfg._obj.renormalize))
+    for v in (True, np.True_, 1, False, np.False_, 0):
+        ops._route_cfg.cache_clear()                     # (True and np.True_ are one key)
+        ops.route(torch.ones(3, 8), 2, renormalize=v)
+    assert seen == [1, 1, 1, 0, 0, 0]
+    with pytest.raises(ValueError, match="renormalize"):
+        ops.route(torch.ones(3, 8), 2, renormalize=torch.tensor(True))
