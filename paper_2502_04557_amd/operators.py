@@ -53,6 +53,8 @@ def _call(name, device, *args):
 def _tensor(name, t, device, dtype):
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
+    if t.is_neg():                                       # (its memory holds the values before the minus)
+        raise ValueError(f"{name}: a negated view; resolve_neg it")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: gradients are not computed here; detach it")
     if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:

@@ -111,3 +111,19 @@ def test_truth_values_of_numpy(no_device, monkeypatch):
     assert seen == [1, 1, 1, 0, 0, 0]
     with pytest.raises(ValueError, match="renormalize"):
         ops.route(torch.ones(3, 8), 2, renormalize=torch.tensor(True))
+
+
+def test_negated_views_are_refused(no_device, lib):  # noqa: F811
+    """The imaginary part of a conjugate is a view with a minus that its memory does not hold."""
+    def view(*s):
+        v = torch.complex(torch.ones(*s), torch.ones(*s)).conj().imag
+        assert v.is_neg() and (v == -1).all()
+        return v
+
+    f, e = torch.ones, _experts()
+    for call in (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), gate=view(3, 8)), lambda: ops.block_norm(f(3, 1), view(3, 1), f(1)),
+                 lambda: ops.route(view(3, 1), 1), lambda: e(f(1, 8), torch.zeros(1, 1, dtype=torch.int32), view(1, 1))):
+        with pytest.raises(ValueError, match="negated"):
+            call()
+    assert not no_device
+    ops.block_norm(f(3, 8), f(3, 8), f(8), gate=view(3, 8).resolve_neg())
