@@ -1,4 +1,4 @@
-"""The checker of the experts' outputs rejects what it is there for: fewer bits, a k tile, a column tile, an expert, an element."""
+"""The comparison of the experts' outputs rejects what it is there for: fewer bits, a k tile, a column tile, an expert, an element."""
 import pytest
 import torch
 import operator_checks as K
@@ -43,7 +43,7 @@ def _run(x, ids, w, mats, half, cut=None):
 
 @pytest.mark.parametrize("half", [False, True])
 @pytest.mark.parametrize("shape", SHAPES + [WIDE])
-def test_the_checker(shape, half):
+def test_what_is_wrong_is_rejected(shape, half):
     T, E, k, d, ff = shape
     x, ids, w, mats = _case(shape, half)
     ref, expected = K.experts(x, ids, w, *mats, half)
