@@ -22,6 +22,7 @@ EXPORTS = ("sprinter_workspace_bytes", "sprinter_create", "sprinter_create_stati
            "sprinter_create_blocks", "sprinter_load_weights", "sprinter_prefill",
            "sprinter_step", "sprinter_generate", "sprinter_sd_generate", "sprinter_set_tau", "sprinter_get_stats",
            "sprinter_route", "sprinter_experts_bytes", "sprinter_experts_pack", "sprinter_experts", "sprinter_block_norm",
+           "sprinter_cache_append", "sprinter_cache_attend_bytes", "sprinter_cache_attend", "sprinter_cache_keep", "sprinter_adjust_logits",
            "sprinter_destroy", "sprinter_last_error")
 
 
@@ -88,6 +89,11 @@ def load_library(path: str = LIB_PATH):
     lib.sprinter_experts_pack.argtypes = [vp, i32, vp, vp, vp]
     lib.sprinter_experts.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, i32, i32, vp, i64, vp, sz, vp]
     lib.sprinter_block_norm.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, i64, vp, i64, vp]
+    lib.sprinter_cache_append.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp]
+    lib.sprinter_cache_attend_bytes.argtypes = [vp, i32, i32, i32, i32, psz]
+    lib.sprinter_cache_attend.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, vp, vp, vp, i32, i32, C.c_float, vp, i64, i32, vp, i64, vp, sz, vp]
+    lib.sprinter_cache_keep.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, i64, i32, vp, vp]
+    lib.sprinter_adjust_logits.argtypes = [vp, vp]
     lib.sprinter_destroy.argtypes = [vp]
     lib.sprinter_destroy.restype = None
     lib.sprinter_last_error.argtypes = [vp]

@@ -35,6 +35,45 @@ int check_pairs(int n_rows, int top_k, const char* who) {
   return SPRINTER_OK;
 }
 
+constexpr int MAX_TREE_ROWS = 1 << 20;
+
+// What every call on a cache in pages has; fills *c for one layer's arrays.
+int check_cache(const sprinter_cache_cfg* g, int layer, const void* keys, const void* values, const int32_t* table, int64_t ld_table, int n_seq,
+                int n_table, const char* who, PagedArgs* c) {
+  if (!g) return op_fail(SPRINTER_E_NULL, "%s: NULL configuration", who);
+  if (g->dtype != SPRINTER_F32 && g->dtype != SPRINTER_BF16) return op_fail(SPRINTER_E_CONFIG, "%s: unknown dtype %d", who, g->dtype);
+  if (g->n_layer < 1 || g->n_layer > 65535) return op_fail(SPRINTER_E_CONFIG, "%s: n_layer %d outside [1, 65535]", who, g->n_layer);
+  if (g->n_page < 1) return op_fail(SPRINTER_E_CONFIG, "%s: n_page %d is not positive", who, g->n_page);
+  if (g->page_size < 8 || g->page_size > 1024 || (g->page_size & (g->page_size - 1)))
+    return op_fail(SPRINTER_E_CONFIG, "%s: page_size %d is no power of two in [8, 1024]", who, g->page_size);
+  if (g->n_kv_head < 1 || g->n_kv_head > 1024) return op_fail(SPRINTER_E_CONFIG, "%s: n_kv_head %d outside [1, 1024]", who, g->n_kv_head);
+  if (g->d_head != 64 && g->d_head != 128) return op_fail(SPRINTER_E_CONFIG, "%s: d_head %d is neither 64 nor 128", who, g->d_head);
+  if (layer < 0 || layer >= g->n_layer) return op_fail(SPRINTER_E_RANGE, "%s: layer %d outside [0, %d)", who, layer, g->n_layer);
+  if (n_seq < 0 || n_seq > MAX_TREE_ROWS) return op_fail(SPRINTER_E_RANGE, "%s: %d sequences are not in [0, %d]", who, n_seq, MAX_TREE_ROWS);
+  if (n_table < 0 || (long long)n_table * g->page_size >= 1 << 30)
+    return op_fail(SPRINTER_E_RANGE, "%s: %d pages of %d slots are not in [0, 2^30)", who, n_table, g->page_size);
+  if (!keys || !values || (!table && n_table > 0 && n_seq > 0)) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  if (n_seq > 1 && ld_table < n_table) return op_fail(SPRINTER_E_RANGE, "%s: rows %lld apart hold no %d pages", who, (long long)ld_table, n_table);
+  if (!aligned(keys, 16) || !aligned(values, 16)) return op_fail(SPRINTER_E_RANGE, "%s: keys or values are not 16-byte aligned", who);
+  if (!aligned(table, 4)) return op_fail(SPRINTER_E_RANGE, "%s: table is not aligned to its elements", who);
+  const long long off = (long long)layer * g->n_page * g->n_kv_head * g->page_size * g->d_head * element(g->dtype);
+  int shift = 0;
+  while (1 << shift < g->page_size) ++shift;
+  *c = PagedArgs{(char*)keys + off, (char*)values + off, table, ld_table, n_seq, n_table, g->n_page, shift, g->n_kv_head, g->d_head};
+  return SPRINTER_OK;
+}
+
+int check_heads(const sprinter_cache_cfg* g, int n_head, const char* who) {
+  if (n_head < 1 || n_head > 4096 || n_head % g->n_kv_head)
+    return op_fail(SPRINTER_E_RANGE, "%s: n_head %d is no multiple of n_kv_head %d up to 4096", who, n_head, g->n_kv_head);
+  return SPRINTER_OK;
+}
+
+int check_tree_rows(int n_rows, const char* who) {
+  if (n_rows < 0 || n_rows > MAX_TREE_ROWS) return op_fail(SPRINTER_E_RANGE, "%s: %d rows are not in [0, %d]", who, n_rows, MAX_TREE_ROWS);
+  return SPRINTER_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -136,6 +175,145 @@ int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, 
   launching();
   launch_block_norm(a, (hipStream_t)hip_stream);
   return launched("sprinter_block_norm");
+}
+
+int sprinter_cache_append(const sprinter_cache_cfg* cfg, int layer, void* dev_keys, void* dev_values, const int32_t* dev_table,
+                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_seq, const int32_t* dev_slot, const int32_t* dev_pos,
+                          const double* dev_freq, int n_turned, int pairs, int rows_dtype, const void* dev_k, int64_t ld_k, const void* dev_v,
+                          int64_t ld_v, const void* dev_q, int64_t ld_q, int n_head, int n_rows, void* dev_q_out, int64_t ld_q_out,
+                          void* hip_stream) {
+  const char* who = "sprinter_cache_append";
+  AppendArgs a{};
+  int rc = check_cache(cfg, layer, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
+  if (rc || (rc = check_tree_rows(n_rows, who)) || (n_head != 0 && (rc = check_heads(cfg, n_head, who)))) return rc;
+  if (n_turned < 0 || n_turned > cfg->d_head || n_turned % 2)
+    return op_fail(SPRINTER_E_RANGE, "%s: n_turned %d is no even number up to d_head %d", who, n_turned, cfg->d_head);
+  if (pairs != SPRINTER_PAIRS_HALVES && pairs != SPRINTER_PAIRS_NEIGHBOURS) return op_fail(SPRINTER_E_CONFIG, "%s: unknown pairs %d", who, pairs);
+  if (rows_dtype != SPRINTER_F32 && rows_dtype != SPRINTER_BF16) return op_fail(SPRINTER_E_CONFIG, "%s: unknown rows_dtype %d", who, rows_dtype);
+  if (n_rows == 0 || n_seq == 0) return SPRINTER_OK;
+  if (!dev_seq || !dev_slot || !dev_k || !dev_v || (n_turned && !dev_freq) || (n_head && (!dev_q || !dev_q_out)))
+    return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  const int w = cfg->n_kv_head * cfg->d_head, wq = n_head * cfg->d_head;
+  if (n_rows > 1 && (ld_k < w || ld_v < w || (n_head && (ld_q < wq || ld_q_out < wq))))
+    return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their columns", who);
+  const size_t in = element(rows_dtype), out = element(cfg->dtype);
+  if (!aligned(dev_seq, 4) || !aligned(dev_slot, 4) || !aligned(dev_pos, 4) || !aligned(dev_freq, 8) || !aligned(dev_k, in) || !aligned(dev_v, in) ||
+      (n_head && (!aligned(dev_q, in) || !aligned(dev_q_out, out))))
+    return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
+  a.cache_type = cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16;
+  a.row_type = rows_dtype == SPRINTER_F32 ? X_F32 : X_BF16;
+  a.H = n_head; a.T = n_rows; a.n_turned = n_turned; a.pairs = pairs;
+  a.seq = dev_seq; a.slot = dev_slot; a.pos = dev_pos; a.freq = dev_freq;
+  a.k = dev_k; a.ld_k = ld_k; a.v = dev_v; a.ld_v = ld_v; a.q = dev_q; a.ld_q = ld_q; a.q_out = dev_q_out; a.ld_q_out = ld_q_out;
+  launching();
+  launch_cache_append(a, (hipStream_t)hip_stream);
+  return launched(who);
+}
+
+int sprinter_cache_attend_bytes(const sprinter_cache_cfg* cfg, int n_head, int n_seq, int n_table, int n_rows, size_t* out_workspace) {
+  const char* who = "sprinter_cache_attend_bytes";
+  PagedArgs c;
+  const void* some = (const void*)256;                 // (only the sizes are looked at)
+  int rc = check_cache(cfg, 0, some, some, (const int32_t*)some, n_table, n_seq, n_table, who, &c);
+  if (rc || (rc = check_heads(cfg, n_head, who)) || (rc = check_tree_rows(n_rows, who))) return rc;
+  if (!out_workspace) return op_fail(SPRINTER_E_NULL, "%s: NULL result", who);
+  *out_workspace = attend_workspace(cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16, cfg->d_head, n_head, cfg->n_kv_head, n_seq, n_rows,
+                                    (long long)n_table * cfg->page_size);
+  return SPRINTER_OK;
+}
+
+int sprinter_cache_attend(const sprinter_cache_cfg* cfg, int layer, const void* dev_keys, const void* dev_values, const int32_t* dev_table,
+                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_len, const int32_t* dev_first,
+                          const uint64_t* dev_visible, int n_words, int n_head, float scale, const void* dev_q, int64_t ld_q, int n_rows,
+                          void* dev_y, int64_t ld_y, void* dev_workspace, size_t workspace_bytes, void* hip_stream) {
+  const char* who = "sprinter_cache_attend";
+  AttendArgs a{};
+  int rc = check_cache(cfg, layer, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
+  if (rc || (rc = check_heads(cfg, n_head, who)) || (rc = check_tree_rows(n_rows, who))) return rc;
+  if (dev_visible && (n_words < 1 || n_words > MAX_NODE_WORDS))
+    return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, n_words, MAX_NODE_WORDS);
+  if (!(scale - scale == 0.f)) return op_fail(SPRINTER_E_CONFIG, "%s: scale is not finite", who);
+  if (n_rows == 0 || n_seq == 0) return SPRINTER_OK;
+  if (!dev_len || !dev_first || !dev_q || !dev_y) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  const int w = n_head * cfg->d_head;
+  const size_t es = element(cfg->dtype);
+  if (n_rows > 1 && (ld_q < w || ld_y < w)) return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their %d columns", who, w);
+  if (!aligned(dev_q, 16) || !aligned(dev_y, 16) || (n_rows > 1 && ((ld_q * es) % 16 || (ld_y * es) % 16)))
+    return op_fail(SPRINTER_E_RANGE, "%s: rows are not 16-byte aligned", who);
+  if (!aligned(dev_len, 4) || !aligned(dev_first, 4) || !aligned(dev_visible, 8))
+    return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
+  a.type = cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16;
+  const size_t need = attend_workspace(a.type, cfg->d_head, n_head, cfg->n_kv_head, n_seq, n_rows, (long long)n_table * cfg->page_size);
+  if (need && !dev_workspace) return op_fail(SPRINTER_E_NULL, "%s: NULL workspace", who);
+  if (!aligned(dev_workspace, 256)) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace is not 256-byte aligned", who);
+  if (workspace_bytes < need) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+  a.H = n_head; a.T = n_rows; a.n_words = n_words; a.scale = scale; a.lens = dev_len; a.first = dev_first;
+  a.visible = (const unsigned long long*)dev_visible; a.q = dev_q; a.ld_q = ld_q; a.y = dev_y; a.ld_y = ld_y;
+  launching();
+  launch_cache_attend(a, dev_workspace, (hipStream_t)hip_stream);
+  return launched(who);
+}
+
+int sprinter_cache_keep(const sprinter_cache_cfg* cfg, void* dev_keys, void* dev_values, const int32_t* dev_table, int64_t ld_table, int n_seq,
+                        int n_table, const int32_t* dev_len, const int32_t* dev_first, const int32_t* dev_path, int64_t ld_path, int n_path,
+                        const int32_t* dev_n_keep, void* hip_stream) {
+  const char* who = "sprinter_cache_keep";
+  KeepArgs a{};
+  const int rc = check_cache(cfg, 0, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
+  if (rc) return rc;
+  if (n_path < 0) return op_fail(SPRINTER_E_RANGE, "%s: a path of %d", who, n_path);
+  if (n_seq == 0 || n_path == 0) return SPRINTER_OK;
+  if (!dev_len || !dev_first || !dev_path || !dev_n_keep) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  if (n_seq > 1 && ld_path < n_path) return op_fail(SPRINTER_E_RANGE, "%s: rows %lld apart hold no path of %d", who, (long long)ld_path, n_path);
+  if (!aligned(dev_len, 4) || !aligned(dev_first, 4) || !aligned(dev_path, 4) || !aligned(dev_n_keep, 4))
+    return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
+  a.n_layer = cfg->n_layer;
+  a.element = (int)element(cfg->dtype);
+  a.layer_bytes = (long long)cfg->n_page * cfg->n_kv_head * cfg->page_size * cfg->d_head * a.element;
+  a.lens = dev_len; a.first = dev_first; a.path = dev_path; a.ld_path = ld_path; a.n_path = n_path; a.n_keep = dev_n_keep;
+  launching();
+  launch_cache_keep(a, (hipStream_t)hip_stream);
+  return launched(who);
+}
+
+int sprinter_adjust_logits(const sprinter_logits* args, void* hip_stream) {
+  const char* who = "sprinter_adjust_logits";
+  if (!args) return op_fail(SPRINTER_E_NULL, "%s: NULL arguments", who);
+  const sprinter_logits& a = *args;
+  if (a.dtype != SPRINTER_F32 && a.dtype != SPRINTER_BF16) return op_fail(SPRINTER_E_CONFIG, "%s: unknown dtype %d", who, a.dtype);
+  if (a.vocab < 1 || a.vocab > 1 << 24) return op_fail(SPRINTER_E_CONFIG, "%s: vocab %d outside [1, 2^24]", who, a.vocab);
+  int rc = check_tree_rows(a.n_rows, who);
+  if (rc) return rc;
+  if (a.n_seq < 0 || a.n_seq > MAX_TREE_ROWS) return op_fail(SPRINTER_E_RANGE, "%s: %d sequences are not in [0, %d]", who, a.n_seq, MAX_TREE_ROWS);
+  if (a.n_tokens < 0 || a.n_tokens > MAX_HISTORY) return op_fail(SPRINTER_E_RANGE, "%s: n_tokens %d outside [0, 2^19]", who, a.n_tokens);
+  if (a.draft && a.n_rows > MAX_HISTORY) return op_fail(SPRINTER_E_RANGE, "%s: %d rows with draft are more than 2^19", who, a.n_rows);
+  if (a.visible && (a.n_words < 1 || a.n_words > MAX_NODE_WORDS))
+    return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, a.n_words, MAX_NODE_WORDS);
+  if (a.n_bias < 0 || a.n_bias > MAX_BIASES) return op_fail(SPRINTER_E_RANGE, "%s: n_bias %d outside [0, %d]", who, a.n_bias, MAX_BIASES);
+  if (a.n_mask < 0) return op_fail(SPRINTER_E_RANGE, "%s: %d masks", who, a.n_mask);
+  if (a.n_rows == 0) return SPRINTER_OK;
+  if (!a.logits || !a.out) return op_fail(SPRINTER_E_NULL, "%s: NULL logits or out", who);
+  if (!a.bias != !a.bias_ids) return op_fail(SPRINTER_E_NULL, "%s: bias and bias_ids come together", who);
+  if (!a.tokens && (a.n_token || a.n_prompt)) return op_fail(SPRINTER_E_NULL, "%s: n_token or n_prompt without tokens", who);
+  if (!a.mask && a.mask_row) return op_fail(SPRINTER_E_NULL, "%s: mask_row without mask", who);
+  const bool of_sequences = a.tokens || a.draft || a.bias || a.repetition || a.presence || a.frequency;
+  if (!a.first && of_sequences && a.n_rows > a.n_seq)
+    return op_fail(SPRINTER_E_RANGE, "%s: %d rows without first are more than %d sequences", who, a.n_rows, a.n_seq);
+  if (a.mask && !a.mask_row && a.n_rows > a.n_mask)
+    return op_fail(SPRINTER_E_RANGE, "%s: %d rows without mask_row are more than %d masks", who, a.n_rows, a.n_mask);
+  const int words = (a.vocab + 31) / 32;
+  if (a.n_rows > 1 && (a.ld_logits < a.vocab || a.ld_out < a.vocab)) return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their %d columns", who, a.vocab);
+  if ((a.tokens && a.n_seq > 1 && a.ld_tokens < a.n_tokens) || (a.bias && a.n_seq > 1 && (a.ld_bias < a.n_bias || a.ld_bias_ids < a.n_bias)) ||
+      (a.mask && a.n_mask > 1 && a.ld_mask < words))
+    return op_fail(SPRINTER_E_RANGE, "%s: rows of tokens, biases or masks lie closer than their columns", who);
+  const size_t es = element(a.dtype);
+  if (!aligned(a.logits, es) || !aligned(a.out, es) || !aligned(a.first, 4) || !aligned(a.tokens, 4) || !aligned(a.n_token, 4) || !aligned(a.n_prompt, 4) ||
+      !aligned(a.repetition, 4) || !aligned(a.presence, 4) || !aligned(a.frequency, 4) || !aligned(a.draft, 4) || !aligned(a.visible, 8) ||
+      !aligned(a.bias_ids, 4) || !aligned(a.bias, 4) || !aligned(a.mask, 4) || !aligned(a.mask_row, 4))
+    return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
+  launching();
+  launch_adjust_logits(a, (hipStream_t)hip_stream);
+  return launched(who);
 }
 
 }  // extern "C"

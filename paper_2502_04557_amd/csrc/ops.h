@@ -46,6 +46,44 @@ struct BlockNormArgs {
 };
 void launch_block_norm(const BlockNormArgs& a, hipStream_t s);
 
+// A cache in pages, one layer of it (k_cache.hip, k_tree_attn.hip): keys and values [n_page][KVH][page][dh]; slot s of sequence b is place
+// s % page of page table[b][s / page], and not there where that is no page.
+struct PagedArgs {
+  void *keys, *values;
+  const int* table; long long ld_table;
+  int n_seq, n_table, n_page, shift, KVH, dh;    // page size 1 << shift
+};
+struct AppendArgs {
+  PagedArgs c;
+  int cache_type, row_type, H, T, n_turned, pairs;   // pairs 0: columns (i, i + n / 2), 1: (2 i, 2 i + 1)
+  const int *seq, *slot, *pos;                   // pos NULL: the slot
+  const double* freq;                            // [n_turned / 2]
+  const void *k, *v, *q; long long ld_k, ld_v, ld_q;   // q NULL: none
+  void* q_out; long long ld_q_out;               // of the cache's type
+};
+void launch_cache_append(const AppendArgs& a, hipStream_t s);
+struct KeepArgs {
+  PagedArgs c;                                   // keys, values of layer 0
+  int n_layer; long long layer_bytes;
+  int element;                                   // bytes
+  const int *lens, *first, *path, *n_keep; long long ld_path; int n_path;
+};
+void launch_cache_keep(const KeepArgs& a, hipStream_t s);
+struct AttendArgs {
+  PagedArgs c;
+  int type, H, T, n_words;
+  float scale;
+  const int *lens, *first;
+  const unsigned long long* visible;             // [T][n_words], or NULL: the nodes up to the row's own
+  const void* q; long long ld_q;
+  void* y; long long ld_y;
+};
+size_t attend_workspace(int type, int dh, int H, int KVH, int n_seq, int T, long long slots);
+void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s);
+
+constexpr int MAX_HISTORY = 1 << 19, MAX_BIASES = 2047, MAX_NODE_WORDS = 16;
+void launch_adjust_logits(const sprinter_logits& a, hipStream_t s);
+
 int op_fail(int code, const char* fmt, ...);     // the thread's last error (abi.cpp)
 
 }  // namespace sprinter

@@ -1,4 +1,5 @@
-"""The operators of include/sprinter.h on torch tensors: routing to experts, the experts' products, the norms around a block.
+"""The operators of include/sprinter.h on torch tensors: routing to experts, the experts' products, the norms around a block; a cache in pages,
+the attention of drafted trees over it, and the adjustments of logits.
 
 Argument marshalling only; every call runs the library's HIP kernels on the device and the current stream of its tensors, allocates its
 outputs (and workspace) through torch and waits for nothing.  Options are plain numbers, no tensors.  What the library refuses raises
@@ -250,3 +251,245 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
     if given:
         _written(h_out)
     return h_out, out
+
+
+# ------------------------------------------------------------------------------------ a round of drafted trees over a cache in pages
+PAIRS = {"halves": 0, "neighbours": 1}
+
+
+class CacheCfgC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_layer", "n_page", "page_size", "n_kv_head", "d_head")]
+
+
+class LogitsC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_rows", "vocab", "n_seq")] + [
+        ("logits", C.c_void_p), ("ld_logits", C.c_int64), ("out", C.c_void_p), ("ld_out", C.c_int64), ("first", C.c_void_p),
+        ("tokens", C.c_void_p), ("ld_tokens", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("n_token", "n_prompt", "repetition", "presence", "frequency", "draft", "visible")] + [
+        ("bias_ids", C.c_void_p), ("ld_bias_ids", C.c_int64), ("bias", C.c_void_p), ("ld_bias", C.c_int64), ("mask", C.c_void_p), ("ld_mask", C.c_int64),
+        ("mask_row", C.c_void_p)] + [(n, C.c_int32) for n in ("n_tokens", "n_words", "n_bias", "n_mask")]
+
+
+def _wrote(t):
+    """A tensor that is written in place; one of inference mode counts no versions."""
+    if not t.is_inference():
+        _written(t)
+
+
+def _vector(name, t, device, dtype, n):
+    """A contiguous vector of n elements."""
+    _tensor(name, t, device, dtype)
+    shape = t.shape
+    if len(shape) != 1 or shape[0] != n:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected [{n}]")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name}: not contiguous")
+
+
+def _trees(first, visible, device, rows):
+    """Checks what describes a batch of trees -> (sequences, words of a row of `visible`)."""
+    n = first.shape[0] - 1 if isinstance(first, torch.Tensor) and first.dim() == 1 else -1
+    if n < 0:
+        raise ValueError("first: an int32 vector [n_seq + 1] is needed")
+    _vector("first", first, device, torch.int32, n + 1)
+    return _int32("n_seq", n), _words(visible, device, rows)
+
+
+def _words(visible, device, rows):
+    if visible is None:
+        return 0
+    words = visible.shape[1] if isinstance(visible, torch.Tensor) and visible.dim() == 2 else 0
+    _whole("visible", visible, device, torch.int64, rows, max(1, words))
+    return words
+
+
+class PagedCache:
+    """A cache in pages on two tensors of the caller's: keys, values [n_layer, n_page, n_kv_head, page_size, d_head], bfloat16 or float32.
+
+    Slot s of sequence b is place s % page_size of page table[b, s // page_size] (table int32 [n_seq, n], entries outside the cache: no page).  page_size is a
+    power of two in [8, 1024], d_head 64 or 128.  The tensors are written in place; the object keeps no state beside them.
+
+    A batch of trees: sequence b has lens[b] committed slots and the rows first[b] .. first[b + 1] - 1 as its drafted nodes (lens int32 [n_seq], first int32
+    [n_seq + 1]), node i in slot lens[b] + i.  visible int64 [T, words]: bit j % 64 of word j // 64 says whether a row sees node j of its sequence,
+    itself among them; None: the nodes up to itself (a decode step, a window of drafted tokens, a piece of a prompt)."""
+
+    def __init__(self, keys, values):
+        dev = _device(keys, "keys")
+        if keys.dtype not in DTYPES or keys.dim() != 5:
+            raise ValueError("keys: bfloat16 or float32 [n_layer, n_page, n_kv_head, page_size, d_head] is needed")
+        shape = tuple(keys.shape)
+        for name, t in (("keys", keys), ("values", values)):
+            _whole(name, t, dev, keys.dtype, *shape)
+        self.keys, self.values, self.device, self.dtype = keys, values, dev, keys.dtype
+        self.n_layer, self.n_page, self.n_kv_head, self.page_size, self.d_head = shape
+        self._cfg = CacheCfgC(DTYPES[keys.dtype], *(_int32("keys' sizes", shape[i]) for i in (0, 1, 3, 2, 4)))
+        self._ref = C.byref(self._cfg)
+        self._arrays = keys.data_ptr(), values.data_ptr()
+        self._need = {}
+
+    def _table(self, table):
+        _rows("table", table, self.device, torch.int32, None, None)
+        n_seq, n = table.shape
+        return n_seq, (table.data_ptr(), table.stride(0), n_seq, _int32("table's columns", n))
+
+    def append(self, layer, keys, values, table, seq, slot, *, q=None, pos=None, freq=None, pairs="halves", q_out=None):
+        """Writes the rows keys, values [T, n_kv_head * d_head] to slot[t] of sequence seq[t] (both int32 [T]); -> q turned, or None (sprinter_cache_append).
+
+        With freq (float64 [n / 2]) the first n columns of each head of the keys and of q [T, n_head * d_head] are turned by the angles pos[t] * freq (pos int32
+        [T], by default the slot), in the pairs (i, i + n / 2) ("halves") or (2 i, 2 i + 1) ("neighbours").  Rows are bfloat16 or float32, all of one
+        type; what is written has the cache's.  A token of no sequence (-1) is padding.  q_out: where the turned q goes (q itself turns it in place)."""
+        dev = self.device
+        if not isinstance(keys, torch.Tensor) or keys.dtype not in DTYPES:
+            raise ValueError("keys: bfloat16 or float32 rows are needed")
+        width = self.n_kv_head * self.d_head
+        _rows("keys", keys, dev, keys.dtype, None, width)
+        T = keys.shape[0]
+        _rows("values", values, dev, keys.dtype, T, width)
+        _, table_args = self._table(table)
+        _vector("seq", seq, dev, torch.int32, T)
+        _vector("slot", slot, dev, torch.int32, T)
+        if pos is not None:
+            _vector("pos", pos, dev, torch.int32, T)
+        n = 0
+        if freq is not None:
+            n = freq.shape[0] if isinstance(freq, torch.Tensor) and freq.dim() == 1 else 0
+            _vector("freq", freq, dev, torch.float64, n)
+        if pairs not in PAIRS:
+            raise ValueError(f"pairs is one of {tuple(PAIRS)}")
+        H, given = 0, q_out is not None
+        if q is not None:
+            _rows("q", q, dev, keys.dtype, T, None)
+            H = q.shape[1] // self.d_head
+            if H < 1 or q.shape[1] != H * self.d_head:
+                raise ValueError(f"q: {q.shape[1]} columns are no heads of {self.d_head}")
+            if given:
+                _rows("q_out", q_out, dev, self.dtype, T, q.shape[1])
+            else:
+                q_out = torch.empty(T, q.shape[1], dtype=self.dtype, device=dev)
+        elif given:
+            raise ValueError("q_out: there is no q")
+        _call("sprinter_cache_append", dev, self._ref, _int32("layer", layer), *self._arrays, *table_args, seq.data_ptr(), slot.data_ptr(), _ptr(pos),
+              _ptr(freq), 2 * n, PAIRS[pairs], DTYPES[keys.dtype], keys.data_ptr(), keys.stride(0), values.data_ptr(), values.stride(0), _ptr(q),
+              0 if q is None else q.stride(0), H, T, _ptr(q_out), 0 if q_out is None else q_out.stride(0))
+        _wrote(self.keys)
+        _wrote(self.values)
+        if given:
+            _wrote(q_out)
+        return q_out
+
+    def attend(self, layer, q, table, lens, first, *, visible=None, scale=None, out=None):
+        """q [T, n_head * d_head] of the cache's type -> y [T, n_head * d_head]: each node attends to the committed slots and to the nodes that it
+        sees (sprinter_cache_attend).  scale: of the scores, by default d_head ** -0.5.  A row that sees nothing gives zeros; rows of no
+        sequence are not written."""
+        dev = self.device
+        _rows("q", q, dev, self.dtype, None, None)
+        T, width = q.shape
+        H = width // self.d_head
+        if H < 1 or width != H * self.d_head:
+            raise ValueError(f"q: {width} columns are no heads of {self.d_head}")
+        n_seq, table_args = self._table(table)
+        _vector("lens", lens, dev, torch.int32, n_seq)
+        n, words = _trees(first, visible, dev, T)
+        if n != n_seq:
+            raise ValueError(f"first: {n} sequences, table has {n_seq}")
+        given = out is not None
+        if given:
+            _rows("out", out, dev, self.dtype, T, width)
+        else:
+            out = torch.empty(T, width, dtype=self.dtype, device=dev)
+        scale = self.d_head ** -0.5 if scale is None else float(_number("scale", scale))
+        need = self._workspace(H, n_seq, table_args[3], T)
+        work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _call("sprinter_cache_attend", dev, self._ref, _int32("layer", layer), *self._arrays, *table_args, lens.data_ptr(), first.data_ptr(),
+              _ptr(visible), words, H, scale, q.data_ptr(), q.stride(0), T, out.data_ptr(), out.stride(0), _ptr(work), need)
+        if given:
+            _wrote(out)
+        return out
+
+    def _workspace(self, H, n_seq, n_table, T):
+        n = self._need.get((H, n_seq, n_table, T))
+        if n is None:
+            v = C.c_size_t(0)
+            rc = _entry("sprinter_cache_attend_bytes")(self._ref, _int32("heads", H), n_seq, n_table, T, C.byref(v))
+            if rc:
+                raise SprinterError(rc, _lib.sprinter_last_error(None).decode())
+            if len(self._need) >= 4096:
+                self._need.clear()
+            n = self._need[H, n_seq, n_table, T] = v.value
+        return n
+
+    def keep(self, table, lens, first, path, n_keep):
+        """Slot lens[b] + path[b, j] -> slot lens[b] + j in every layer, j < n_keep[b] (path int32 [n_seq, n], nodes in ascending order; n_keep int32
+        [n_seq]): the accepted nodes become the next committed slots (sprinter_cache_keep).  lens is the caller's to advance."""
+        dev = self.device
+        n_seq, table_args = self._table(table)
+        _vector("lens", lens, dev, torch.int32, n_seq)
+        _vector("first", first, dev, torch.int32, n_seq + 1)
+        _rows("path", path, dev, torch.int32, n_seq, None)
+        _vector("n_keep", n_keep, dev, torch.int32, n_seq)
+        _call("sprinter_cache_keep", dev, self._ref, *self._arrays, *table_args, lens.data_ptr(), first.data_ptr(), path.data_ptr(), path.stride(0),
+              _int32("path's columns", path.shape[1]), n_keep.data_ptr())
+        _wrote(self.keys)
+        _wrote(self.values)
+
+
+def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=None, repetition=None, presence=None, frequency=None, draft=None,
+                  visible=None, bias_ids=None, bias=None, mask=None, mask_row=None, out=None):
+    """logits [T, V] float32 or bfloat16 -> penalties for the tokens of each row, biases and a mask applied (sprinter_adjust_logits).
+
+    Rows first[b] .. first[b + 1] - 1 are the nodes of sequence b (None: row t is sequence t).  tokens int32 [n_seq, n] with n_token, n_prompt int32 [n_seq]: a
+    sequence's tokens, how many there are (None: n), and how many of them are its prompt (None: none); draft int32 [T] with visible, as for
+    PagedCache: the drafted tokens, of which a row's own are those that it sees.  repetition divides positive logits of a row's tokens and multiplies others;
+    frequency times how often a token was generated, and presence if it was, are subtracted (float32 [n_seq]).  bias_ids int32, bias float32
+    [n_seq, n]: biases of tokens (an id outside the vocabulary is padding, the last of equal ids counts).  mask int32 [n, ceil(V / 32)], mask_row
+    int32 [T]: row t may take the tokens whose bits mask[mask_row[t]] has, the others become -inf (-1: all allowed; None: mask t).  out: logits itself changes them in
+    place."""
+    dev = _device(logits, "logits")
+    if logits.dtype not in DTYPES:
+        raise ValueError("logits: bfloat16 or float32 is needed")
+    _rows("logits", logits, dev, logits.dtype, None, None)
+    T, V = logits.shape
+    _int32("logits' columns", V)
+    f32, i32 = torch.float32, torch.int32
+    if first is not None:
+        n_seq, words = _trees(first, visible, dev, T)
+    else:
+        n_seq, words = T, _words(visible, dev, T)
+    n_tokens = n_bias = n_mask = 0
+    for name, t, dtype in (("n_token", n_token, i32), ("n_prompt", n_prompt, i32), ("repetition", repetition, f32), ("presence", presence, f32),
+                           ("frequency", frequency, f32)):
+        if t is not None:
+            _vector(name, t, dev, dtype, n_seq)
+    if tokens is not None:
+        _rows("tokens", tokens, dev, i32, n_seq, None)
+        n_tokens = _int32("tokens' columns", tokens.shape[1])
+        if n_tokens == 0:                                # (no history: an empty tensor has no address)
+            tokens = n_token = n_prompt = None
+    if draft is not None:
+        _vector("draft", draft, dev, i32, T)
+    if bias is not None or bias_ids is not None:
+        _rows("bias_ids", bias_ids, dev, i32, n_seq, None)
+        n_bias = _int32("bias' columns", bias_ids.shape[1])
+        _rows("bias", bias, dev, f32, n_seq, n_bias)
+    if mask is not None:
+        _rows("mask", mask, dev, i32, None, (V + 31) // 32)
+        n_mask = mask.shape[0]
+    if mask_row is not None:
+        _vector("mask_row", mask_row, dev, i32, T)
+    if mask is not None and n_mask == 0:
+        if mask_row is None and T > 0:
+            raise ValueError(f"mask: {T} rows without mask_row, and no masks")
+        mask = mask_row = None
+    given = out is not None
+    if given:
+        _rows("out", out, dev, logits.dtype, T, V)
+    else:
+        out = torch.empty(T, V, dtype=logits.dtype, device=dev)
+    ld = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
+    a = LogitsC(DTYPES[logits.dtype], T, V, n_seq, logits.data_ptr(), logits.stride(0), out.data_ptr(), out.stride(0), _ptr(first), _ptr(tokens), ld(tokens),
+                _ptr(n_token), _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(draft), _ptr(visible), _ptr(bias_ids), ld(bias_ids),
+                _ptr(bias), ld(bias), _ptr(mask), ld(mask), _ptr(mask_row), n_tokens, words, n_bias, n_mask)
+    _call("sprinter_adjust_logits", dev, C.byref(a))
+    if given:
+        _wrote(out)
+    return out
