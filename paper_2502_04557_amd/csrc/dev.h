@@ -266,6 +266,20 @@ __device__ __forceinline__ float group_max16(float v) {
   return v;
 }
 
+// Maximum / sum over the four lanes that share lane % 16 (lanes 16 apart), in all of them: two lane swaps on the vector ALU.
+__device__ __forceinline__ float quarter_max(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // Maximum of 64-bit keys over an aligned group of 16 consecutive lanes, in every lane of the group.
 __device__ __forceinline__ u64 group_umax64_16(u64 k) {
 #define SPRINTER_DPP_STEP(CTRL)                                                                              \

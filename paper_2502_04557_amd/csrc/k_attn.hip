@@ -581,20 +581,6 @@ __global__ __launch_bounds__(64) void k_kv_append_bf16(AttnArgs a) {
   }
 }
 
-// Maximum / sum over the four lanes that share lane % 16 (lanes 16 apart), in all of them: two lane swaps on the vector ALU.
-__device__ __forceinline__ float quarter_max(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float quarter_sum(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
 // The queries of one wave of the two kernels below, rotated and scaled (in base-2 units), to LDS in operand layout [set][32 columns]
 // [hi, lo][lane]: 16 entries from `first` on (beyond the last row: that one again) of heads h0 and h0 + 1 (PAIR), or 32 entries of head
 // h0.  The lanes go along the rows, 4 columns each (16 rows x 16 pieces of 32 bytes at once took the memory pipeline 4 times as

@@ -91,13 +91,60 @@ template <> struct Tree<float> { static constexpr int KB = 16, NK = 4, VEC = 4; 
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ float quarters_max(float v) {   // over the lanes l, l + 16, l + 32, l + 48
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+// Which of a lane's NK keys a row sees: those from node j0 on (below 0: committed), of which `there` are there.
+template <int NK>
+__device__ __forceinline__ unsigned seen_keys(const AttendArgs& a, long long row, int node, int j0, unsigned there) {
+  unsigned see = (1u << NK) - 1;
+  if (j0 + NK > 0) {
+    if (a.visible) {
+      const int j = max(j0, 0), word = j >> 6, sh = j & 63;
+      const unsigned long long* v = a.visible + row * a.n_words;
+      see = word < a.n_words ? (unsigned)(v[word] >> sh) : 0u;
+      if (sh > 64 - NK && word + 1 < a.n_words) see |= (unsigned)(v[word + 1] << (64 - sh));
+      if (j0 < 0) see = see << -j0 | ((1u << -j0) - 1);
+    } else {
+      see = (1u << min(max(node - j0 + 1, 0), NK)) - 1;
+    }
+  }
+  return see & there;
 }
-__device__ __forceinline__ float quarters_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+
+// The scores of a lane's NK keys (of one row, in p) become weights in units of the running maximum m, a base-2 exponent; l is the lane's sum of them.  The
+// maximum moves only when a score passes it by more than 2^8 (uniform: any row of the wave), so that the common block needs no exchange between lanes: weights up
+// to 2^8 cost float32 sums and bf16 pairs nothing.  masked: keys outside `bits` have weight 0.
+constexpr float LOW = -3.402823466e38f;
+template <int NK, int N>
+__device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsigned bits, float c, float& m, float& l, f32x4 (&O)[N]) {
+  if (masked) {
+#pragma unroll
+    for (int e = 0; e < NK; ++e) p[e] = bits >> e & 1 ? p[e] : -INFINITY;
+  }
+  float mx = p[0];
+#pragma unroll
+  for (int e = 1; e < NK; ++e) mx = fmaxf(mx, p[e]);
+  mx *= c;
+  if (__any(mx > m + 8.f)) {
+    const float mn = fmaxf(m, fmaxf(quarter_max(mx), LOW));   // (NaN: left out here, and in the weights below)
+    const float corr = __builtin_amdgcn_exp2f(m - mn);
+    l *= corr;
+#pragma unroll
+    for (int i = 0; i < N; ++i) O[i] *= corr;
+    m = mn;
+  }
+#pragma unroll
+  for (int e = 0; e < NK; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -m));
+  if (masked) {                                    // (also where -infinity times a scale of 0 is NaN)
+#pragma unroll
+    for (int e = 0; e < NK; ++e) p[e] = bits >> e & 1 ? p[e] : 0.f;
+  }
+  float s[NK / 2];
+#pragma unroll
+  for (int e = 0; e < NK / 2; ++e) s[e] = p[2 * e] + p[2 * e + 1];
+#pragma unroll
+  for (int n = NK / 4; n > 0; n >>= 1)
+#pragma unroll
+    for (int e = 0; e < n; ++e) s[e] = s[2 * e] + s[2 * e + 1];
+  l += s[0];
 }
 
 // The attention of one item by NW waves, each with all QB = 16 QT rows and every NW-th block of the item's keys; one pass with running maxima and sums.
@@ -107,13 +154,12 @@ __device__ __forceinline__ float quarters_sum(float v) {
 //     lane's, which for bf16 is one byte permutation per pair of keys.  The accumulators then hold DH / 4 neighbouring columns of a row.
 // P enters as two bf16 (16 bits, as the values of the plain bfloat16 path deserve: one alone would double the error of the result).
 template <typename T, int DH, int QT, int NW>
-__global__ __launch_bounds__(NW * 64, QT == 4 ? 1 : 2) void k_tree_attn(AttendArgs a, TreePlan plan) {
+__global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan plan) {
   using P = Tree<T>;
   constexpr bool HALF = sizeof(T) == 2;
   constexpr int KB = P::KB, NK = P::NK, QB = 16 * QT, CPL = DH / 16, KF = DH / (HALF ? 32 : 16);   // columns of V per lane; 16-byte pieces of a key per lane and tile
   constexpr int KT = HALF ? 2 : 1;                 // key tiles
   constexpr int VW = CPL * sizeof(T) / 4;          // dwords of a key's columns
-  constexpr float LOW = -3.402823466e38f;
   __shared__ float merge[NW / 2][QB][DH];
   __shared__ float stats[NW][QB][2];
   TreeItem it;
@@ -230,64 +276,20 @@ __global__ __launch_bounds__(NW * 64, QT == 4 ? 1 : 2) void k_tree_attn(AttendAr
 
     float p[QT][NK];
     unsigned bits[QT];
+    const int kl = kb + NK * lq;                   // this lane's first key
+    const unsigned there = plain ? (1u << NK) - 1 : v_ok ? (1u << min(max(end - kl, 0), NK)) - 1 : 0u;
+    uint4 ph[QT], pl[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
 #pragma unroll
       for (int e = 0; e < NK; ++e) p[t][e] = sc[t][e >> 2][e & 3];
-      bits[t] = (1u << NK) - 1;
-    }
-    const int kl = kb + NK * lq;                   // this lane's first key
-    unsigned there = (1u << NK) - 1;
-    if (!plain) {
-      there = v_ok ? (1u << min(max(end - kl, 0), NK)) - 1 : 0u;
-      const int j0 = kl - it.len;                  // as a node
-#pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        unsigned see = (1u << NK) - 1;
-        if (j0 + NK > 0) {
-          if (a.visible) {
-            const int j = max(j0, 0), word = j >> 6, sh = j & 63;
-            const unsigned long long* v = a.visible + at_q[t] * a.n_words;
-            see = word < a.n_words ? (unsigned)(v[word] >> sh) : 0u;
-            if (sh > 64 - NK && word + 1 < a.n_words) see |= (unsigned)(v[word + 1] << (64 - sh));
-            if (j0 < 0) see = see << -j0 | ((1u << -j0) - 1);
-          } else {
-            see = (1u << min(max(node[t] - j0 + 1, 0), NK)) - 1;
-          }
-        }
-        bits[t] = see & there;
-#pragma unroll
-        for (int e = 0; e < NK; ++e) p[t][e] = bits[t] >> e & 1 ? p[t][e] : -INFINITY;
-      }
-    }
-    uint4 ph[QT], pl[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float mx = p[t][0];
-#pragma unroll
-      for (int e = 1; e < NK; ++e) mx = fmaxf(mx, p[t][e]);
-      const float mn = fmaxf(m_run[t], fmaxf(quarters_max(mx) * c, LOW));
-      if (__any(mn > m_run[t])) {                  // (uniform) the maximum of some row moves
-        const float corr = __builtin_amdgcn_exp2f(m_run[t] - mn);
-        l_run[t] *= corr;
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) O[t][i] *= corr;
-        m_run[t] = mn;
-      }
-#pragma unroll
-      for (int e = 0; e < NK; ++e) p[t][e] = __builtin_amdgcn_exp2f(fmaf(p[t][e], c, -mn));
-      if (!plain) {                                // (also where -infinity times a scale of 0 is NaN)
-#pragma unroll
-        for (int e = 0; e < NK; ++e) p[t][e] = bits[t] >> e & 1 ? p[t][e] : 0.f;
-      }
+      bits[t] = plain ? there : seen_keys<NK>(a, at_q[t], node[t], kl - it.len, there);
+      softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
       if constexpr (HALF) {
-        l_run[t] += ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
         split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
         split2(p[t][2], p[t][3], ph[t].y, pl[t].y);
         split2(p[t][4], p[t][5], ph[t].z, pl[t].z);
         split2(p[t][6], p[t][7], ph[t].w, pl[t].w);
-      } else {
-        l_run[t] += (p[t][0] + p[t][1]) + (p[t][2] + p[t][3]);
       }
     }
     // What no row, or not every row, sees must not meet a weight of 0 as an infinity or NaN: slots that are not there are cleared, and elements of nodes
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(NW * 64, QT == 4 ? 1 : 2) void k_tree_attn(AttendAr
   // The waves' results, put together in pairs through LDS: every wave's in units of the largest maximum.
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    l_run[t] = quarters_sum(l_run[t]);
+    l_run[t] = quarter_sum(l_run[t]);
     if (lq == 0) { stats[w][16 * t + l16][0] = m_run[t]; stats[w][16 * t + l16][1] = l_run[t]; }
   }
   __syncthreads();
@@ -436,6 +438,234 @@ __global__ __launch_bounds__(NW * 64, QT == 4 ? 1 : 2) void k_tree_attn(AttendAr
   }
 }
 
+// 16 bytes per lane from memory to LDS at `lds` + 16 x lane.  In asm, since the compiler waits for every such load of its builtin in front of the next read of
+// LDS; the kernel's own waits count them.
+__device__ __forceinline__ void piece_to_lds(const bf16_t* src, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+
+// The same for many rows (bf16): the NW waves share the keys and values of the item through a ring of S stages of 32 keys in LDS and have 16 QT rows each.
+// Half of the waves bring keys, in operand order, half values, as rows of DH columns; the fragments of V^T are read with ds_read_b64_tr_b16, four keys
+// of a column at a time.  The row's 32-byte pieces lie where an exclusive-or with its number puts them, so that those reads meet no bank twice.
+template <int DH, int QT, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, TreePlan plan) {
+  constexpr int QB = 16 * QT * NW, KF = DH / 32, CT = DH / 16, F = 2 * KF + CT, LPW = F / NW, S = 4, PPR = DH / 8;   // F pieces of 1 KiB a stage, LPW of them by a wave
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  __shared__ __align__(1024) u32x4 ring[S][F][64];
+  TreeItem it;
+  if (!find_item(a, plan, QB, blockIdx.x, -1, it)) return;
+  const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.y, G = a.H / a.c.KVH;
+  const int shift = a.c.shift, place_mask = (1 << shift) - 1;
+  const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
+  const int k0 = it.part * it.share * STEP, end = min(k0 + it.share * STEP, slots), sure = min(it.len, end);
+  const int n_blk = max(0, (end - k0 + 31) >> 5);
+  const int* __restrict__ table = a.c.table + (long long)it.b * a.c.ld_table;
+  const int last = max(a.c.n_table - 1, 0);
+
+  // entries of the table, 64 at a time in the lanes of two registers (k0 is a multiple of 128, so that a block's lie in one of them)
+  auto ok = [&](int page) { return (unsigned)page < (unsigned)a.c.n_page; };
+  int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
+  u64 ok_now = __ballot(ok(now)), ok_before = 0;   // which of these, and of the 64 before them, are pages
+  auto element = [&](int page, int s) {
+    return ((((long long)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) + (s & place_mask)) * DH;
+  };
+  const bool key_wave = w < NW / 2;
+  const int first_piece = (key_wave ? w : w - NW / 2) * LPW;
+  auto issue = [&](int i) {
+    const int kb = k0 + 32 * min(i, n_blk - 1);
+    if ((kb >> shift) - e0 >= 64) {
+      e0 += 64;
+      now = then;
+      ok_before = ok_now;
+      ok_now = __ballot(ok(now));
+      then = table[min(e0 + 64 + lane, last)];
+    }
+    const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[i % S][(key_wave ? 0 : 2 * KF) + first_piece][0];
+    if (key_wave) {
+      const int s = kb + 8 * (l16 >> 2);
+      const bf16_t* src = (const bf16_t*)a.c.keys + element(__shfl(now, (s >> shift) - e0), s) + (l16 & 3) * DH + lq * 8;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        const int t = (first_piece + j) / KF, f = (first_piece + j) % KF;
+        piece_to_lds(src + t * 4 * DH + f * 32, uniform(dst + j * 1024));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        const int row = (first_piece + j) * (64 / PPR) + lane / PPR, s = kb + (row & ~7);
+        const int swap = DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1;
+        const int piece = (lane % PPR) ^ (swap << 1);
+        piece_to_lds((const bf16_t*)a.c.values + element(__shfl(now, (s >> shift) - e0), s) + (row & 7) * DH + piece * 8, uniform(dst + j * 1024));
+      }
+    }
+  };
+  if (n_blk > 0) {
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) issue(i);
+  }
+
+  // this lane's rows
+  long long at_q[QT];
+  int node[QT];
+  bool row_there[QT];
+  u32x4 q[QT][KF];
+  float c = a.scale * 1.4426950408889634f;
+  const unsigned flip = c < 0.f ? 0x80008000u : 0u;
+  c = fabsf(c);
+  const long long r0 = (long long)it.block * QB + 16 * QT * w;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const long long i = r0 + 16 * t + l16;
+    row_there[t] = i < (long long)it.n * G;
+    const int g = (int)(i % G);
+    node[t] = row_there[t] ? (int)(i / G) : 0;
+    at_q[t] = (long long)(it.f0 + node[t]);
+    const bf16_t* src = (const bf16_t*)a.q + at_q[t] * a.ld_q + ((row_there[t] ? g : 0) + kvh * G) * DH;
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      q[t][f] = *reinterpret_cast<const u32x4*>(src + f * 32 + lq * 8);
+      q[t][f] = row_there[t] ? q[t][f] ^ flip : (u32x4){0, 0, 0, 0};
+    }
+  }
+  // the slots that some row of this wave sees end here: none, a chain's last node, all
+  const long long rows_left = (long long)it.n * G - r0;
+  const int reach = rows_left <= 0 ? 0 : a.visible ? end : (int)min((long long)end, it.len + (r0 + min(rows_left, 16ll * QT) - 1) / G + 1);
+
+  f32x4 O[QT][CT];
+  float m_run[QT], l_run[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m_run[t] = LOW; l_run[t] = 0.f;
+#pragma unroll
+    for (int i = 0; i < CT; ++i) O[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  // where this lane's first column of V^T begins in a stage: 4 keys of tile 0, keys 8 lq + l16 / 4 (+ 4)
+  const int v_row = 8 * lq + (l16 >> 2), v_swap = DH == 128 ? (v_row & 3) | (v_row >> 3 & 1) << 2 : (v_row >> 1 & 1) | (v_row >> 3 & 1) << 1;
+  const unsigned v_off = 2 * KF * 1024 + v_row * (2 * DH) + (v_swap << 5) + (l16 & 3) * 8;
+  for (int i = 0; i < n_blk; ++i) {
+    // this wave's part of block i has landed, its reads of block i - 1 are back; then the same of every wave
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * LPW) : "memory");
+    issue(i + S - 1);
+    const int kb = k0 + i * 32;
+    if (kb >= reach) continue;                     // (scalar) nothing that a row of this wave sees
+    const u32x4(*blk)[64] = ring[i % S];
+    f32x4 sc[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      const uint4 x0 = __builtin_bit_cast(uint4, blk[f][lane]), x1 = __builtin_bit_cast(uint4, blk[KF + f][lane]);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        sc[t][0] = mfma_bf16(x0, __builtin_bit_cast(uint4, q[t][f]), sc[t][0]);
+        sc[t][1] = mfma_bf16(x1, __builtin_bit_cast(uint4, q[t][f]), sc[t][1]);
+      }
+    }
+    uint4 V[CT];
+    const unsigned v_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)blk + v_off;
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(v_at ^ (x << 5)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((v_at ^ (x << 5)) + 8 * DH));
+      const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+      V[x] = make_uint4(l2.x, l2.y, h2.x, h2.y);
+    }
+    const int kl = kb + 8 * lq;
+    float p[QT][8];
+    unsigned bits[QT];
+    const int entry = (kb >> shift) - e0, more = ((kb + 31) >> shift) - (kb >> shift);   // (the registers may be a few blocks ahead)
+    const u64 pages = (entry < 0 ? ok_before >> (entry + 64) : ok_now >> entry) & ((2u << more) - 1);
+    const bool plain = kb + 32 <= sure && pages == (2u << more) - 1;   // (scalar) every key is there and seen by every row
+    unsigned there = 0xff;
+    if (!plain) there = pages >> ((kl >> shift) - (kb >> shift)) & 1 ? (1u << min(max(end - kl, 0), 8)) - 1 : 0u;
+    uint4 ph[QT], pl[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[t][e] = sc[t][e >> 2][e & 3];
+      bits[t] = plain ? there : seen_keys<8>(a, at_q[t], node[t], kl - it.len, there);
+      softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
+      split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
+      split2(p[t][2], p[t][3], ph[t].y, pl[t].y);
+      split2(p[t][4], p[t][5], ph[t].z, pl[t].z);
+      split2(p[t][6], p[t][7], ph[t].w, pl[t].w);
+    }
+    u64 sick[8];
+    bool any_sick = false;
+    if (!plain) {                                  // (as above; a lane has one column of its 8 keys in each tile)
+      unsigned bad = 0;
+#pragma unroll
+      for (int x = 0; x < CT; ++x) {
+        unsigned* v = reinterpret_cast<unsigned*>(&V[x]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          unsigned y = v[e] & ((there >> (2 * e) & 1 ? 0xffffu : 0u) | (there >> (2 * e + 1) & 1 ? 0xffff0000u : 0u));
+          const bool lo = kl + 2 * e >= it.len && (y & 0x7f80u) == 0x7f80u, hi = kl + 2 * e + 1 >= it.len && (y & 0x7f800000u) == 0x7f800000u;
+          bad |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
+          v[e] = y & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sick[j] = __ballot(bad >> j & 1);
+        any_sick |= sick[j] != 0;
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) O[t][x] = mfma_bf16(V[x], ph[t], O[t][x]);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) O[t][x] = mfma_bf16(V[x], pl[t], O[t][x]);
+    }
+    if (any_sick) {                                // (uniform, rare)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        for (int g = 0; g < 4; ++g) {
+          if (!(sick[j] >> (16 * g) & 0xffff)) continue;
+          const int s = kb + 8 * g + j;
+          const bf16_t* src = (const bf16_t*)a.c.values + element(table[min(s >> shift, last)], s) + 4 * lq;
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const float pj = __shfl(p[t][j], 16 * g + l16);
+            const bool sees = __shfl((int)bits[t], 16 * g + l16) >> j & 1;
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float v = __uint_as_float((unsigned)src[16 * x + r] << 16);
+                if (sees && !(fabsf(v) < INFINITY)) O[t][x][r] += pj * v;
+              }
+          }
+        }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last stages' loads still write to LDS)
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const float l = quarter_sum(l_run[t]);
+    if (!row_there[t]) continue;
+    const int i = (int)(16 * QT * w + 16 * t + l16);
+    if (it.parts > 1) {
+      const long long at = ((long long)blockIdx.x * a.c.KVH + kvh) * QB + i;
+#pragma unroll
+      for (int x = 0; x < CT; ++x)
+        *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(O[t][x][0], O[t][x][1], O[t][x][2], O[t][x][3]);
+      if (lq == 0) *reinterpret_cast<float2*>(plan.ml + at * 2) = make_float2(m_run[t], l);
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int g = (int)((r0 + 16 * t + l16) % G);
+      bf16_t* dst = (bf16_t*)a.y + at_q[t] * a.ld_y + (kvh * G + g) * DH + 4 * lq;
+#pragma unroll
+      for (int x = 0; x < CT; ++x) {
+        const f32x4 o = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t][x] * inv;
+        *reinterpret_cast<uint2*>(dst + 16 * x) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
+      }
+    }
+  }
+}
+
 // The shares of a split sequence put together: a wave per row and head, the shares in their order.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan, int QB) {
@@ -446,7 +676,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
   const long long i = (long long)(t - it.f0) * G + h % G;
   const int block = (int)(i / QB), row = (int)(i % QB), item = it.base + block * it.parts;
   auto at = [&](int part) { return ((long long)(item + part) * a.c.KVH + kvh) * QB + row; };
-  float m = -3.402823466e38f, l = 0.f;
+  float m = LOW, l = 0.f;
   for (int x = lane; x < it.parts; x += 64) m = fmaxf(m, plan.ml[at(x) * 2]);
   m = wave_max(m);
   float o[DH / 64] = {};
@@ -465,22 +695,26 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
   }
 }
 
-// Row tiles of a wave: as many as the rows of a sequence fill in the mean.
-static int tree_tiles(int type, int H, int KVH, int n_seq, int T) {
+// How the rows of an item are laid out: QT tiles of 16 rows a wave; NW waves that share the keys, or (1) waves that have the rows each and share the
+// keys among them.  By the mean of rows (nodes x heads of a KV head) per sequence.
+struct TreeShape { int QT, NW, QB; };
+static TreeShape tree_shape(int type, int dh, int H, int KVH, int n_seq, int T) {
   const double rows = (double)T * (H / KVH) / std::max(1, std::min(n_seq, T));
-  return rows <= 16 ? 1 : rows <= 32 || type == X_F32 ? 2 : 4;
+  auto of = [](int QT, int NW) { return TreeShape{QT, NW, 16 * QT * NW}; };
+  if (rows <= 16 || (type == X_F32 && dh == 128)) return of(1, 1);
+  if (rows <= 32 || type == X_F32) return of(2, 1);
+  return rows <= 64 ? of(1, 4) : rows <= 128 ? of(2, 4) : of(2, 8);
 }
 
-static TreePlan tree_plan(int type, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
-  const int QB = 16 * tree_tiles(type, H, KVH, n_seq, T);
+static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
   TreePlan p{};
-  p.target = std::max(1, (512 + KVH - 1) / KVH);
-  const long long blocks = (long long)T * (H / KVH) / QB + std::min(n_seq, T);   // at most
+  p.target = std::max(1, ((shape.NW == 8 ? 256 : 512) + KVH - 1) / KVH);
+  const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
   const bool whole = slots <= STEP;                // one share each
   p.items = (int)(blocks + (whole ? 0 : p.target));
   bytes = 0;
   if (!whole) {
-    const size_t rows = (size_t)p.items * KVH * QB;
+    const size_t rows = (size_t)p.items * KVH * shape.QB;
     bytes = rows * (dh + 2) * sizeof(float);
     p.o = (float*)ws;
     p.ml = (float*)ws + rows * dh;
@@ -491,22 +725,27 @@ static TreePlan tree_plan(int type, int dh, int H, int KVH, int n_seq, int T, lo
 size_t attend_workspace(int type, int dh, int H, int KVH, int n_seq, int T, long long slots) {
   size_t bytes;
   if (n_seq < 1 || T < 1) return 0;
-  tree_plan(type, dh, H, KVH, n_seq, T, slots, bytes, nullptr);
+  tree_plan(tree_shape(type, dh, H, KVH, n_seq, T), dh, H, KVH, n_seq, T, slots, bytes, nullptr);
   return bytes;
 }
 
 void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
   size_t bytes;
-  const TreePlan p = tree_plan(a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
-  const int QT = tree_tiles(a.type, a.H, a.c.KVH, a.c.n_seq, a.T);
+  const TreeShape shape = tree_shape(a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T);
+  const TreePlan p = tree_plan(shape, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
   const dim3 grid(p.items, a.c.KVH), block(256);
   auto go = [&](auto type, auto dh) {
     using T = decltype(type);
     constexpr int DH = decltype(dh)::value;
-    if (QT == 1) hipLaunchKernelGGL((k_tree_attn<T, DH, 1, 4>), grid, block, 0, s, a, p);
-    else if (QT == 2) hipLaunchKernelGGL((k_tree_attn<T, DH, 2, 4>), grid, block, 0, s, a, p);
-    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_tree_attn<T, DH, 4, 4>), grid, block, 0, s, a, p);
-    if (bytes) hipLaunchKernelGGL((k_tree_merge<T, DH>), dim3(a.T, (a.H + 3) / 4), block, 0, s, a, p, 16 * QT);
+    if (shape.NW == 1 && shape.QT == 1) hipLaunchKernelGGL((k_tree_attn<T, DH, 1, 4>), grid, block, 0, s, a, p);
+    if constexpr (sizeof(T) == 2 || DH == 64)
+      if (shape.NW == 1 && shape.QT == 2) hipLaunchKernelGGL((k_tree_attn<T, DH, 2, 4>), grid, block, 0, s, a, p);
+    if constexpr (sizeof(T) == 2) {
+      if (shape.NW == 4 && shape.QT == 1) hipLaunchKernelGGL((k_tree_attn_shared<DH, 1, 4>), grid, block, 0, s, a, p);
+      else if (shape.NW == 4) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 4>), grid, block, 0, s, a, p);
+      else if (shape.NW == 8) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 8>), grid, dim3(512), 0, s, a, p);
+    }
+    if (bytes) hipLaunchKernelGGL((k_tree_merge<T, DH>), dim3(a.T, (a.H + 3) / 4), block, 0, s, a, p, shape.QB);
   };
   auto typed = [&](auto dh) { if (a.type == X_F32) go(float(), dh); else go(bf16_t(), dh); };
   if (a.c.dh == 64) typed(std::integral_constant<int, 64>()); else typed(std::integral_constant<int, 128>());
