@@ -9,16 +9,17 @@ namespace sprinter {
 // A launch cuts the batch into items: a block of QB rows (node x head of one KV head) of a sequence against a share of its slots.  Lengths and trees are known
 // on the device alone, so every workgroup works the cut out for itself from `lens` and `first`: `steps` of STEP slots over all blocks of rows,
 // dealt out in shares of `share` steps so that about `target` items come out, however ragged the batch is.
+struct TreeItem {
+  int f0, n, len, b;                               // the sequence: rows f0 .. f0 + n - 1
+  int block, part, parts, share;                   // block of rows, share of slots, how many of them, steps of each
+};
 struct TreePlan {
   int target, items;                               // shares to aim for; the most items there can be (per KV head)
+  TreeItem* list;                                  // [items] parts 0: there is none
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
   float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
 };
 constexpr int STEP = 128;
-
-struct TreeItem {
-  int b, f0, n, len, block, part, parts, share, base;   // rows f0 .. f0 + n - 1; block of rows, share of slots; base: the block's first item
-};
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -35,8 +36,8 @@ __device__ __forceinline__ TreeSeq tree_seq(const AttendArgs& a, int b, int QB, 
   return s;
 }
 
-// The item of index `item`, or (row >= 0) the first item of the block that holds this row's first head; false: there is none.  By a whole wave.
-__device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p, int QB, int item, int row, TreeItem& out) {
+// The item of index `item`; false: there is none.  By a whole wave.
+__device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p, int QB, int item, TreeItem& out) {
   const int lane = threadIdx.x & 63, n = a.c.n_seq;
   TreeSeq s = tree_seq(a, lane, QB, lane < n);
   float work = (float)s.blocks * (float)s.steps;
@@ -46,8 +47,9 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
   }
   work = wave_sum(work);
   // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
-  const int share = (int)(work * (1.0001f / (float)p.target)) + 1;
+  const int share = (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1;
   int base = 0;
+  out.parts = 0;
   for (int b0 = 0; b0 < n; b0 += 64) {
     if (b0) s = tree_seq(a, b0 + lane, QB, b0 + lane < n);
     const int parts = (s.steps + share - 1) / share, mine = s.blocks * parts;
@@ -58,7 +60,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
       if (lane >= o) sum += x;
     }
     const int before = base + sum - mine;
-    const u64 hit = __ballot(row >= 0 ? s.blocks > 0 && row >= s.f0 && row < s.f0 + s.n : item >= before && item < before + mine);
+    const u64 hit = __ballot(item >= before && item < before + mine);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       out.b = uniform(b0 + l);
@@ -67,20 +69,15 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
       out.len = __builtin_amdgcn_readlane(s.len, l);
       out.parts = __builtin_amdgcn_readlane(parts, l);
       out.share = uniform(share);
-      const int first = __builtin_amdgcn_readlane(before, l);
-      if (row >= 0) {
-        out.block = 0; out.part = 0; out.base = first;
-      } else {
-        const int i = item - first;
-        out.block = i / out.parts;
-        out.part = i - out.block * out.parts;
-        out.base = item - out.part;
-      }
-      return true;
+      const int i = item - __builtin_amdgcn_readlane(before, l);
+      out.block = i / out.parts;
+      out.part = i - out.block * out.parts;
+      break;
     }
     base += __builtin_amdgcn_readlane(sum, 63);
   }
-  return false;
+  if (p.list && blockIdx.y == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
+  return out.parts > 0;
 }
 
 // bf16: 32 keys a block, of which a lane ends up with the scores of 8; float32: 16 and 4.
@@ -163,7 +160,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   __shared__ float merge[NW / 2][QB][DH];
   __shared__ float stats[NW][QB][2];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x, -1, it)) return;
+  if (!find_item(a, plan, QB, blockIdx.x, it)) return;
   const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.y, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
@@ -246,8 +243,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     fetch_v(kb);
     fetch_pages(kb + NW * KB);
   }
-  for (; kb < end; kb += NW * KB) {
-    const bool plain = kb + KB <= sure && __all(ok(page_k));   // (uniform) every key is there and seen by every row
+  // One block of KB keys, and the requests for the wave's next one.  plain: every key is there and seen by every row.
+  auto attend = [&](auto is_plain) __attribute__((always_inline)) {
+    constexpr bool plain = decltype(is_plain)::value;
     const bool v_ok = ok(page_v);
     f32x4 sc[QT][KT];
 #pragma unroll
@@ -294,31 +292,25 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     }
     // What no row, or not every row, sees must not meet a weight of 0 as an infinity or NaN: slots that are not there are cleared, and elements of nodes
     // that are not finite are taken out here and added below to the rows that see them.
-    u64 sick[NK];
-    bool any_sick = false;
+    unsigned bad = 0;                              // which of this lane's keys have an element that is not finite here
     if (!plain) {
 #pragma unroll
       for (int j = 0; j < NK; ++j) {
-        bool bad = false;
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
           unsigned x = V[j][i / 4][i & 3];
           x = there >> j & 1 ? x : 0u;
-          if (kl + j >= it.len) {
-            if constexpr (HALF) {
-              const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
-              bad |= lo || hi;
-              x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
-            } else {
-              const bool b = (x & 0x7f800000u) == 0x7f800000u;
-              bad |= b;
-              x = b ? 0u : x;
-            }
+          if constexpr (HALF) {
+            const bool lo = kl + j >= it.len && (x & 0x7f80u) == 0x7f80u, hi = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
+            bad |= (lo || hi ? 1u : 0u) << j;
+            x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+          } else {
+            const bool b = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
+            bad |= (b ? 1u : 0u) << j;
+            x = b ? 0u : x;
           }
           V[j][i / 4][i & 3] = x;
         }
-        sick[j] = __ballot(bad);
-        any_sick |= sick[j] != 0;
       }
     }
 #pragma unroll
@@ -348,29 +340,36 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
       fetch_pages(kb + 2 * NW * KB);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (any_sick) {                                // (uniform, rare)
+    if (!plain && __any(bad)) {                    // (rare)
+      for (int key = 0; key < KB; ++key) {
+        const int j = key % NK, g = key / NK;
+        if (!(__ballot(bad >> j & 1) >> (16 * g) & 0xffff)) continue;
+        const long long at = ((long long)__builtin_amdgcn_readlane((int)(v_here >> 32), 16 * g) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v_here, 16 * g)) + j * DH;
+        const T* src = (const T*)a.c.values + at + 4 * CPL * lq;
 #pragma unroll
-      for (int j = 0; j < NK; ++j)
-        for (int g = 0; g < 4; ++g) {
-          if (!(sick[j] >> (16 * g) & 0xffff)) continue;
-          const long long at = ((long long)__builtin_amdgcn_readlane((int)(v_here >> 32), 16 * g) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v_here, 16 * g)) + j * DH;
-          const T* src = (const T*)a.c.values + at + 4 * CPL * lq;
+        for (int t = 0; t < QT; ++t) {
+          float pj = p[t][0];
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            const float pj = __shfl(p[t][j], 16 * g + l16);
-            const bool sees = __shfl((int)bits[t], 16 * g + l16) >> j & 1;
+          for (int e = 1; e < NK; ++e) pj = j == e ? p[t][e] : pj;
+          pj = __shfl(pj, 16 * g + l16);
+          const bool sees = __shfl((int)bits[t], 16 * g + l16) >> j & 1;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+          for (int r = 0; r < 4; ++r) {
 #pragma unroll
-              for (int i = 0; i < CPL; ++i) {
-                float v;
-                if constexpr (HALF) v = __uint_as_float((unsigned)src[CPL * r + i] << 16); else v = src[CPL * r + i];
-                if (sees && !(fabsf(v) < INFINITY)) O[t][i][r] += pj * v;
-              }
+            for (int i = 0; i < CPL; ++i) {
+              float v;
+              if constexpr (HALF) v = __uint_as_float((unsigned)src[CPL * r + i] << 16); else v = src[CPL * r + i];
+              if (sees && !(fabsf(v) < INFINITY)) O[t][i][r] += pj * v;
+            }
+            asm volatile("" ::: "memory");         // (a few loads at a time: registers)
           }
         }
+      }
     }
-  }
+  };
+  // First the blocks that every row sees and whose pages are there, up to the first that is none, then the others.
+  for (; kb + KB <= sure && __all(ok(page_k)); kb += NW * KB) attend(std::true_type());
+  for (; kb < end; kb += NW * KB) attend(std::false_type());
 
   // The waves' results, put together in pairs through LDS: every wave's in units of the largest maximum.
 #pragma unroll
@@ -453,7 +452,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   __shared__ __align__(1024) u32x4 ring[S][F][64];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x, -1, it)) return;
+  if (!find_item(a, plan, QB, blockIdx.x, it)) return;
   const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.y, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
@@ -469,6 +468,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   auto element = [&](int page, int s) {
     return ((((long long)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) + (s & place_mask)) * DH;
   };
+  auto page = [&](int s) { return __builtin_amdgcn_readlane(now, (s >> shift) - e0); };
   const bool key_wave = w < NW / 2;
   const int first_piece = (key_wave ? w : w - NW / 2) * LPW;
   auto issue = [&](int i) {
@@ -482,8 +482,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     }
     const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[i % S][(key_wave ? 0 : 2 * KF) + first_piece][0];
     if (key_wave) {
-      const int s = kb + 8 * (l16 >> 2);
-      const bf16_t* src = (const bf16_t*)a.c.keys + element(__shfl(now, (s >> shift) - e0), s) + (l16 & 3) * DH + lq * 8;
+      const int s = kb + 8 * (l16 >> 2), g = l16 >> 2;
+      const int p0 = page(kb), p1 = page(kb + 8), p2 = page(kb + 16), p3 = page(kb + 24);
+      const bf16_t* src = (const bf16_t*)a.c.keys + element(g & 2 ? g & 1 ? p3 : p2 : g & 1 ? p1 : p0, s) + (l16 & 3) * DH + lq * 8;
 #pragma unroll
       for (int j = 0; j < LPW; ++j) {
         const int t = (first_piece + j) / KF, f = (first_piece + j) % KF;
@@ -492,10 +493,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     } else {
 #pragma unroll
       for (int j = 0; j < LPW; ++j) {
-        const int row = (first_piece + j) * (64 / PPR) + lane / PPR, s = kb + (row & ~7);
+        constexpr int RPP = 64 / PPR;              // rows of a piece: half of 8 keys, or 8
+        const int row = (first_piece + j) * RPP + lane / PPR, s = kb + ((first_piece + j) * RPP & ~7);
         const int swap = DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1;
         const int piece = (lane % PPR) ^ (swap << 1);
-        piece_to_lds((const bf16_t*)a.c.values + element(__shfl(now, (s >> shift) - e0), s) + (row & 7) * DH + piece * 8, uniform(dst + j * 1024));
+        piece_to_lds((const bf16_t*)a.c.values + element(page(s), s) + (row & 7) * DH + piece * 8, uniform(dst + j * 1024));
       }
     }
   };
@@ -542,13 +544,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   // where this lane's first column of V^T begins in a stage: 4 keys of tile 0, keys 8 lq + l16 / 4 (+ 4)
   const int v_row = 8 * lq + (l16 >> 2), v_swap = DH == 128 ? (v_row & 3) | (v_row >> 3 & 1) << 2 : (v_row >> 1 & 1) | (v_row >> 3 & 1) << 1;
   const unsigned v_off = 2 * KF * 1024 + v_row * (2 * DH) + (v_swap << 5) + (l16 & 3) * 8;
-  for (int i = 0; i < n_blk; ++i) {
-    // this wave's part of block i has landed, its reads of block i - 1 are back; then the same of every wave
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * LPW) : "memory");
-    issue(i + S - 1);
-    const int kb = k0 + i * 32;
-    if (kb >= reach) continue;                     // (scalar) nothing that a row of this wave sees
-    const u32x4(*blk)[64] = ring[i % S];
+  // One block of 32 keys.  plain: every key is there and seen by every row.
+  auto attend = [&](auto is_plain, int kb, const u32x4(*blk)[64], unsigned pages) __attribute__((always_inline)) {
+    constexpr bool plain = decltype(is_plain)::value;
     f32x4 sc[QT][2];
 #pragma unroll
     for (int t = 0; t < QT; ++t) sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -574,9 +572,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     const int kl = kb + 8 * lq;
     float p[QT][8];
     unsigned bits[QT];
-    const int entry = (kb >> shift) - e0, more = ((kb + 31) >> shift) - (kb >> shift);   // (the registers may be a few blocks ahead)
-    const u64 pages = (entry < 0 ? ok_before >> (entry + 64) : ok_now >> entry) & ((2u << more) - 1);
-    const bool plain = kb + 32 <= sure && pages == (2u << more) - 1;   // (scalar) every key is there and seen by every row
     unsigned there = 0xff;
     if (!plain) there = pages >> ((kl >> shift) - (kb >> shift)) & 1 ? (1u << min(max(end - kl, 0), 8)) - 1 : 0u;
     uint4 ph[QT], pl[QT];
@@ -591,10 +586,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
       split2(p[t][4], p[t][5], ph[t].z, pl[t].z);
       split2(p[t][6], p[t][7], ph[t].w, pl[t].w);
     }
-    u64 sick[8];
-    bool any_sick = false;
+    unsigned bad = 0;                              // which of this lane's keys have an element that is not finite here
     if (!plain) {                                  // (as above; a lane has one column of its 8 keys in each tile)
-      unsigned bad = 0;
 #pragma unroll
       for (int x = 0; x < CT; ++x) {
         unsigned* v = reinterpret_cast<unsigned*>(&V[x]);
@@ -606,11 +599,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
           v[e] = y & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
         }
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sick[j] = __ballot(bad >> j & 1);
-        any_sick |= sick[j] != 0;
-      }
     }
 #pragma unroll
     for (int x = 0; x < CT; ++x) {
@@ -619,27 +607,51 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
 #pragma unroll
       for (int t = 0; t < QT; ++t) O[t][x] = mfma_bf16(V[x], pl[t], O[t][x]);
     }
-    if (any_sick) {                                // (uniform, rare)
+    if (!plain && __any(bad)) {                    // (rare)
+      for (int key = 0; key < 32; ++key) {
+        const int j = key & 7, g = key >> 3;
+        if (!(__ballot(bad >> j & 1) >> (16 * g) & 0xffff)) continue;
+        const int s = kb + key;
+        const bf16_t* src = (const bf16_t*)a.c.values + element(table[min(s >> shift, last)], s) + 4 * lq;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        for (int g = 0; g < 4; ++g) {
-          if (!(sick[j] >> (16 * g) & 0xffff)) continue;
-          const int s = kb + 8 * g + j;
-          const bf16_t* src = (const bf16_t*)a.c.values + element(table[min(s >> shift, last)], s) + 4 * lq;
+        for (int t = 0; t < QT; ++t) {
+          float pj = p[t][0];
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            const float pj = __shfl(p[t][j], 16 * g + l16);
-            const bool sees = __shfl((int)bits[t], 16 * g + l16) >> j & 1;
+          for (int e = 1; e < 8; ++e) pj = j == e ? p[t][e] : pj;
+          pj = __shfl(pj, 16 * g + l16);
+          const bool sees = __shfl((int)bits[t], 16 * g + l16) >> j & 1;
 #pragma unroll
-            for (int x = 0; x < CT; ++x)
+          for (int x = 0; x < CT; ++x) {
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float v = __uint_as_float((unsigned)src[16 * x + r] << 16);
-                if (sees && !(fabsf(v) < INFINITY)) O[t][x][r] += pj * v;
-              }
+            for (int r = 0; r < 4; ++r) {
+              const float v = __uint_as_float((unsigned)src[16 * x + r] << 16);
+              if (sees && !(fabsf(v) < INFINITY)) O[t][x][r] += pj * v;
+            }
+            asm volatile("" ::: "memory");         // (one tile's loads at a time: registers)
           }
         }
+      }
     }
+  };
+  auto next = [&](int i) {
+    // this wave's part of block i has landed, its reads of block i - 1 are back; then the same of every wave
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * LPW) : "memory");
+    issue(i + S - 1);
+    const int entry = ((k0 + i * 32) >> shift) - e0;             // (the registers may be a few blocks ahead)
+    return (unsigned)(entry < 0 ? ok_before >> (entry + 64) : ok_now >> entry);
+  };
+  // First the blocks that every row sees and whose pages are there, up to the first that is none, then the others.
+  int i = 0;
+  unsigned pages = n_blk > 0 ? next(0) : 0u;
+  for (; i < n_blk; pages = next(++i)) {
+    const int kb = k0 + i * 32;
+    const unsigned all = (2u << (((kb + 31) >> shift) - (kb >> shift))) - 1;
+    if (kb + 32 > sure || (pages & all) != all) break;
+    if (kb < reach) attend(std::true_type(), kb, ring[i % S], all);
+  }
+  for (; i < n_blk; pages = next(++i)) {
+    const int kb = k0 + i * 32;
+    if (kb < reach) attend(std::false_type(), kb, ring[i % S], pages);   // (scalar: something that a row of this wave sees)
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last stages' loads still write to LDS)
 #pragma unroll
@@ -666,32 +678,48 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   }
 }
 
-// The shares of a split sequence put together: a wave per row and head, the shares in their order.
+// The shares of split sequences put together, in their order: the workgroups of a block's shares take its rows in turn, a wave one at a time.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan, int QB) {
-  const int t = blockIdx.x, h = blockIdx.y * 4 + wave_index(), lane = threadIdx.x & 63;
-  TreeItem it;
-  if (h >= a.H || !find_item(a, plan, QB, 0, t, it) || it.parts < 2) return;
-  const int G = a.H / a.c.KVH, kvh = h / G;
-  const long long i = (long long)(t - it.f0) * G + h % G;
-  const int block = (int)(i / QB), row = (int)(i % QB), item = it.base + block * it.parts;
-  auto at = [&](int part) { return ((long long)(item + part) * a.c.KVH + kvh) * QB + row; };
-  float m = LOW, l = 0.f;
-  for (int x = lane; x < it.parts; x += 64) m = fmaxf(m, plan.ml[at(x) * 2]);
-  m = wave_max(m);
-  float o[DH / 64] = {};
-  for (int x = 0; x < it.parts; ++x) {
-    const float2 ml = *reinterpret_cast<const float2*>(plan.ml + at(x) * 2);
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    l += ml.y * f;
+  constexpr int N = DH / 64;
+  const TreeItem it = plan.list[blockIdx.x];
+  if (it.parts < 2) return;
+  const int G = a.H / a.c.KVH, kvh = blockIdx.y, lane = threadIdx.x & 63, first = blockIdx.x - it.part, parts = min(it.parts, plan.items - first);
+  const int rows = (int)min((long long)QB, (long long)it.n * G - (long long)it.block * QB);
+  for (int r = it.part + it.parts * wave_index(); r < rows; r += it.parts * 4) {
+    auto at = [&](int part) { return ((long long)(first + part) * a.c.KVH + kvh) * QB + r; };
+    float2 ml = lane < parts ? *reinterpret_cast<const float2*>(plan.ml + at(lane) * 2) : make_float2(LOW, 0.f);
+    float m = ml.x, l = 0.f, o[N] = {};
+    for (int x = lane + 64; x < parts; x += 64) m = fmaxf(m, plan.ml[at(x) * 2]);
+    m = wave_max(m);
+    for (int x0 = 0; x0 < parts; x0 += 64) {
+      if (x0) ml = x0 + lane < parts ? *reinterpret_cast<const float2*>(plan.ml + at(x0 + lane) * 2) : make_float2(LOW, 0.f);
+      const float f = __builtin_amdgcn_exp2f(ml.x - m);
+      l += wave_sum(ml.y * f);
+      const int here = min(parts - x0, 64);
+      int x = 0;
+      for (; x + 4 <= here; x += 4) {              // (four shares' loads at a time)
+        float v[4][N];
 #pragma unroll
-    for (int e = 0; e < DH / 64; ++e) o[e] += plan.o[at(x) * DH + lane * (DH / 64) + e] * f;
-  }
-  T* y = (T*)a.y + (long long)t * a.ld_y + h * DH + lane * (DH / 64);
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-  for (int e = 0; e < DH / 64; ++e) {
-    const float r = l == 0.f ? 0.f : o[e] / l;
-    if constexpr (sizeof(T) == 4) y[e] = r; else y[e] = f2bf(r);
+          for (int e = 0; e < N; ++e) v[u][e] = plan.o[at(x0 + x + u) * DH + lane * N + e];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int e = 0; e < N; ++e) o[e] += v[u][e] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x + u));
+      }
+      for (; x < here; ++x)
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] += plan.o[at(x0 + x) * DH + lane * N + e] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x));
+    }
+    const long long i = (long long)it.block * QB + r;
+    T* y = (T*)a.y + (it.f0 + i / G) * a.ld_y + (kvh * G + i % G) * DH + lane * N;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float v = l == 0.f ? 0.f : o[e] / l;
+      if constexpr (sizeof(T) == 4) y[e] = v; else y[e] = f2bf(v);
+    }
   }
 }
 
@@ -711,13 +739,14 @@ static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_
   p.target = std::max(1, ((shape.NW == 8 ? 256 : 512) + KVH - 1) / KVH);
   const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
   const bool whole = slots <= STEP;                // one share each
-  p.items = (int)(blocks + (whole ? 0 : p.target));
+  p.items = (int)(blocks + (whole ? 0 : p.target + 1));
   bytes = 0;
   if (!whole) {
     const size_t rows = (size_t)p.items * KVH * shape.QB;
-    bytes = rows * (dh + 2) * sizeof(float);
+    bytes = rows * (dh + 2) * sizeof(float) + p.items * sizeof(TreeItem);
     p.o = (float*)ws;
-    p.ml = (float*)ws + rows * dh;
+    p.ml = p.o + rows * dh;
+    p.list = (TreeItem*)(p.ml + rows * 2);
   }
   return p;
 }
@@ -745,7 +774,7 @@ void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
       else if (shape.NW == 4) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 4>), grid, block, 0, s, a, p);
       else if (shape.NW == 8) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 8>), grid, dim3(512), 0, s, a, p);
     }
-    if (bytes) hipLaunchKernelGGL((k_tree_merge<T, DH>), dim3(a.T, (a.H + 3) / 4), block, 0, s, a, p, shape.QB);
+    if (bytes) hipLaunchKernelGGL((k_tree_merge<T, DH>), grid, block, 0, s, a, p, shape.QB);
   };
   auto typed = [&](auto dh) { if (a.type == X_F32) go(float(), dh); else go(bf16_t(), dh); };
   if (a.c.dh == 64) typed(std::integral_constant<int, 64>()); else typed(std::integral_constant<int, 128>());
