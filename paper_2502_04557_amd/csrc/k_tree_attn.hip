@@ -46,6 +46,19 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     work += (float)x.blocks * (float)x.steps;
   }
   work = wave_sum(work);
+  // The longest sequences first, where there are enough of them to wait for a place and one wave holds them all.
+  int from = lane;                                 // the sequence that this lane stands for
+  if (n > 4 && n <= 64) {
+    const int key = s.blocks > 0 ? s.steps : -1;
+    int rank = 0;
+    for (int x = 0; x < n; ++x) {
+      const int other = __builtin_amdgcn_readlane(key, x);
+      rank += other > key || (other == key && x < lane) ? 1 : 0;
+    }
+    auto to = [&](int v) { return __builtin_amdgcn_ds_permute(4 * (lane < n ? rank : lane), v); };
+    s.f0 = to(s.f0); s.n = to(s.n); s.len = to(s.len); s.blocks = to(s.blocks); s.steps = to(s.steps);
+    from = to(lane);
+  }
   // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
   const int share = (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1;
   int base = 0;
@@ -63,7 +76,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     const u64 hit = __ballot(item >= before && item < before + mine);
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      out.b = uniform(b0 + l);
+      out.b = b0 + __builtin_amdgcn_readlane(from, l);
       out.f0 = __builtin_amdgcn_readlane(s.f0, l);
       out.n = __builtin_amdgcn_readlane(s.n, l);
       out.len = __builtin_amdgcn_readlane(s.len, l);
@@ -76,7 +89,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     }
     base += __builtin_amdgcn_readlane(sum, 63);
   }
-  if (p.list && blockIdx.y == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
+  if (p.list && blockIdx.x % a.c.KVH == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
   return out.parts > 0;
 }
 
@@ -87,6 +100,7 @@ template <> struct Tree<float> { static constexpr int KB = 16, NK = 4, VEC = 4; 
 
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // Which of a lane's NK keys a row sees: those from node j0 on (below 0: committed), of which `there` are there.
 template <int NK>
@@ -160,8 +174,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   __shared__ float merge[NW / 2][QB][DH];
   __shared__ float stats[NW][QB][2];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x, it)) return;
-  const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.y, G = a.H / a.c.KVH;
+  if (!find_item(a, plan, QB, blockIdx.x / a.c.KVH, it)) return;
+  const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.x % a.c.KVH, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
   const int k0 = it.part * it.share * STEP, end = min(k0 + it.share * STEP, slots), sure = min(it.len, end);   // slots below `sure` are seen by every row
@@ -293,23 +307,47 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     // What no row, or not every row, sees must not meet a weight of 0 as an infinity or NaN: slots that are not there are cleared, and elements of nodes
     // that are not finite are taken out here and added below to the rows that see them.
     unsigned bad = 0;                              // which of this lane's keys have an element that is not finite here
-    if (!plain) {
+    if constexpr (!plain) {
+      if (__any(there != (1u << NK) - 1)) {
 #pragma unroll
-      for (int j = 0; j < NK; ++j) {
+        for (int j = 0; j < NK; ++j)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          unsigned x = V[j][i / 4][i & 3];
-          x = there >> j & 1 ? x : 0u;
-          if constexpr (HALF) {
-            const bool lo = kl + j >= it.len && (x & 0x7f80u) == 0x7f80u, hi = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
-            bad |= (lo || hi ? 1u : 0u) << j;
-            x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
-          } else {
-            const bool b = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
-            bad |= (b ? 1u : 0u) << j;
-            x = b ? 0u : x;
-          }
-          V[j][i / 4][i & 3] = x;
+          for (int i = 0; i < VW; ++i) V[j][i / 4][i & 3] = there >> j & 1 ? V[j][i / 4][i & 3] : 0u;
+      }
+      if (kb + KB > it.len) {
+        bool some = false;
+        if constexpr (HALF) {
+          u16x2 top = {0, 0};                      // the largest magnitudes, as integers: 0x7f80 and more are not finite
+#pragma unroll
+          for (int j = 0; j < NK; ++j)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, V[j][i / 4][i & 3] & 0x7fff7fffu));
+          some = top[0] >= 0x7f80 || top[1] >= 0x7f80;
+        } else {
+          unsigned top = 0;
+#pragma unroll
+          for (int j = 0; j < NK; ++j)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) top = max(top, V[j][i / 4][i & 3] & 0x7fffffffu);
+          some = top >= 0x7f800000u;
+        }
+        if (__any(some)) {
+#pragma unroll
+          for (int j = 0; j < NK; ++j)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+              unsigned x = V[j][i / 4][i & 3];
+              if constexpr (HALF) {
+                const bool lo = kl + j >= it.len && (x & 0x7f80u) == 0x7f80u, hi = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
+                bad |= (lo || hi ? 1u : 0u) << j;
+                x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+              } else {
+                const bool b = kl + j >= it.len && (x & 0x7f800000u) == 0x7f800000u;
+                bad |= (b ? 1u : 0u) << j;
+                x = b ? 0u : x;
+              }
+              V[j][i / 4][i & 3] = x;
+            }
         }
       }
     }
@@ -417,7 +455,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
 #pragma unroll
       for (int i = 0; i < CPL; ++i) x[CPL * r + i] = l_all[t] == 0.f ? 0.f : O[t][i][r] * inv;
     if (it.parts > 1) {
-      const long long at = (((long long)blockIdx.x * a.c.KVH + kvh) * QB + 16 * t + l16);
+      const long long at = (((long long)blockIdx.x) * QB + 16 * t + l16);
       float* dst = plan.o + at * DH + 4 * CPL * lq;
 #pragma unroll
       for (int i = 0; i < 4 * CPL; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
@@ -452,8 +490,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   __shared__ __align__(1024) u32x4 ring[S][F][64];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x, it)) return;
-  const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.y, G = a.H / a.c.KVH;
+  if (!find_item(a, plan, QB, blockIdx.x / a.c.KVH, it)) return;
+  const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.x % a.c.KVH, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
   const int k0 = it.part * it.share * STEP, end = min(k0 + it.share * STEP, slots), sure = min(it.len, end);
@@ -587,16 +625,32 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
       split2(p[t][6], p[t][7], ph[t].w, pl[t].w);
     }
     unsigned bad = 0;                              // which of this lane's keys have an element that is not finite here
-    if (!plain) {                                  // (as above; a lane has one column of its 8 keys in each tile)
-#pragma unroll
-      for (int x = 0; x < CT; ++x) {
-        unsigned* v = reinterpret_cast<unsigned*>(&V[x]);
+    if constexpr (!plain) {                        // (as above; a lane has one column of its 8 keys in each tile)
+      if (__any(there != 0xff)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          unsigned y = v[e] & ((there >> (2 * e) & 1 ? 0xffffu : 0u) | (there >> (2 * e + 1) & 1 ? 0xffff0000u : 0u));
-          const bool lo = kl + 2 * e >= it.len && (y & 0x7f80u) == 0x7f80u, hi = kl + 2 * e + 1 >= it.len && (y & 0x7f800000u) == 0x7f800000u;
-          bad |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
-          v[e] = y & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+          const unsigned keep = (there >> (2 * e) & 1 ? 0xffffu : 0u) | (there >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int x = 0; x < CT; ++x) reinterpret_cast<unsigned*>(&V[x])[e] &= keep;
+        }
+      }
+      if (kb + 32 > it.len) {
+        u16x2 top = {0, 0};                        // the largest magnitudes, as integers: 0x7f80 and more are not finite
+#pragma unroll
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, reinterpret_cast<const unsigned*>(&V[x])[e] & 0x7fff7fffu));
+        if (__any(top[0] >= 0x7f80 || top[1] >= 0x7f80)) {
+#pragma unroll
+          for (int x = 0; x < CT; ++x) {
+            unsigned* v = reinterpret_cast<unsigned*>(&V[x]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool lo = kl + 2 * e >= it.len && (v[e] & 0x7f80u) == 0x7f80u, hi = kl + 2 * e + 1 >= it.len && (v[e] & 0x7f800000u) == 0x7f800000u;
+              bad |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
+              v[e] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+            }
+          }
         }
       }
     }
@@ -660,7 +714,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     if (!row_there[t]) continue;
     const int i = (int)(16 * QT * w + 16 * t + l16);
     if (it.parts > 1) {
-      const long long at = ((long long)blockIdx.x * a.c.KVH + kvh) * QB + i;
+      const long long at = ((long long)blockIdx.x) * QB + i;
 #pragma unroll
       for (int x = 0; x < CT; ++x)
         *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(O[t][x][0], O[t][x][1], O[t][x][2], O[t][x][3]);
@@ -682,9 +736,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan, int QB) {
   constexpr int N = DH / 64;
-  const TreeItem it = plan.list[blockIdx.x];
+  const int item = blockIdx.x / a.c.KVH;
+  const TreeItem it = plan.list[item];
   if (it.parts < 2) return;
-  const int G = a.H / a.c.KVH, kvh = blockIdx.y, lane = threadIdx.x & 63, first = blockIdx.x - it.part, parts = min(it.parts, plan.items - first);
+  const int G = a.H / a.c.KVH, kvh = blockIdx.x - item * a.c.KVH, lane = threadIdx.x & 63, first = item - it.part, parts = min(it.parts, plan.items - first);
   const int rows = (int)min((long long)QB, (long long)it.n * G - (long long)it.block * QB);
   for (int r = it.part + it.parts * wave_index(); r < rows; r += it.parts * 4) {
     auto at = [&](int part) { return ((long long)(first + part) * a.c.KVH + kvh) * QB + r; };
@@ -731,7 +786,7 @@ static TreeShape tree_shape(int type, int dh, int H, int KVH, int n_seq, int T) 
   auto of = [](int QT, int NW) { return TreeShape{QT, NW, 16 * QT * NW}; };
   if (rows <= 16 || (type == X_F32 && dh == 128)) return of(1, 1);
   if (rows <= 32 || type == X_F32) return of(2, 1);
-  return rows <= 64 ? of(1, 4) : rows <= 128 ? of(2, 4) : of(2, 8);
+  return rows <= 64 ? of(1, 4) : getenv("X8") && rows > 128 ? of(2, 8) : of(2, 4);
 }
 
 static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
@@ -762,7 +817,7 @@ void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
   size_t bytes;
   const TreeShape shape = tree_shape(a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T);
   const TreePlan p = tree_plan(shape, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
-  const dim3 grid(p.items, a.c.KVH), block(256);
+  const dim3 grid(a.c.KVH * p.items), block(256);
   auto go = [&](auto type, auto dh) {
     using T = decltype(type);
     constexpr int DH = decltype(dh)::value;
