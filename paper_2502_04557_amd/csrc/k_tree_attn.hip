@@ -14,7 +14,7 @@ struct TreeItem {
   int block, part, parts, share;                   // block of rows, share of slots, how many of them, steps of each
 };
 struct TreePlan {
-  int target, items;                               // shares to aim for; the most items there can be (per KV head)
+  int target, items, sort;                         // shares to aim for; the most items there can be (per KV head)
   TreeItem* list;                                  // [items] parts 0: there is none
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
   float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
@@ -36,7 +36,21 @@ __device__ __forceinline__ TreeSeq tree_seq(const AttendArgs& a, int b, int QB, 
   return s;
 }
 
-// The item of index `item`; false: there is none.  By a whole wave.
+// Sums over the lanes up to this one (itself among them); `all`: over the whole wave.
+__device__ __forceinline__ int scan_to_lane(int v, int& all) {
+#define SPRINTER_SCAN_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+  SPRINTER_SCAN_STEP(0x111, 0xF);   // row_shr:1, 2, 4, 8, then the last lanes of rows into the rows behind them
+  SPRINTER_SCAN_STEP(0x112, 0xF);
+  SPRINTER_SCAN_STEP(0x114, 0xF);
+  SPRINTER_SCAN_STEP(0x118, 0xF);
+  SPRINTER_SCAN_STEP(0x142, 0xA);
+  SPRINTER_SCAN_STEP(0x143, 0xC);
+#undef SPRINTER_SCAN_STEP
+  all = __builtin_amdgcn_readlane(v, 63);
+  return v;
+}
+
+// The item of index `item`, by one wave; false: there is none.
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p, int QB, int item, TreeItem& out) {
   const int lane = threadIdx.x & 63, n = a.c.n_seq;
   TreeSeq s = tree_seq(a, lane, QB, lane < n);
@@ -45,34 +59,27 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     const TreeSeq x = tree_seq(a, b, QB, true);
     work += (float)x.blocks * (float)x.steps;
   }
-  work = wave_sum(work);
-  // The longest sequences first, where there are enough of them to wait for a place and one wave holds them all.
+  work = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_total(work)), 63));
+  // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
+  const int share = (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1;
+  // The longest sequences first, where workgroups wait for a place and one wave holds them all.
   int from = lane;                                 // the sequence that this lane stands for
-  if (n > 4 && n <= 64) {
-    const int key = s.blocks > 0 ? s.steps : -1;
+  if (p.sort) {
+    const int key = (s.blocks > 0 ? min(s.steps, 1 << 24) : 0) * 64 + 63 - lane;   // (no two alike)
     int rank = 0;
-    for (int x = 0; x < n; ++x) {
-      const int other = __builtin_amdgcn_readlane(key, x);
-      rank += other > key || (other == key && x < lane) ? 1 : 0;
-    }
-    auto to = [&](int v) { return __builtin_amdgcn_ds_permute(4 * (lane < n ? rank : lane), v); };
+#pragma unroll
+    for (int x = 0; x < 64; ++x) rank += __builtin_amdgcn_readlane(key, x) > key ? 1 : 0;
+    auto to = [&](int v) { return __builtin_amdgcn_ds_permute(4 * rank, v); };
     s.f0 = to(s.f0); s.n = to(s.n); s.len = to(s.len); s.blocks = to(s.blocks); s.steps = to(s.steps);
     from = to(lane);
   }
-  // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
-  const int share = (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1;
   int base = 0;
   out.parts = 0;
   for (int b0 = 0; b0 < n; b0 += 64) {
     if (b0) s = tree_seq(a, b0 + lane, QB, b0 + lane < n);
     const int parts = (s.steps + share - 1) / share, mine = s.blocks * parts;
-    int sum = mine;                                // items up to this sequence, itself among them
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(sum, o);
-      if (lane >= o) sum += x;
-    }
-    const int before = base + sum - mine;
+    int all;
+    const int before = base + scan_to_lane(mine, all) - mine;
     const u64 hit = __ballot(item >= before && item < before + mine);
     if (hit) {
       const int l = __builtin_ctzll(hit);
@@ -87,9 +94,23 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
       out.part = i - out.block * out.parts;
       break;
     }
-    base += __builtin_amdgcn_readlane(sum, 63);
+    base += all;
   }
   if (p.list && blockIdx.x % a.c.KVH == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
+  return out.parts > 0;
+}
+// The same by a workgroup: its first wave looks, the others get it through LDS.
+__device__ __forceinline__ bool find_item_of_block(const AttendArgs& a, const TreePlan& p, int QB, TreeItem& out) {
+  __shared__ TreeItem shared;
+  if (wave_index() == 0) {
+    find_item(a, p, QB, blockIdx.x / a.c.KVH, out);
+    if (threadIdx.x == 0) shared = out;
+  }
+  __syncthreads();
+  int v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = uniform(reinterpret_cast<const int*>(&shared)[i]);
+  out = TreeItem{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
   return out.parts > 0;
 }
 
@@ -102,15 +123,16 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-// Which of a lane's NK keys a row sees: those from node j0 on (below 0: committed), of which `there` are there.
+// Which of a lane's NK keys a row sees: those from node j0 on (below 0: committed), of which `there` are there.  first: the row's first word of `visible`.
 template <int NK>
-__device__ __forceinline__ unsigned seen_keys(const AttendArgs& a, long long row, int node, int j0, unsigned there) {
+__device__ __forceinline__ unsigned seen_keys(const AttendArgs& a, u64 first, long long row, int node, int j0, unsigned there) {
   unsigned see = (1u << NK) - 1;
   if (j0 + NK > 0) {
     if (a.visible) {
       const int j = max(j0, 0), word = j >> 6, sh = j & 63;
       const unsigned long long* v = a.visible + row * a.n_words;
-      see = word < a.n_words ? (unsigned)(v[word] >> sh) : 0u;
+      see = (unsigned)(first >> sh);
+      if (word) see = word < a.n_words ? (unsigned)(v[word] >> sh) : 0u;
       if (sh > 64 - NK && word + 1 < a.n_words) see |= (unsigned)(v[word + 1] << (64 - sh));
       if (j0 < 0) see = see << -j0 | ((1u << -j0) - 1);
     } else {
@@ -174,7 +196,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   __shared__ float merge[NW / 2][QB][DH];
   __shared__ float stats[NW][QB][2];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x / a.c.KVH, it)) return;
+  if (!find_item_of_block(a, plan, QB, it)) return;
   const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.x % a.c.KVH, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
@@ -185,6 +207,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   long long at_q[QT];
   int node[QT];
   bool row_there[QT];
+  u64 first_word[QT];
   u32x4 q[QT][KF];
   float c = a.scale * 1.4426950408889634f;
   const unsigned flip = c < 0.f ? (HALF ? 0x80008000u : 0x80000000u) : 0u;   // (a negative scale: the queries change their sign)
@@ -196,6 +219,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     const int g = (int)(i % G);
     node[t] = row_there[t] ? (int)(i / G) : 0;
     at_q[t] = (long long)(it.f0 + node[t]);
+    first_word[t] = a.visible ? a.visible[at_q[t] * a.n_words] : 0;
     const T* src = (const T*)a.q + at_q[t] * a.ld_q + ((row_there[t] ? g : 0) + kvh * G) * DH;
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
@@ -295,7 +319,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     for (int t = 0; t < QT; ++t) {
 #pragma unroll
       for (int e = 0; e < NK; ++e) p[t][e] = sc[t][e >> 2][e & 3];
-      bits[t] = plain ? there : seen_keys<NK>(a, at_q[t], node[t], kl - it.len, there);
+      bits[t] = plain ? there : seen_keys<NK>(a, first_word[t], at_q[t], node[t], kl - it.len, there);
       softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
       if constexpr (HALF) {
         split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
@@ -490,7 +514,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   __shared__ __align__(1024) u32x4 ring[S][F][64];
   TreeItem it;
-  if (!find_item(a, plan, QB, blockIdx.x / a.c.KVH, it)) return;
+  if (!find_item_of_block(a, plan, QB, it)) return;
   const int lane = threadIdx.x & 63, w = wave_index(), l16 = lane & 15, lq = lane >> 4, kvh = blockIdx.x % a.c.KVH, G = a.H / a.c.KVH;
   const int shift = a.c.shift, place_mask = (1 << shift) - 1;
   const int slots = (int)min((long long)it.len + it.n, (long long)a.c.n_table << shift);
@@ -502,7 +526,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   // entries of the table, 64 at a time in the lanes of two registers (k0 is a multiple of 128, so that a block's lie in one of them)
   auto ok = [&](int page) { return (unsigned)page < (unsigned)a.c.n_page; };
   int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
-  u64 ok_now = __ballot(ok(now)), ok_before = 0;   // which of these, and of the 64 before them, are pages
+  u64 ok_now = 0, ok_before = 0;                   // which of these, and of the 64 before them, are pages
   auto element = [&](int page, int s) {
     return ((((long long)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) + (s & place_mask)) * DH;
   };
@@ -539,15 +563,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
       }
     }
   };
-  if (n_blk > 0) {
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) issue(i);
-  }
-
   // this lane's rows
   long long at_q[QT];
   int node[QT];
   bool row_there[QT];
+  u64 first_word[QT];
   u32x4 q[QT][KF];
   float c = a.scale * 1.4426950408889634f;
   const unsigned flip = c < 0.f ? 0x80008000u : 0u;
@@ -560,6 +580,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     const int g = (int)(i % G);
     node[t] = row_there[t] ? (int)(i / G) : 0;
     at_q[t] = (long long)(it.f0 + node[t]);
+    first_word[t] = a.visible ? a.visible[at_q[t] * a.n_words] : 0;
     const bf16_t* src = (const bf16_t*)a.q + at_q[t] * a.ld_q + ((row_there[t] ? g : 0) + kvh * G) * DH;
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
@@ -567,6 +588,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
       q[t][f] = row_there[t] ? q[t][f] ^ flip : (u32x4){0, 0, 0, 0};
     }
   }
+  __builtin_amdgcn_sched_barrier(0);               // (the rows' loads are back before the ring's: the compiler's wait for them would be for these too)
+  ok_now = __ballot(ok(now));
+  if (n_blk > 0) {
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) issue(i);
+  }
+
   // the slots that some row of this wave sees end here: none, a chain's last node, all
   const long long rows_left = (long long)it.n * G - r0;
   const int reach = rows_left <= 0 ? 0 : a.visible ? end : (int)min((long long)end, it.len + (r0 + min(rows_left, 16ll * QT) - 1) / G + 1);
@@ -617,7 +645,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     for (int t = 0; t < QT; ++t) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[t][e] = sc[t][e >> 2][e & 3];
-      bits[t] = plain ? there : seen_keys<8>(a, at_q[t], node[t], kl - it.len, there);
+      bits[t] = plain ? there : seen_keys<8>(a, first_word[t], at_q[t], node[t], kl - it.len, there);
       softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
       split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
       split2(p[t][2], p[t][3], ph[t].y, pl[t].y);
@@ -795,6 +823,7 @@ static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_
   const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
   const bool whole = slots <= STEP;                // one share each
   p.items = (int)(blocks + (whole ? 0 : p.target + 1));
+  p.sort = n_seq > 1 && n_seq <= 64 && (long long)p.items * KVH > 512;
   bytes = 0;
   if (!whole) {
     const size_t rows = (size_t)p.items * KVH * shape.QB;
