@@ -501,8 +501,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
 
 // 16 bytes per lane from memory to LDS at `lds` + 16 x lane.  In asm, since the compiler waits for every such load of its builtin in front of the next read of
 // LDS; the kernel's own waits count them.
-__device__ __forceinline__ void piece_to_lds(const bf16_t* src, unsigned lds) {
+__device__ __forceinline__ void piece_to_lds(u64 src, unsigned lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+__device__ __forceinline__ void piece_to_lds(u64 base, unsigned off, unsigned lds) {   // a scalar address and a lane's offset
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 
 // The same for many rows (bf16): the NW waves share the keys and values of the item through a ring of S stages of 32 keys in LDS and have 16 QT rows each.
@@ -523,43 +526,61 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   const int* __restrict__ table = a.c.table + (long long)it.b * a.c.ld_table;
   const int last = max(a.c.n_table - 1, 0);
 
-  // entries of the table, 64 at a time in the lanes of two registers (k0 is a multiple of 128, so that a block's lie in one of them)
-  auto ok = [&](int page) { return (unsigned)page < (unsigned)a.c.n_page; };
-  int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
-  u64 ok_now = 0, ok_before = 0;                   // which of these, and of the 64 before them, are pages
-  auto element = [&](int page, int s) {
-    return ((((long long)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) + (s & place_mask)) * DH;
-  };
-  auto page = [&](int s) { return __builtin_amdgcn_readlane(now, (s >> shift) - e0); };
+  // Entries of the table, 64 at a time in the lanes (k0 is a multiple of 128, so that a block's never lie in two groups of 64): where a page's slots of this KV head
+  // begin, in the keys or in the values as this wave brings them.
   const bool key_wave = w < NW / 2;
   const int first_piece = (key_wave ? w : w - NW / 2) * LPW;
+  auto ok = [&](int page) { return (unsigned)page < (unsigned)a.c.n_page; };
+  auto slots_of = [&](const void* array, int page) {   // (page 0 where the page is not there: read, not used)
+    return (u64)array + (((u64)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) * (2 * DH);
+  };
+  int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
+  u64 at_now = 0, ok_now = 0, ok_before = 0;       // ok: which of these, and of the 64 before them, are pages
+  // A lane's 16 bytes of each of its pieces: rows of 8 keys from group `lane_g` of the block on, and the offset if all of the block lay in one page.  Row i of key
+  // tile t is key 8 (i / 4) + 4 t + i % 4; the 32-byte pieces of a value's row change places.
+  int lane_g[LPW];
+  unsigned lane_off[LPW];
+#pragma unroll
+  for (int j = 0; j < LPW; ++j) {
+    const int piece = first_piece + j;
+    if (key_wave) {
+      lane_g[j] = l16 >> 2;
+      lane_off[j] = (8 * (l16 >> 2) + 4 * (piece / KF) + (l16 & 3)) * (2 * DH) + (piece % KF) * 64 + lq * 16;
+    } else {
+      const int row = piece * (64 / PPR) + lane / PPR;
+      const int swap = DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1;
+      lane_g[j] = row >> 3;
+      lane_off[j] = row * (2 * DH) + ((lane % PPR) ^ (swap << 1)) * 16;
+    }
+  }
+  const unsigned my_ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0][(key_wave ? 0 : 2 * KF) + first_piece][0];
+  auto take_pages = [&]() {
+    ok_now = __ballot(ok(now));
+    at_now = slots_of(key_wave ? a.c.keys : a.c.values, now);
+  };
   auto issue = [&](int i) {
     const int kb = k0 + 32 * min(i, n_blk - 1);
-    if ((kb >> shift) - e0 >= 64) {
+    int e = (kb >> shift) - e0;
+    if (e >= 64) {
       e0 += 64;
+      e -= 64;
       now = then;
       ok_before = ok_now;
-      ok_now = __ballot(ok(now));
+      take_pages();
       then = table[min(e0 + 64 + lane, last)];
     }
-    const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[i % S][(key_wave ? 0 : 2 * KF) + first_piece][0];
-    if (key_wave) {
-      const int s = kb + 8 * (l16 >> 2), g = l16 >> 2;
-      const int p0 = page(kb), p1 = page(kb + 8), p2 = page(kb + 16), p3 = page(kb + 24);
-      const bf16_t* src = (const bf16_t*)a.c.keys + element(g & 2 ? g & 1 ? p3 : p2 : g & 1 ? p1 : p0, s) + (l16 & 3) * DH + lq * 8;
+    const unsigned dst = uniform(my_ring + (i % S) * (F * 1024));
+    if (shift >= 5) {                              // (scalar) the block lies in one page
+      const u64 base = ((u64)(unsigned)__builtin_amdgcn_readlane((int)(at_now >> 32), e) << 32 | (unsigned)__builtin_amdgcn_readlane((int)at_now, e)) +
+                       (unsigned)((kb & place_mask) * (2 * DH));
 #pragma unroll
-      for (int j = 0; j < LPW; ++j) {
-        const int t = (first_piece + j) / KF, f = (first_piece + j) % KF;
-        piece_to_lds(src + t * 4 * DH + f * 32, uniform(dst + j * 1024));
-      }
+      for (int j = 0; j < LPW; ++j) piece_to_lds(base, lane_off[j], dst + j * 1024);
     } else {
 #pragma unroll
       for (int j = 0; j < LPW; ++j) {
-        constexpr int RPP = 64 / PPR;              // rows of a piece: half of 8 keys, or 8
-        const int row = (first_piece + j) * RPP + lane / PPR, s = kb + ((first_piece + j) * RPP & ~7);
-        const int swap = DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1;
-        const int piece = (lane % PPR) ^ (swap << 1);
-        piece_to_lds((const bf16_t*)a.c.values + element(page(s), s) + (row & 7) * DH + piece * 8, uniform(dst + j * 1024));
+        const int s = kb + 8 * lane_g[j], from = (s >> shift) - e0;
+        const u64 page_at = (u64)(unsigned)__shfl((int)(at_now >> 32), from) << 32 | (unsigned)__shfl((int)at_now, from);
+        piece_to_lds(page_at + (s & place_mask) * (2 * DH) + lane_off[j] - lane_g[j] * (16 * DH), dst + j * 1024);
       }
     }
   };
@@ -585,16 +606,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
       q[t][f] = *reinterpret_cast<const u32x4*>(src + f * 32 + lq * 8);
-      q[t][f] = row_there[t] ? q[t][f] ^ flip : (u32x4){0, 0, 0, 0};
     }
   }
-  __builtin_amdgcn_sched_barrier(0);               // (the rows' loads are back before the ring's: the compiler's wait for them would be for these too)
-  ok_now = __ballot(ok(now));
+  take_pages();
   if (n_blk > 0) {
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) issue(i);
   }
 
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int f = 0; f < KF; ++f) q[t][f] = row_there[t] ? q[t][f] ^ flip : (u32x4){0, 0, 0, 0};
   // the slots that some row of this wave sees end here: none, a chain's last node, all
   const long long rows_left = (long long)it.n * G - r0;
   const int reach = rows_left <= 0 ? 0 : a.visible ? end : (int)min((long long)end, it.len + (r0 + min(rows_left, 16ll * QT) - 1) / G + 1);
@@ -611,20 +634,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   const int v_row = 8 * lq + (l16 >> 2), v_swap = DH == 128 ? (v_row & 3) | (v_row >> 3 & 1) << 2 : (v_row >> 1 & 1) | (v_row >> 3 & 1) << 1;
   const unsigned v_off = 2 * KF * 1024 + v_row * (2 * DH) + (v_swap << 5) + (l16 & 3) * 8;
   // One block of 32 keys.  plain: every key is there and seen by every row.
-  auto attend = [&](auto is_plain, int kb, const u32x4(*blk)[64], unsigned pages) __attribute__((always_inline)) {
+  auto attend = [&](auto is_plain, int kb, const uint4 (&K)[2 * KF], const u32x4(*blk)[64], unsigned pages) __attribute__((always_inline)) {
     constexpr bool plain = decltype(is_plain)::value;
     f32x4 sc[QT][2];
 #pragma unroll
     for (int t = 0; t < QT; ++t) sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int f = 0; f < KF; ++f) {
-      const uint4 x0 = __builtin_bit_cast(uint4, blk[f][lane]), x1 = __builtin_bit_cast(uint4, blk[KF + f][lane]);
+    for (int f = 0; f < KF; ++f)
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        sc[t][0] = mfma_bf16(x0, __builtin_bit_cast(uint4, q[t][f]), sc[t][0]);
-        sc[t][1] = mfma_bf16(x1, __builtin_bit_cast(uint4, q[t][f]), sc[t][1]);
+        sc[t][0] = mfma_bf16(K[f], __builtin_bit_cast(uint4, q[t][f]), sc[t][0]);
+        sc[t][1] = mfma_bf16(K[KF + f], __builtin_bit_cast(uint4, q[t][f]), sc[t][1]);
       }
-    }
     uint4 V[CT];
     const unsigned v_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)blk + v_off;
 #pragma unroll
@@ -694,7 +715,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
         const int j = key & 7, g = key >> 3;
         if (!(__ballot(bad >> j & 1) >> (16 * g) & 0xffff)) continue;
         const int s = kb + key;
-        const bf16_t* src = (const bf16_t*)a.c.values + element(table[min(s >> shift, last)], s) + 4 * lq;
+        const bf16_t* src = (const bf16_t*)slots_of(a.c.values, table[min(s >> shift, last)]) + (s & place_mask) * DH + 4 * lq;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           float pj = p[t][0];
@@ -715,26 +736,36 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
       }
     }
   };
-  auto next = [&](int i) {
-    // this wave's part of block i has landed, its reads of block i - 1 are back; then the same of every wave
+  auto landed = [&]() {   // this wave's part of the next block has, its reads of the last one are back; then the same of every wave
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * LPW) : "memory");
-    issue(i + S - 1);
-    const int entry = ((k0 + i * 32) >> shift) - e0;             // (the registers may be a few blocks ahead)
+  };
+  auto block = [&](auto is_plain, int i, unsigned pages) __attribute__((always_inline)) {
+    const int kb = k0 + i * 32;
+    const u32x4(*blk)[64] = ring[i % S];
+    if (kb < reach) {                              // (scalar) something that a row of this wave sees
+      uint4 K[2 * KF];
+#pragma unroll
+      for (int f = 0; f < 2 * KF; ++f) K[f] = __builtin_bit_cast(uint4, blk[f][lane]);
+      issue(i + S - 1);                            // (next to the keys' way out of LDS)
+      attend(is_plain, kb, K, blk, pages);
+    } else {
+      issue(i + S - 1);
+    }
+  };
+  auto pages_of = [&](int i) {                     // (the registers may be a few blocks ahead)
+    const int entry = ((k0 + i * 32) >> shift) - e0;
     return (unsigned)(entry < 0 ? ok_before >> (entry + 64) : ok_now >> entry);
   };
   // First the blocks that every row sees and whose pages are there, up to the first that is none, then the others.
   int i = 0;
-  unsigned pages = n_blk > 0 ? next(0) : 0u;
-  for (; i < n_blk; pages = next(++i)) {
+  if (n_blk > 0) landed();
+  for (; i < n_blk; ++i, landed()) {
     const int kb = k0 + i * 32;
     const unsigned all = (2u << (((kb + 31) >> shift) - (kb >> shift))) - 1;
-    if (kb + 32 > sure || (pages & all) != all) break;
-    if (kb < reach) attend(std::true_type(), kb, ring[i % S], all);
+    if (kb + 32 > sure || (pages_of(i) & all) != all) break;
+    block(std::true_type(), i, all);
   }
-  for (; i < n_blk; pages = next(++i)) {
-    const int kb = k0 + i * 32;
-    if (kb < reach) attend(std::false_type(), kb, ring[i % S], pages);   // (scalar: something that a row of this wave sees)
-  }
+  for (; i < n_blk; ++i, landed()) block(std::false_type(), i, pages_of(i));
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last stages' loads still write to LDS)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
