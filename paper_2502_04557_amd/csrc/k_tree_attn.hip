@@ -509,11 +509,11 @@ __device__ __forceinline__ void piece_to_lds(u64 base, unsigned off, unsigned ld
 }
 
 // The same for many rows (bf16): the NW waves share the keys and values of the item through a ring of S stages of 32 keys in LDS and have 16 QT rows each.
-// Half of the waves bring keys, in operand order, half values, as rows of DH columns; the fragments of V^T are read with ds_read_b64_tr_b16, four keys
-// of a column at a time.  The row's 32-byte pieces lie where an exclusive-or with its number puts them, so that those reads meet no bank twice.
+// Half of the waves bring keys, half values, as whole rows of DH columns; the fragments of V^T are read with ds_read_b64_tr_b16, four keys of a column at a
+// time.  The pieces of a row lie where an exclusive-or with its number puts them, so that no read meets a bank twice.
 template <int DH, int QT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, TreePlan plan) {
-  constexpr int QB = 16 * QT * NW, KF = DH / 32, CT = DH / 16, F = 2 * KF + CT, LPW = F / NW, S = 4, PPR = DH / 8;   // F pieces of 1 KiB a stage, LPW of them by a wave
+  constexpr int QB = 16 * QT * NW, KF = DH / 32, CT = DH / 16, F = 2 * CT, LPW = F / NW, S = 4, PPR = DH / 8;   // F pieces of 1 KiB a stage, LPW of them by a wave
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   __shared__ __align__(1024) u32x4 ring[S][F][64];
   TreeItem it;
@@ -536,24 +536,19 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   };
   int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
   u64 at_now = 0, ok_now = 0, ok_before = 0;       // ok: which of these, and of the 64 before them, are pages
-  // A lane's 16 bytes of each of its pieces: rows of 8 keys from group `lane_g` of the block on, and the offset if all of the block lay in one page.  Row i of key
-  // tile t is key 8 (i / 4) + 4 t + i % 4; the 32-byte pieces of a value's row change places.
+  // A lane's 16 bytes of each of its pieces: whole rows of DH columns, from group `lane_g` of 8 keys of the block on, and the offset if all of the block lay in
+  // one page.  A row's 16-byte pieces (keys) or 32-byte ones (values) lie where an exclusive-or with its number puts them.
+  auto swap_key = [&](int row) { return DH == 128 ? (row & 3) | (row >> 3 & 3) << 2 : (row >> 1 & 1) | (row >> 3 & 3) << 1; };
+  auto swap_value = [&](int row) { return DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1; };
   int lane_g[LPW];
   unsigned lane_off[LPW];
 #pragma unroll
   for (int j = 0; j < LPW; ++j) {
-    const int piece = first_piece + j;
-    if (key_wave) {
-      lane_g[j] = l16 >> 2;
-      lane_off[j] = (8 * (l16 >> 2) + 4 * (piece / KF) + (l16 & 3)) * (2 * DH) + (piece % KF) * 64 + lq * 16;
-    } else {
-      const int row = piece * (64 / PPR) + lane / PPR;
-      const int swap = DH == 128 ? (row & 3) | (row >> 3 & 1) << 2 : (row >> 1 & 1) | (row >> 3 & 1) << 1;
-      lane_g[j] = row >> 3;
-      lane_off[j] = row * (2 * DH) + ((lane % PPR) ^ (swap << 1)) * 16;
-    }
+    const int row = (first_piece + j) * (64 / PPR) + lane / PPR;
+    lane_g[j] = row >> 3;
+    lane_off[j] = row * (2 * DH) + ((lane % PPR) ^ (key_wave ? swap_key(row) : swap_value(row) << 1)) * 16;
   }
-  const unsigned my_ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0][(key_wave ? 0 : 2 * KF) + first_piece][0];
+  const unsigned my_ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0][(key_wave ? 0 : CT) + first_piece][0];
   auto take_pages = [&]() {
     ok_now = __ballot(ok(now));
     at_now = slots_of(key_wave ? a.c.keys : a.c.values, now);
@@ -630,9 +625,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
 #pragma unroll
     for (int i = 0; i < CT; ++i) O[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
-  // where this lane's first column of V^T begins in a stage: 4 keys of tile 0, keys 8 lq + l16 / 4 (+ 4)
-  const int v_row = 8 * lq + (l16 >> 2), v_swap = DH == 128 ? (v_row & 3) | (v_row >> 3 & 1) << 2 : (v_row >> 1 & 1) | (v_row >> 3 & 1) << 1;
-  const unsigned v_off = 2 * KF * 1024 + v_row * (2 * DH) + (v_swap << 5) + (l16 & 3) * 8;
+  // Where this lane's fragments begin in a stage: its 8 columns of key 8 (l16 / 4) + l16 % 4 of tile 0 (4 keys on: tile 1), and its first column of V^T, 4
+  // keys of tile 0, 8 lq + l16 / 4 (4 on: the others).  The pieces of the others are an exclusive-or away.
+  const int k_row = 8 * (l16 >> 2) + (l16 & 3), v_row = 8 * lq + (l16 >> 2);
+  const unsigned k_off = k_row * (2 * DH) + ((lq ^ swap_key(k_row)) << 4);
+  const unsigned v_off = CT * 1024 + v_row * (2 * DH) + (swap_value(v_row) << 5) + (l16 & 3) * 8;
   // One block of 32 keys.  plain: every key is there and seen by every row.
   auto attend = [&](auto is_plain, int kb, const uint4 (&K)[2 * KF], const u32x4(*blk)[64], unsigned pages) __attribute__((always_inline)) {
     constexpr bool plain = decltype(is_plain)::value;
@@ -745,7 +742,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     if (kb < reach) {                              // (scalar) something that a row of this wave sees
       uint4 K[2 * KF];
 #pragma unroll
-      for (int f = 0; f < 2 * KF; ++f) K[f] = __builtin_bit_cast(uint4, blk[f][lane]);
+      for (int f = 0; f < KF; ++f) {
+        typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+        const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)blk + (k_off ^ (f << 6));
+        K[f] = __builtin_bit_cast(uint4, *(lds_u32x4*)(uintptr_t)at);
+        K[KF + f] = __builtin_bit_cast(uint4, *(lds_u32x4*)(uintptr_t)(at + 8 * DH));
+      }
       issue(i + S - 1);                            // (next to the keys' way out of LDS)
       attend(is_plain, kb, K, blk, pages);
     } else {
@@ -845,7 +847,7 @@ static TreeShape tree_shape(int type, int dh, int H, int KVH, int n_seq, int T) 
   auto of = [](int QT, int NW) { return TreeShape{QT, NW, 16 * QT * NW}; };
   if (rows <= 16 || (type == X_F32 && dh == 128)) return of(1, 1);
   if (rows <= 32 || type == X_F32) return of(2, 1);
-  return rows <= 64 ? of(1, 4) : getenv("X8") && rows > 128 ? of(2, 8) : of(2, 4);
+  return rows <= 64 ? of(1, 4) : rows <= 128 ? of(2, 4) : of(2, 8);
 }
 
 static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
