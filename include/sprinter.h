@@ -407,10 +407,11 @@ int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, 
  * The cache: keys and values, each [n_layer, n_page, n_kv_head, page_size, d_head] of dtype, 16-byte aligned; page_size a power of two in
  * [8, 1024], d_head 64 or 128.  Slot s of sequence b is place s % page_size of page table[b, s / page_size], for s < n_table * page_size; table
  * is [n_seq, n_table], rows ld_table apart.  A slot whose entry is outside [0, n_page) is not there: nothing is written to it or read from it.
- * Limits: n_table * page_size < 2^30, n_rows 2^20, n_seq 2^20.
+ * Limits: n_table * page_size < 2^30, n_rows and n_seq 2^20; attend: n_rows * n_head 2^23.  The arguments of a call are a struct in host memory, of pointers to
+ * device memory; it may go when the call has returned.
  *
- * A batch of trees: sequence b has dev_len[b] committed slots, and its nodes are the rows first[b] .. first[b + 1] - 1 of all n_rows rows (first
- * [n_seq + 1], ascending); node i's slot is dev_len[b] + i.  dev_visible [n_rows, n_words], n_words 1 to 16: bit j % 64 of word j / 64 of a
+ * A batch of trees: sequence b has len[b] committed slots, and its nodes are the rows first[b] .. first[b + 1] - 1 of all n_rows rows (first
+ * [n_seq + 1], ascending); node i's slot is len[b] + i.  visible [n_rows, n_words], n_words 1 to 16: bit j % 64 of word j / 64 of a
  * row says whether it sees node j of its sequence (itself among them); nodes beyond the words are not seen.  NULL: a row sees the nodes up to
  * itself.  Rows of no sequence are left as they were. */
 typedef struct {
@@ -418,37 +419,60 @@ typedef struct {
 } sprinter_cache_cfg;
 enum { SPRINTER_PAIRS_HALVES = 0, SPRINTER_PAIRS_NEIGHBOURS = 1 };
 
-/* Writes keys and values of n_rows tokens into one layer, keys turned by their positions on the way: token t goes to slot dev_slot[t] of sequence
- * dev_seq[t].  k, v [n_rows, n_kv_head * d_head] and q [n_rows, n_head * d_head] are of rows_dtype (rows ld_* elements apart); q may be NULL
+/* Writes keys and values of n_rows tokens into one layer, keys turned by their positions on the way: token t goes to slot slot[t] of sequence
+ * seq[t].  k, v [n_rows, n_kv_head * d_head] and q [n_rows, n_head * d_head] are of rows_dtype (rows ld_* elements apart); q may be NULL
  * (n_head 0): else it is turned like the keys and written to q_out, of the cache's dtype (q_out may be q itself where the types agree).  Turned
- * are the first n_turned columns of a head (even, 0 for none) in the pairs (i, i + n_turned / 2) or (2 i, 2 i + 1), by the angle dev_pos[t] * dev_freq[i] (dev_pos
+ * are the first n_turned columns of a head (even, 0 for none) in the pairs (i, i + n_turned / 2) or (2 i, 2 i + 1), by the angle pos[t] * freq[i] (pos
  * NULL: the slot; freq float64 [n_turned / 2], 8-byte aligned); angles in 64 bits, the rest in float32, rounded once.  A token whose sequence is outside [0, n_seq)
  * is padding: nothing of it is written.  No two tokens of a call have one slot: which of them it would hold is not said. */
-int sprinter_cache_append(const sprinter_cache_cfg* cfg, int layer, void* dev_keys, void* dev_values, const int32_t* dev_table,
-                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_seq, const int32_t* dev_slot,
-                          const int32_t* dev_pos, const double* dev_freq, int n_turned, int pairs, int rows_dtype, const void* dev_k,
-                          int64_t ld_k, const void* dev_v, int64_t ld_v, const void* dev_q, int64_t ld_q, int n_head, int n_rows,
-                          void* dev_q_out, int64_t ld_q_out, void* hip_stream);
+typedef struct {
+  int32_t layer, n_seq, n_table, n_rows;
+  void *keys, *values;
+  const int32_t* table; int64_t ld_table;
+  const int32_t *seq, *slot, *pos;
+  const double* freq;
+  const void* k; int64_t ld_k;
+  const void* v; int64_t ld_v;
+  const void* q; int64_t ld_q;
+  void* q_out; int64_t ld_q_out;
+  int32_t n_head, n_turned, pairs, rows_dtype;
+} sprinter_append;
+int sprinter_cache_append(const sprinter_cache_cfg* cfg, const sprinter_append* args, void* hip_stream);
 
 /* y[t, h] = sum over the slots j that row t sees of softmax_j(scale q[t, h] . key_j) value_j, with the keys and values of KV head h / (n_head /
  * n_kv_head): the committed slots of t's sequence and its visible nodes, as far as they are there.  q and y [n_rows, n_head * d_head] have the cache's dtype, rows 16-byte
  * aligned.  A score of -infinity has no weight; a row that sees nothing, or nothing else, gives zeros.  What a row does not see does not reach
  * it, not as infinity or NaN either.  float32: float32 throughout.  bf16: products of bf16 with float32 sums, the weights of the values as two
- * bf16 each (16 bits), statistics float32.  The same call gives the same bits.  dev_workspace: sprinter_cache_attend_bytes, 256-byte aligned, in use
+ * bf16 each (16 bits), statistics float32.  The same call gives the same bits.  workspace: sprinter_cache_attend_bytes, 256-byte aligned, in use
  * until the call's work is done (0 bytes: may be NULL). */
+typedef struct {
+  int32_t layer, n_seq, n_table, n_rows;
+  const void *keys, *values;
+  const int32_t* table; int64_t ld_table;
+  const int32_t *len, *first;
+  const uint64_t* visible;
+  const void* q; int64_t ld_q;
+  void* y; int64_t ld_y;
+  void* workspace; uint64_t workspace_bytes;
+  int32_t n_words, n_head;
+  float scale;
+} sprinter_attend;
 int sprinter_cache_attend_bytes(const sprinter_cache_cfg* cfg, int n_head, int n_seq, int n_table, int n_rows, size_t* out_workspace);
-int sprinter_cache_attend(const sprinter_cache_cfg* cfg, int layer, const void* dev_keys, const void* dev_values, const int32_t* dev_table,
-                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_len, const int32_t* dev_first,
-                          const uint64_t* dev_visible, int n_words, int n_head, float scale, const void* dev_q, int64_t ld_q,
-                          int n_rows, void* dev_y, int64_t ld_y, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+int sprinter_cache_attend(const sprinter_cache_cfg* cfg, const sprinter_attend* args, void* hip_stream);
 
-/* The accepted path of each tree becomes committed: in every layer, slot dev_len[b] + path[b, j] is copied to slot dev_len[b] + j, for j < n_keep[b] (at
+/* The accepted path of each tree becomes committed: in every layer, slot len[b] + path[b, j] is copied to slot len[b] + j, for j < n_keep[b] (at
  * most n_path), as if all were read before one is written.  path [n_seq, n_path] (rows ld_path apart) names nodes in ascending order; an entry below j, or that
- * is no node of the tree, moves nothing, nor does a slot that is not there.  dev_len itself is the caller's to advance.  dev_keys and dev_values are the whole
+ * is no node of the tree, moves nothing, nor does a slot that is not there.  len itself is the caller's to advance.  keys and values are the whole
  * cache. */
-int sprinter_cache_keep(const sprinter_cache_cfg* cfg, void* dev_keys, void* dev_values, const int32_t* dev_table, int64_t ld_table,
-                        int n_seq, int n_table, const int32_t* dev_len, const int32_t* dev_first, const int32_t* dev_path,
-                        int64_t ld_path, int n_path, const int32_t* dev_n_keep, void* hip_stream);
+typedef struct {
+  int32_t n_seq, n_table, n_path;
+  void *keys, *values;
+  const int32_t* table; int64_t ld_table;
+  const int32_t *len, *first;
+  const int32_t* path; int64_t ld_path;
+  const int32_t* n_keep;
+} sprinter_keep;
+int sprinter_cache_keep(const sprinter_cache_cfg* cfg, const sprinter_keep* args, void* hip_stream);
 
 /* out[t, v] of logits [n_rows, vocab] (dtype; out may be logits itself), each step only where its arrays are given:
  *   x = logits[t, v];  x = x > 0 ? x / repetition : x * repetition, if v is among the row's tokens;

@@ -89,10 +89,10 @@ def load_library(path: str = LIB_PATH):
     lib.sprinter_experts_pack.argtypes = [vp, i32, vp, vp, vp]
     lib.sprinter_experts.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, i32, i32, vp, i64, vp, sz, vp]
     lib.sprinter_block_norm.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, i64, vp, i64, vp]
-    lib.sprinter_cache_append.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp]
+    lib.sprinter_cache_append.argtypes = [vp, vp, vp]
     lib.sprinter_cache_attend_bytes.argtypes = [vp, i32, i32, i32, i32, psz]
-    lib.sprinter_cache_attend.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, vp, vp, vp, i32, i32, C.c_float, vp, i64, i32, vp, i64, vp, sz, vp]
-    lib.sprinter_cache_keep.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, i64, i32, vp, vp]
+    lib.sprinter_cache_attend.argtypes = [vp, vp, vp]
+    lib.sprinter_cache_keep.argtypes = [vp, vp, vp]
     lib.sprinter_adjust_logits.argtypes = [vp, vp]
     lib.sprinter_destroy.argtypes = [vp]
     lib.sprinter_destroy.restype = None

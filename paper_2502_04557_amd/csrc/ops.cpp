@@ -36,6 +36,8 @@ int check_pairs(int n_rows, int top_k, const char* who) {
 }
 
 constexpr int MAX_TREE_ROWS = 1 << 20;
+static_assert(sizeof(sprinter_append) == 160 && sizeof(sprinter_attend) == 136 && sizeof(sprinter_keep) == 88 && sizeof(sprinter_logits) == 200,
+              "the layouts that bindings pack");
 
 // What every call on a cache in pages has; fills *c for one layer's arrays.
 int check_cache(const sprinter_cache_cfg* g, int layer, const void* keys, const void* values, const int32_t* table, int64_t ld_table, int n_seq,
@@ -71,6 +73,13 @@ int check_heads(const sprinter_cache_cfg* g, int n_head, const char* who) {
 
 int check_tree_rows(int n_rows, const char* who) {
   if (n_rows < 0 || n_rows > MAX_TREE_ROWS) return op_fail(SPRINTER_E_RANGE, "%s: %d rows are not in [0, %d]", who, n_rows, MAX_TREE_ROWS);
+  return SPRINTER_OK;
+}
+
+int check_attended(int n_rows, int n_head, const char* who) {
+  const int rc = check_tree_rows(n_rows, who);
+  if (rc) return rc;
+  if ((long long)n_rows * n_head > 1 << 23) return op_fail(SPRINTER_E_RANGE, "%s: %d rows of %d heads are more than 2^23", who, n_rows, n_head);
   return SPRINTER_OK;
 }
 
@@ -177,34 +186,32 @@ int sprinter_block_norm(const sprinter_block_norm_cfg* cfg, const float* dev_h, 
   return launched("sprinter_block_norm");
 }
 
-int sprinter_cache_append(const sprinter_cache_cfg* cfg, int layer, void* dev_keys, void* dev_values, const int32_t* dev_table,
-                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_seq, const int32_t* dev_slot, const int32_t* dev_pos,
-                          const double* dev_freq, int n_turned, int pairs, int rows_dtype, const void* dev_k, int64_t ld_k, const void* dev_v,
-                          int64_t ld_v, const void* dev_q, int64_t ld_q, int n_head, int n_rows, void* dev_q_out, int64_t ld_q_out,
-                          void* hip_stream) {
+int sprinter_cache_append(const sprinter_cache_cfg* cfg, const sprinter_append* args, void* hip_stream) {
   const char* who = "sprinter_cache_append";
+  if (!args) return op_fail(SPRINTER_E_NULL, "%s: NULL arguments", who);
+  const sprinter_append& x = *args;
   AppendArgs a{};
-  int rc = check_cache(cfg, layer, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
-  if (rc || (rc = check_tree_rows(n_rows, who)) || (n_head != 0 && (rc = check_heads(cfg, n_head, who)))) return rc;
-  if (n_turned < 0 || n_turned > cfg->d_head || n_turned % 2)
-    return op_fail(SPRINTER_E_RANGE, "%s: n_turned %d is no even number up to d_head %d", who, n_turned, cfg->d_head);
-  if (pairs != SPRINTER_PAIRS_HALVES && pairs != SPRINTER_PAIRS_NEIGHBOURS) return op_fail(SPRINTER_E_CONFIG, "%s: unknown pairs %d", who, pairs);
-  if (rows_dtype != SPRINTER_F32 && rows_dtype != SPRINTER_BF16) return op_fail(SPRINTER_E_CONFIG, "%s: unknown rows_dtype %d", who, rows_dtype);
-  if (n_rows == 0 || n_seq == 0) return SPRINTER_OK;
-  if (!dev_seq || !dev_slot || !dev_k || !dev_v || (n_turned && !dev_freq) || (n_head && (!dev_q || !dev_q_out)))
+  int rc = check_cache(cfg, x.layer, x.keys, x.values, x.table, x.ld_table, x.n_seq, x.n_table, who, &a.c);
+  if (rc || (rc = check_tree_rows(x.n_rows, who)) || (x.n_head != 0 && (rc = check_heads(cfg, x.n_head, who)))) return rc;
+  if (x.n_turned < 0 || x.n_turned > cfg->d_head || x.n_turned % 2)
+    return op_fail(SPRINTER_E_RANGE, "%s: n_turned %d is no even number up to d_head %d", who, x.n_turned, cfg->d_head);
+  if (x.pairs != SPRINTER_PAIRS_HALVES && x.pairs != SPRINTER_PAIRS_NEIGHBOURS) return op_fail(SPRINTER_E_CONFIG, "%s: unknown pairs %d", who, x.pairs);
+  if (x.rows_dtype != SPRINTER_F32 && x.rows_dtype != SPRINTER_BF16) return op_fail(SPRINTER_E_CONFIG, "%s: unknown rows_dtype %d", who, x.rows_dtype);
+  if (x.n_rows == 0 || x.n_seq == 0) return SPRINTER_OK;
+  if (!x.seq || !x.slot || !x.k || !x.v || (x.n_turned && !x.freq) || (x.n_head && (!x.q || !x.q_out)))
     return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
-  const int w = cfg->n_kv_head * cfg->d_head, wq = n_head * cfg->d_head;
-  if (n_rows > 1 && (ld_k < w || ld_v < w || (n_head && (ld_q < wq || ld_q_out < wq))))
+  const int w = cfg->n_kv_head * cfg->d_head, wq = x.n_head * cfg->d_head;
+  if (x.n_rows > 1 && (x.ld_k < w || x.ld_v < w || (x.n_head && (x.ld_q < wq || x.ld_q_out < wq))))
     return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their columns", who);
-  const size_t in = element(rows_dtype), out = element(cfg->dtype);
-  if (!aligned(dev_seq, 4) || !aligned(dev_slot, 4) || !aligned(dev_pos, 4) || !aligned(dev_freq, 8) || !aligned(dev_k, in) || !aligned(dev_v, in) ||
-      (n_head && (!aligned(dev_q, in) || !aligned(dev_q_out, out))))
+  const size_t in = element(x.rows_dtype), out = element(cfg->dtype);
+  if (!aligned(x.seq, 4) || !aligned(x.slot, 4) || !aligned(x.pos, 4) || !aligned(x.freq, 8) || !aligned(x.k, in) || !aligned(x.v, in) ||
+      (x.n_head && (!aligned(x.q, in) || !aligned(x.q_out, out))))
     return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
   a.cache_type = cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16;
-  a.row_type = rows_dtype == SPRINTER_F32 ? X_F32 : X_BF16;
-  a.H = n_head; a.T = n_rows; a.n_turned = n_turned; a.pairs = pairs;
-  a.seq = dev_seq; a.slot = dev_slot; a.pos = dev_pos; a.freq = dev_freq;
-  a.k = dev_k; a.ld_k = ld_k; a.v = dev_v; a.ld_v = ld_v; a.q = dev_q; a.ld_q = ld_q; a.q_out = dev_q_out; a.ld_q_out = ld_q_out;
+  a.row_type = x.rows_dtype == SPRINTER_F32 ? X_F32 : X_BF16;
+  a.H = x.n_head; a.T = x.n_rows; a.n_turned = x.n_turned; a.pairs = x.pairs;
+  a.seq = x.seq; a.slot = x.slot; a.pos = x.pos; a.freq = x.freq;
+  a.k = x.k; a.ld_k = x.ld_k; a.v = x.v; a.ld_v = x.ld_v; a.q = x.q; a.ld_q = x.ld_q; a.q_out = x.q_out; a.ld_q_out = x.ld_q_out;
   launching();
   launch_cache_append(a, (hipStream_t)hip_stream);
   return launched(who);
@@ -215,62 +222,62 @@ int sprinter_cache_attend_bytes(const sprinter_cache_cfg* cfg, int n_head, int n
   PagedArgs c;
   const void* some = (const void*)256;                 // (only the sizes are looked at)
   int rc = check_cache(cfg, 0, some, some, (const int32_t*)some, n_table, n_seq, n_table, who, &c);
-  if (rc || (rc = check_heads(cfg, n_head, who)) || (rc = check_tree_rows(n_rows, who))) return rc;
+  if (rc || (rc = check_heads(cfg, n_head, who)) || (rc = check_attended(n_rows, n_head, who))) return rc;
   if (!out_workspace) return op_fail(SPRINTER_E_NULL, "%s: NULL result", who);
   *out_workspace = attend_workspace(cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16, cfg->d_head, n_head, cfg->n_kv_head, n_seq, n_rows,
                                     (long long)n_table * cfg->page_size);
   return SPRINTER_OK;
 }
 
-int sprinter_cache_attend(const sprinter_cache_cfg* cfg, int layer, const void* dev_keys, const void* dev_values, const int32_t* dev_table,
-                          int64_t ld_table, int n_seq, int n_table, const int32_t* dev_len, const int32_t* dev_first,
-                          const uint64_t* dev_visible, int n_words, int n_head, float scale, const void* dev_q, int64_t ld_q, int n_rows,
-                          void* dev_y, int64_t ld_y, void* dev_workspace, size_t workspace_bytes, void* hip_stream) {
+int sprinter_cache_attend(const sprinter_cache_cfg* cfg, const sprinter_attend* args, void* hip_stream) {
   const char* who = "sprinter_cache_attend";
+  if (!args) return op_fail(SPRINTER_E_NULL, "%s: NULL arguments", who);
+  const sprinter_attend& x = *args;
   AttendArgs a{};
-  int rc = check_cache(cfg, layer, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
-  if (rc || (rc = check_heads(cfg, n_head, who)) || (rc = check_tree_rows(n_rows, who))) return rc;
-  if (dev_visible && (n_words < 1 || n_words > MAX_NODE_WORDS))
-    return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, n_words, MAX_NODE_WORDS);
-  if (!(scale - scale == 0.f)) return op_fail(SPRINTER_E_CONFIG, "%s: scale is not finite", who);
-  if (n_rows == 0 || n_seq == 0) return SPRINTER_OK;
-  if (!dev_len || !dev_first || !dev_q || !dev_y) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
-  const int w = n_head * cfg->d_head;
+  int rc = check_cache(cfg, x.layer, x.keys, x.values, x.table, x.ld_table, x.n_seq, x.n_table, who, &a.c);
+  if (rc || (rc = check_heads(cfg, x.n_head, who)) || (rc = check_attended(x.n_rows, x.n_head, who))) return rc;
+  if (x.visible && (x.n_words < 1 || x.n_words > MAX_NODE_WORDS))
+    return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, x.n_words, MAX_NODE_WORDS);
+  if (!(x.scale - x.scale == 0.f)) return op_fail(SPRINTER_E_CONFIG, "%s: scale is not finite", who);
+  if (x.n_rows == 0 || x.n_seq == 0) return SPRINTER_OK;
+  if (!x.len || !x.first || !x.q || !x.y) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  const int w = x.n_head * cfg->d_head;
   const size_t es = element(cfg->dtype);
-  if (n_rows > 1 && (ld_q < w || ld_y < w)) return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their %d columns", who, w);
-  if (!aligned(dev_q, 16) || !aligned(dev_y, 16) || (n_rows > 1 && ((ld_q * es) % 16 || (ld_y * es) % 16)))
+  if (x.n_rows > 1 && (x.ld_q < w || x.ld_y < w)) return op_fail(SPRINTER_E_RANGE, "%s: rows lie closer than their %d columns", who, w);
+  if (!aligned(x.q, 16) || !aligned(x.y, 16) || (x.n_rows > 1 && ((x.ld_q * es) % 16 || (x.ld_y * es) % 16)))
     return op_fail(SPRINTER_E_RANGE, "%s: rows are not 16-byte aligned", who);
-  if (!aligned(dev_len, 4) || !aligned(dev_first, 4) || !aligned(dev_visible, 8))
+  if (!aligned(x.len, 4) || !aligned(x.first, 4) || !aligned(x.visible, 8))
     return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
   a.type = cfg->dtype == SPRINTER_F32 ? X_F32 : X_BF16;
-  const size_t need = attend_workspace(a.type, cfg->d_head, n_head, cfg->n_kv_head, n_seq, n_rows, (long long)n_table * cfg->page_size);
-  if (need && !dev_workspace) return op_fail(SPRINTER_E_NULL, "%s: NULL workspace", who);
-  if (!aligned(dev_workspace, 256)) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace is not 256-byte aligned", who);
-  if (workspace_bytes < need) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
-  a.H = n_head; a.T = n_rows; a.n_words = n_words; a.scale = scale; a.lens = dev_len; a.first = dev_first;
-  a.visible = (const unsigned long long*)dev_visible; a.q = dev_q; a.ld_q = ld_q; a.y = dev_y; a.ld_y = ld_y;
+  const size_t need = attend_workspace(a.type, cfg->d_head, x.n_head, cfg->n_kv_head, x.n_seq, x.n_rows, (long long)x.n_table * cfg->page_size);
+  if (need && !x.workspace) return op_fail(SPRINTER_E_NULL, "%s: NULL workspace", who);
+  if (!aligned(x.workspace, 256)) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace is not 256-byte aligned", who);
+  if (x.workspace_bytes < need)
+    return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, (size_t)x.workspace_bytes, need);
+  a.H = x.n_head; a.T = x.n_rows; a.n_words = x.n_words; a.scale = x.scale; a.lens = x.len; a.first = x.first;
+  a.visible = (const unsigned long long*)x.visible; a.q = x.q; a.ld_q = x.ld_q; a.y = x.y; a.ld_y = x.ld_y;
   launching();
-  launch_cache_attend(a, dev_workspace, (hipStream_t)hip_stream);
+  launch_cache_attend(a, x.workspace, (hipStream_t)hip_stream);
   return launched(who);
 }
 
-int sprinter_cache_keep(const sprinter_cache_cfg* cfg, void* dev_keys, void* dev_values, const int32_t* dev_table, int64_t ld_table, int n_seq,
-                        int n_table, const int32_t* dev_len, const int32_t* dev_first, const int32_t* dev_path, int64_t ld_path, int n_path,
-                        const int32_t* dev_n_keep, void* hip_stream) {
+int sprinter_cache_keep(const sprinter_cache_cfg* cfg, const sprinter_keep* args, void* hip_stream) {
   const char* who = "sprinter_cache_keep";
+  if (!args) return op_fail(SPRINTER_E_NULL, "%s: NULL arguments", who);
+  const sprinter_keep& x = *args;
   KeepArgs a{};
-  const int rc = check_cache(cfg, 0, dev_keys, dev_values, dev_table, ld_table, n_seq, n_table, who, &a.c);
+  const int rc = check_cache(cfg, 0, x.keys, x.values, x.table, x.ld_table, x.n_seq, x.n_table, who, &a.c);
   if (rc) return rc;
-  if (n_path < 0) return op_fail(SPRINTER_E_RANGE, "%s: a path of %d", who, n_path);
-  if (n_seq == 0 || n_path == 0) return SPRINTER_OK;
-  if (!dev_len || !dev_first || !dev_path || !dev_n_keep) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
-  if (n_seq > 1 && ld_path < n_path) return op_fail(SPRINTER_E_RANGE, "%s: rows %lld apart hold no path of %d", who, (long long)ld_path, n_path);
-  if (!aligned(dev_len, 4) || !aligned(dev_first, 4) || !aligned(dev_path, 4) || !aligned(dev_n_keep, 4))
+  if (x.n_path < 0) return op_fail(SPRINTER_E_RANGE, "%s: a path of %d", who, x.n_path);
+  if (x.n_seq == 0 || x.n_path == 0) return SPRINTER_OK;
+  if (!x.len || !x.first || !x.path || !x.n_keep) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
+  if (x.n_seq > 1 && x.ld_path < x.n_path) return op_fail(SPRINTER_E_RANGE, "%s: rows %lld apart hold no path of %d", who, (long long)x.ld_path, x.n_path);
+  if (!aligned(x.len, 4) || !aligned(x.first, 4) || !aligned(x.path, 4) || !aligned(x.n_keep, 4))
     return op_fail(SPRINTER_E_RANGE, "%s: an array is not aligned to its elements", who);
   a.n_layer = cfg->n_layer;
   a.element = (int)element(cfg->dtype);
   a.layer_bytes = (long long)cfg->n_page * cfg->n_kv_head * cfg->page_size * cfg->d_head * a.element;
-  a.lens = dev_len; a.first = dev_first; a.path = dev_path; a.ld_path = ld_path; a.n_path = n_path; a.n_keep = dev_n_keep;
+  a.lens = x.len; a.first = x.first; a.path = x.path; a.ld_path = x.ld_path; a.n_path = x.n_path; a.n_keep = x.n_keep;
   launching();
   launch_cache_keep(a, (hipStream_t)hip_stream);
   return launched(who);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 from functools import lru_cache
 from numbers import Integral, Real
+import struct
 import torch
 import torch.autograd.forward_ad as forward_ad
 
@@ -255,52 +256,68 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
 
 # ------------------------------------------------------------------------------------ a round of drafted trees over a cache in pages
 PAIRS = {"halves": 0, "neighbours": 1}
+Tensor = torch.Tensor
+
+# The structs of include/sprinter.h, packed in one go: arguments by the dozen cost ctypes 0.1 us each.
+_APPEND = struct.Struct("4i 2P Pq 3P P Pq Pq Pq Pq 4i")
+_ATTEND = struct.Struct("4i 2P Pq 2P P Pq Pq PQ 2if 0Q")
+_KEEP = struct.Struct("3i 2P Pq 2P Pq P")
+_LOGITS = struct.Struct("4i Pq Pq P Pq 2P 3P P P Pq Pq Pq P 4i")
 
 
 class CacheCfgC(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_layer", "n_page", "page_size", "n_kv_head", "d_head")]
 
 
-class LogitsC(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_rows", "vocab", "n_seq")] + [
-        ("logits", C.c_void_p), ("ld_logits", C.c_int64), ("out", C.c_void_p), ("ld_out", C.c_int64), ("first", C.c_void_p),
-        ("tokens", C.c_void_p), ("ld_tokens", C.c_int64)] + [
-        (n, C.c_void_p) for n in ("n_token", "n_prompt", "repetition", "presence", "frequency", "draft", "visible")] + [
-        ("bias_ids", C.c_void_p), ("ld_bias_ids", C.c_int64), ("bias", C.c_void_p), ("ld_bias", C.c_int64), ("mask", C.c_void_p), ("ld_mask", C.c_int64),
-        ("mask_row", C.c_void_p)] + [(n, C.c_int32) for n in ("n_tokens", "n_words", "n_bias", "n_mask")]
+def _vector(name, t, device, dtype, n):
+    """A contiguous vector of n elements (the checks in the order of their cost first, then the words for what fails one)."""
+    if isinstance(t, Tensor) and t.dtype is dtype and t.device == device and t.shape == (n,) and t.is_contiguous() and not (t.requires_grad or t.is_neg()) and \
+            forward_ad._current_level < 0:
+        return
+    _tensor(name, t, device, dtype)
+    if t.shape != (n,):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{n}]")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+
+
+def _lines(name, t, device, dtype, rows, cols):
+    """`_rows` -> its shape, for what it mostly gets: the checks in the order of their cost first, then the other's words for what fails one."""
+    if isinstance(t, Tensor) and t.dtype is dtype and t.device == device and len(shape := t.shape) == 2:
+        n, m = shape
+        if (rows is None or rows == n) and (cols is None or cols == m) and t.is_contiguous() and not (t.requires_grad or t.is_neg()) and n < 2 ** 31 and \
+                forward_ad._current_level < 0:
+            return shape
+    _rows(name, t, device, dtype, rows, cols)
+    return t.shape
+
+
+def _layer(v):
+    return v if type(v) is int and 0 <= v < 65536 else _int32("layer", v)
+
+
+def _words(visible, device, rows):
+    """The words of a row of `visible`."""
+    if visible is None:
+        return 0
+    words = visible.shape[1] if isinstance(visible, torch.Tensor) and visible.dim() == 2 else 0
+    _whole("visible", visible, device, torch.int64, rows, max(1, words))
+    return words
+
+
+def _address(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _line(t):
+    """The address of a matrix and how far apart its rows lie."""
+    return (0, 0) if t is None else (t.data_ptr(), t.stride(0))
 
 
 def _wrote(t):
     """A tensor that is written in place; one of inference mode counts no versions."""
     if not t.is_inference():
         _written(t)
-
-
-def _vector(name, t, device, dtype, n):
-    """A contiguous vector of n elements."""
-    _tensor(name, t, device, dtype)
-    shape = t.shape
-    if len(shape) != 1 or shape[0] != n:
-        raise ValueError(f"{name}: shape {tuple(shape)}, expected [{n}]")
-    if n > 1 and t.stride(0) != 1:
-        raise ValueError(f"{name}: not contiguous")
-
-
-def _trees(first, visible, device, rows):
-    """Checks what describes a batch of trees -> (sequences, words of a row of `visible`)."""
-    n = first.shape[0] - 1 if isinstance(first, torch.Tensor) and first.dim() == 1 else -1
-    if n < 0:
-        raise ValueError("first: an int32 vector [n_seq + 1] is needed")
-    _vector("first", first, device, torch.int32, n + 1)
-    return _int32("n_seq", n), _words(visible, device, rows)
-
-
-def _words(visible, device, rows):
-    if visible is None:
-        return 0
-    words = visible.shape[1] if isinstance(visible, torch.Tensor) and visible.dim() == 2 else 0
-    _whole("visible", visible, device, torch.int64, rows, max(1, words))
-    return words
 
 
 class PagedCache:
@@ -324,13 +341,8 @@ class PagedCache:
         self.n_layer, self.n_page, self.n_kv_head, self.page_size, self.d_head = shape
         self._cfg = CacheCfgC(DTYPES[keys.dtype], *(_int32("keys' sizes", shape[i]) for i in (0, 1, 3, 2, 4)))
         self._ref = C.byref(self._cfg)
-        self._arrays = keys.data_ptr(), values.data_ptr()
+        self._counted = tuple(t for t in (keys, values) if not t.is_inference())   # (tensors of inference mode count no versions)
         self._need = {}
-
-    def _table(self, table):
-        _rows("table", table, self.device, torch.int32, None, None)
-        n_seq, n = table.shape
-        return n_seq, (table.data_ptr(), table.stride(0), n_seq, _int32("table's columns", n))
 
     def append(self, layer, keys, values, table, seq, slot, *, q=None, pos=None, freq=None, pairs="halves", q_out=None):
         """Writes the rows keys, values [T, n_kv_head * d_head] to slot[t] of sequence seq[t] (both int32 [T]); -> q turned, or None (sprinter_cache_append).
@@ -338,14 +350,13 @@ class PagedCache:
         With freq (float64 [n / 2]) the first n columns of each head of the keys and of q [T, n_head * d_head] are turned by the angles pos[t] * freq (pos int32
         [T], by default the slot), in the pairs (i, i + n / 2) ("halves") or (2 i, 2 i + 1) ("neighbours").  Rows are bfloat16 or float32, all of one
         type; what is written has the cache's.  A token of no sequence (-1) is padding.  q_out: where the turned q goes (q itself turns it in place)."""
-        dev = self.device
+        dev, d = self.device, self.d_head
         if not isinstance(keys, torch.Tensor) or keys.dtype not in DTYPES:
             raise ValueError("keys: bfloat16 or float32 rows are needed")
-        width = self.n_kv_head * self.d_head
-        _rows("keys", keys, dev, keys.dtype, None, width)
-        T = keys.shape[0]
-        _rows("values", values, dev, keys.dtype, T, width)
-        _, table_args = self._table(table)
+        width, dtype = self.n_kv_head * d, keys.dtype
+        T, _ = _lines("keys", keys, dev, dtype, None, width)
+        _lines("values", values, dev, dtype, T, width)
+        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
         _vector("seq", seq, dev, torch.int32, T)
         _vector("slot", slot, dev, torch.int32, T)
         if pos is not None:
@@ -358,21 +369,21 @@ class PagedCache:
             raise ValueError(f"pairs is one of {tuple(PAIRS)}")
         H, given = 0, q_out is not None
         if q is not None:
-            _rows("q", q, dev, keys.dtype, T, None)
-            H = q.shape[1] // self.d_head
-            if H < 1 or q.shape[1] != H * self.d_head:
-                raise ValueError(f"q: {q.shape[1]} columns are no heads of {self.d_head}")
+            _, wide = _lines("q", q, dev, dtype, T, None)
+            H = wide // d
+            if H < 1 or wide != H * d:
+                raise ValueError(f"q: {wide} columns are no heads of {d}")
             if given:
-                _rows("q_out", q_out, dev, self.dtype, T, q.shape[1])
+                _lines("q_out", q_out, dev, self.dtype, T, wide)
             else:
-                q_out = torch.empty(T, q.shape[1], dtype=self.dtype, device=dev)
+                q_out = torch.empty((T, wide), dtype=self.dtype, device=dev)
         elif given:
             raise ValueError("q_out: there is no q")
-        _call("sprinter_cache_append", dev, self._ref, _int32("layer", layer), *self._arrays, *table_args, seq.data_ptr(), slot.data_ptr(), _ptr(pos),
-              _ptr(freq), 2 * n, PAIRS[pairs], DTYPES[keys.dtype], keys.data_ptr(), keys.stride(0), values.data_ptr(), values.stride(0), _ptr(q),
-              0 if q is None else q.stride(0), H, T, _ptr(q_out), 0 if q_out is None else q_out.stride(0))
-        _wrote(self.keys)
-        _wrote(self.values)
+        _call("sprinter_cache_append", dev, self._ref, _APPEND.pack(
+            _layer(layer), n_seq, _int32("table's columns", n_table), T, self.keys.data_ptr(), self.values.data_ptr(), *_line(table), seq.data_ptr(), slot.data_ptr(),
+            _address(pos), _address(freq), *_line(keys), *_line(values), *_line(q), *_line(q_out), H, 2 * n, PAIRS[pairs], DTYPES[dtype]))
+        if self._counted:
+            _written(self._counted)
         if given:
             _wrote(q_out)
         return q_out
@@ -382,26 +393,25 @@ class PagedCache:
         sees (sprinter_cache_attend).  scale: of the scores, by default d_head ** -0.5.  A row that sees nothing gives zeros; rows of no
         sequence are not written."""
         dev = self.device
-        _rows("q", q, dev, self.dtype, None, None)
-        T, width = q.shape
+        T, width = _lines("q", q, dev, self.dtype, None, None)
         H = width // self.d_head
         if H < 1 or width != H * self.d_head:
             raise ValueError(f"q: {width} columns are no heads of {self.d_head}")
-        n_seq, table_args = self._table(table)
+        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
         _vector("lens", lens, dev, torch.int32, n_seq)
-        n, words = _trees(first, visible, dev, T)
-        if n != n_seq:
-            raise ValueError(f"first: {n} sequences, table has {n_seq}")
+        _vector("first", first, dev, torch.int32, n_seq + 1)
+        words = _words(visible, dev, T)
         given = out is not None
         if given:
-            _rows("out", out, dev, self.dtype, T, width)
+            _lines("out", out, dev, self.dtype, T, width)
         else:
-            out = torch.empty(T, width, dtype=self.dtype, device=dev)
+            out = torch.empty((T, width), dtype=self.dtype, device=dev)
         scale = self.d_head ** -0.5 if scale is None else float(_number("scale", scale))
-        need = self._workspace(H, n_seq, table_args[3], T)
+        need = self._workspace(H, n_seq, n_table, T)
         work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        _call("sprinter_cache_attend", dev, self._ref, _int32("layer", layer), *self._arrays, *table_args, lens.data_ptr(), first.data_ptr(),
-              _ptr(visible), words, H, scale, q.data_ptr(), q.stride(0), T, out.data_ptr(), out.stride(0), _ptr(work), need)
+        _call("sprinter_cache_attend", dev, self._ref, _ATTEND.pack(
+            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), *_line(table), lens.data_ptr(), first.data_ptr(), _address(visible),
+            *_line(q), *_line(out), _address(work), need, words, H, scale))
         if given:
             _wrote(out)
         return out
@@ -410,7 +420,7 @@ class PagedCache:
         n = self._need.get((H, n_seq, n_table, T))
         if n is None:
             v = C.c_size_t(0)
-            rc = _entry("sprinter_cache_attend_bytes")(self._ref, _int32("heads", H), n_seq, n_table, T, C.byref(v))
+            rc = _entry("sprinter_cache_attend_bytes")(self._ref, _int32("heads", H), n_seq, _int32("table's columns", n_table), T, C.byref(v))
             if rc:
                 raise SprinterError(rc, _lib.sprinter_last_error(None).decode())
             if len(self._need) >= 4096:
@@ -422,15 +432,16 @@ class PagedCache:
         """Slot lens[b] + path[b, j] -> slot lens[b] + j in every layer, j < n_keep[b] (path int32 [n_seq, n], nodes in ascending order; n_keep int32
         [n_seq]): the accepted nodes become the next committed slots (sprinter_cache_keep).  lens is the caller's to advance."""
         dev = self.device
-        n_seq, table_args = self._table(table)
+        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
         _vector("lens", lens, dev, torch.int32, n_seq)
         _vector("first", first, dev, torch.int32, n_seq + 1)
-        _rows("path", path, dev, torch.int32, n_seq, None)
+        _lines("path", path, dev, torch.int32, n_seq, None)
         _vector("n_keep", n_keep, dev, torch.int32, n_seq)
-        _call("sprinter_cache_keep", dev, self._ref, *self._arrays, *table_args, lens.data_ptr(), first.data_ptr(), path.data_ptr(), path.stride(0),
-              _int32("path's columns", path.shape[1]), n_keep.data_ptr())
-        _wrote(self.keys)
-        _wrote(self.values)
+        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(
+            n_seq, _int32("table's columns", n_table), _int32("path's columns", path.shape[1]), self.keys.data_ptr(), self.values.data_ptr(), *_line(table),
+            lens.data_ptr(), first.data_ptr(), *_line(path), n_keep.data_ptr()))
+        if self._counted:
+            _written(self._counted)
 
 
 def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=None, repetition=None, presence=None, frequency=None, draft=None,
@@ -447,32 +458,43 @@ def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=Non
     dev = _device(logits, "logits")
     if logits.dtype not in DTYPES:
         raise ValueError("logits: bfloat16 or float32 is needed")
-    _rows("logits", logits, dev, logits.dtype, None, None)
-    T, V = logits.shape
-    _int32("logits' columns", V)
-    f32, i32 = torch.float32, torch.int32
+    dtype, f32, i32 = logits.dtype, torch.float32, torch.int32
+    T, V = _lines("logits", logits, dev, dtype, None, None)
+    if V >= 2 ** 31:
+        _int32("logits' columns", V)
+    n_seq = T
     if first is not None:
-        n_seq, words = _trees(first, visible, dev, T)
-    else:
-        n_seq, words = T, _words(visible, dev, T)
+        n_seq = first.shape[0] - 1 if isinstance(first, torch.Tensor) and first.dim() == 1 else -1
+        if n_seq < 0:
+            raise ValueError("first: an int32 vector [n_seq + 1] is needed")
+        _vector("first", first, dev, i32, n_seq + 1)
+        if n_seq >= 2 ** 31:
+            _int32("n_seq", n_seq)
+    words = _words(visible, dev, T)
     n_tokens = n_bias = n_mask = 0
-    for name, t, dtype in (("n_token", n_token, i32), ("n_prompt", n_prompt, i32), ("repetition", repetition, f32), ("presence", presence, f32),
-                           ("frequency", frequency, f32)):
-        if t is not None:
-            _vector(name, t, dev, dtype, n_seq)
+    if n_token is not None:
+        _vector("n_token", n_token, dev, i32, n_seq)
+    if n_prompt is not None:
+        _vector("n_prompt", n_prompt, dev, i32, n_seq)
+    if repetition is not None:
+        _vector("repetition", repetition, dev, f32, n_seq)
+    if presence is not None:
+        _vector("presence", presence, dev, f32, n_seq)
+    if frequency is not None:
+        _vector("frequency", frequency, dev, f32, n_seq)
     if tokens is not None:
-        _rows("tokens", tokens, dev, i32, n_seq, None)
+        _lines("tokens", tokens, dev, i32, n_seq, None)
         n_tokens = _int32("tokens' columns", tokens.shape[1])
         if n_tokens == 0:                                # (no history: an empty tensor has no address)
             tokens = n_token = n_prompt = None
     if draft is not None:
         _vector("draft", draft, dev, i32, T)
     if bias is not None or bias_ids is not None:
-        _rows("bias_ids", bias_ids, dev, i32, n_seq, None)
+        _lines("bias_ids", bias_ids, dev, i32, n_seq, None)
         n_bias = _int32("bias' columns", bias_ids.shape[1])
-        _rows("bias", bias, dev, f32, n_seq, n_bias)
+        _lines("bias", bias, dev, f32, n_seq, n_bias)
     if mask is not None:
-        _rows("mask", mask, dev, i32, None, (V + 31) // 32)
+        _lines("mask", mask, dev, i32, None, (V + 31) // 32)
         n_mask = mask.shape[0]
     if mask_row is not None:
         _vector("mask_row", mask_row, dev, i32, T)
@@ -482,14 +504,13 @@ def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=Non
         mask = mask_row = None
     given = out is not None
     if given:
-        _rows("out", out, dev, logits.dtype, T, V)
+        _lines("out", out, dev, dtype, T, V)
     else:
-        out = torch.empty(T, V, dtype=logits.dtype, device=dev)
-    ld = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
-    a = LogitsC(DTYPES[logits.dtype], T, V, n_seq, logits.data_ptr(), logits.stride(0), out.data_ptr(), out.stride(0), _ptr(first), _ptr(tokens), ld(tokens),
-                _ptr(n_token), _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(draft), _ptr(visible), _ptr(bias_ids), ld(bias_ids),
-                _ptr(bias), ld(bias), _ptr(mask), ld(mask), _ptr(mask_row), n_tokens, words, n_bias, n_mask)
-    _call("sprinter_adjust_logits", dev, C.byref(a))
+        out = torch.empty((T, V), dtype=dtype, device=dev)
+    _call("sprinter_adjust_logits", dev, _LOGITS.pack(
+        DTYPES[dtype], T, V, n_seq, *_line(logits), *_line(out), _address(first), *_line(tokens), _address(n_token), _address(n_prompt), _address(repetition),
+        _address(presence), _address(frequency), _address(draft), _address(visible), *_line(bias_ids), *_line(bias), *_line(mask), _address(mask_row),
+        n_tokens, words, n_bias, n_mask))
     if given:
         _wrote(out)
     return out

@@ -20,36 +20,54 @@ def _cfg(**kw):
     return C.byref(ops.CacheCfgC(*{**CFG, **kw}.values()))
 
 
-def _append(lib, cfg=None, **kw):  # noqa: F811
-    v = dict(layer=0, keys=A, values=A, table=A, ldt=4, n_seq=3, n_table=4, seq=A, slot=A, pos=None, freq=A, n=64, pairs=0, type=1, k=A, ldk=128,
-             v=A, ldv=128, q=A, ldq=256, H=4, T=5, qo=A, ldqo=256)
-    return lib.sprinter_cache_append(cfg or _cfg(), *{**v, **kw}.values(), None)
-
-
-def _attend(lib, cfg=None, **kw):  # noqa: F811
-    v = dict(layer=0, keys=A, values=A, table=A, ldt=4, n_seq=3, n_table=4, lens=A, first=A, vis=A, words=1, H=4, scale=0.125, q=A, ldq=256, T=5, y=A,
-             ldy=256, work=A, bytes=1 << 40)
-    return lib.sprinter_cache_attend(cfg or _cfg(), *{**v, **kw}.values(), None)
-
-
-def _keep(lib, cfg=None, **kw):  # noqa: F811
-    v = dict(keys=A, values=A, table=A, ldt=4, n_seq=3, n_table=4, lens=A, first=A, path=A, ldp=4, n_path=4, n_keep=A)
-    return lib.sprinter_cache_keep(cfg or _cfg(), *{**v, **kw}.values(), None)
-
-
+APPEND = dict(layer=0, n_seq=3, n_table=4, T=5, keys=A, values=A, table=A, ldt=4, seq=A, slot=A, pos=None, freq=A, k=A, ldk=128, v=A, ldv=128, q=A, ldq=256, qo=A,
+              ldqo=256, H=4, n=64, pairs=0, type=1)
+ATTEND = dict(layer=0, n_seq=3, n_table=4, T=5, keys=A, values=A, table=A, ldt=4, lens=A, first=A, vis=A, q=A, ldq=256, y=A, ldy=256, work=A, bytes=1 << 40, words=1, H=4,
+              scale=0.125)
+KEEP = dict(n_seq=3, n_table=4, n_path=4, keys=A, values=A, table=A, ldt=4, lens=A, first=A, path=A, ldp=4, n_keep=A)
 LOGITS = dict(dtype=0, n_rows=3, vocab=100, n_seq=3, logits=A, ld_logits=100, out=A, ld_out=100, first=A, tokens=A, ld_tokens=50, n_token=A, n_prompt=A,
               repetition=A, presence=A, frequency=A, draft=A, visible=A, bias_ids=A, ld_bias_ids=8, bias=A, ld_bias=8, mask=A, ld_mask=4, mask_row=A,
               n_tokens=50, n_words=1, n_bias=8, n_mask=2)
 
 
+def _packed(layout, good, kw):
+    assert not set(kw) - set(good)
+    return layout.pack(*(0 if v is None else v for v in {**good, **kw}.values()))
+
+
+def _append(lib, cfg=None, **kw):  # noqa: F811
+    return lib.sprinter_cache_append(cfg or _cfg(), _packed(ops._APPEND, APPEND, kw), None)
+
+
+def _attend(lib, cfg=None, **kw):  # noqa: F811
+    return lib.sprinter_cache_attend(cfg or _cfg(), _packed(ops._ATTEND, ATTEND, kw), None)
+
+
+def _keep(lib, cfg=None, **kw):  # noqa: F811
+    return lib.sprinter_cache_keep(cfg or _cfg(), _packed(ops._KEEP, KEEP, kw), None)
+
+
 def _logits(lib, **kw):  # noqa: F811
-    return lib.sprinter_adjust_logits(C.byref(ops.LogitsC(*{**LOGITS, **kw}.values())), None)
+    return lib.sprinter_adjust_logits(_packed(ops._LOGITS, LOGITS, kw), None)
 
 
 def test_layouts():
+    """The structs as sprinter.h has them (their sizes are asserted where the library is compiled), field by field."""
+    import os
+    import re
     assert C.sizeof(ops.CacheCfgC) == 24
-    assert C.sizeof(ops.LogitsC) == 16 + 21 * 8 + 16 and ops.LogitsC.n_tokens.offset == 16 + 21 * 8
-    assert tuple(LOGITS) == tuple(n for n, _ in ops.LogitsC._fields_)
+    hdr = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "sprinter.h")).read()
+    for name, layout, size in (("append", ops._APPEND, 160), ("attend", ops._ATTEND, 136), ("keep", ops._KEEP, 88), ("logits", ops._LOGITS, 200)):
+        body = re.search(r"typedef struct \{([^}]*)\} sprinter_%s;" % name, hdr).group(1)
+        codes = ""
+        for line in body.split(";"):
+            words = line.replace("const ", "").split()
+            if not words:
+                continue
+            kind, names = words[0], " ".join(words[1:]).split(",")
+            codes += "".join("P" if "*" in n or kind.endswith("*") else {"int32_t": "i", "int64_t": "q", "uint64_t": "Q", "float": "f"}[kind] for n in names)
+        given = re.sub(r"(\d+)(\w)", lambda m: m.group(2) * int(m.group(1)), layout.format.replace(" ", ""))
+        assert given == codes and layout.size == size, (name, given, codes, layout.size)
 
 
 @pytest.mark.parametrize("change, word", [(dict(dtype=2), "dtype"), (dict(n_layer=0), "n_layer"), (dict(n_page=0), "n_page"), (dict(page_size=4), "page_size"),
@@ -84,7 +102,10 @@ def test_what_all_calls_on_a_cache_refuse(lib):  # noqa: F811
         for H in (3, 5, -2, 4098):
             _refused(lib, call(lib, H=H), RANGE, "n_head")
         assert call(lib, T=0) == 0
-    _refused(lib, lib.sprinter_cache_append(None, 0, *[None] * 3, 0, 0, 0, *[None] * 4, 0, 0, 0, None, 0, None, 0, None, 0, 0, 0, None, 0, None), NULL, "configuration")
+    for name, layout, good in (("append", ops._APPEND, APPEND), ("attend", ops._ATTEND, ATTEND), ("keep", ops._KEEP, KEEP)):
+        call = getattr(lib, "sprinter_cache_" + name)
+        _refused(lib, call(None, _packed(layout, good, {}), None), NULL, "configuration")
+        _refused(lib, call(_cfg(), None, None), NULL, "arguments")
 
 
 def test_append_arguments(lib):  # noqa: F811
@@ -115,6 +136,7 @@ def test_attend_arguments(lib):  # noqa: F811
         _refused(lib, _attend(lib, **{name: 260}), RANGE, "16-byte")
     for name in ("q", "y"):
         _refused(lib, _attend(lib, **{name: A + 8}), RANGE, "16-byte")
+    _refused(lib, _attend(lib, T=1 << 20, H=16, ldq=1024, ldy=1024), RANGE, "2^23")
     for name, by in (("lens", 2), ("first", 2), ("vis", 4)):
         _refused(lib, _attend(lib, **{name: A + by}), RANGE, "aligned")
     _refused(lib, _attend(lib, work=A + 128), WORKSPACE, "256-byte")
