@@ -7,6 +7,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsprinter.so")
+TENSORS = os.path.join(PKG, "_tensors.so")
 NATIVE_BENCH = os.path.join(PKG, "native_bench")
 SOURCES = ["k_norm.hip", "k_gemm.hip", "k_gemm_norm.hip", "k_gemm_tile.hip", "k_attn.hip", "k_lmhead.hip", "k_control.hip", "k_sd.hip", "k_route.hip", "k_experts.hip", "k_experts_tile.hip",
            "k_block_norm.hip", "k_cache.hip", "k_tree_attn.hip", "k_logits.hip", "ops.cpp", "abi.cpp"]
@@ -30,6 +31,16 @@ def _run(cmd, verbose):
         raise RuntimeError("hipcc failed:\n" + out)
 
 
+def build_tensors(verbose: bool = True) -> None:
+    """The Python extension that looks tensors over for the operators (csrc/tensors.cpp; host code only)."""
+    import sysconfig
+    from torch.utils import cpp_extension
+    import torch
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          *("-isystem" + p for p in cpp_extension.include_paths()), "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "tensors.cpp"), "-o", TENSORS,
+          *("-L" + p for p in cpp_extension.library_paths()), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+
+
 def build_library(verbose: bool = True) -> str:
     """Every source is compiled (in parallel) on each call, then linked into the shared library."""
     from concurrent.futures import ThreadPoolExecutor
@@ -37,8 +48,10 @@ def build_library(verbose: bool = True) -> str:
     os.makedirs(objdir, exist_ok=True)
     objs = [os.path.join(objdir, s + ".o") for s in SOURCES]
     cmds = [["hipcc", *FLAGS, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
+    with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
+        tensors = ex.submit(build_tensors, verbose)
         list(ex.map(lambda c: _run(c, verbose), cmds))
+        tensors.result()
     _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], verbose)
     # the Python-free runner of dumped workloads (hardware-counter runs); it only uses the public C ABI
     _run(["hipcc", *FLAGS, "-x", "hip", os.path.join(CSRC, "native_bench.cpp"), "-L" + PKG, "-lsprinter",

@@ -269,55 +269,58 @@ class CacheCfgC(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_layer", "n_page", "page_size", "n_kv_head", "d_head")]
 
 
-def _vector(name, t, device, dtype, n):
-    """A contiguous vector of n elements (the checks in the order of their cost first, then the words for what fails one)."""
-    if isinstance(t, Tensor) and t.dtype is dtype and t.device == device and t.shape == (n,) and t.is_contiguous() and not (t.requires_grad or t.is_neg()) and \
-            forward_ad._current_level < 0:
-        return
-    _tensor(name, t, device, dtype)
-    if t.shape != (n,):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{n}]")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+_native = None
 
 
-def _lines(name, t, device, dtype, rows, cols):
-    """`_rows` -> its shape, for what it mostly gets: the checks in the order of their cost first, then the other's words for what fails one."""
-    if isinstance(t, Tensor) and t.dtype is dtype and t.device == device and len(shape := t.shape) == 2:
-        n, m = shape
-        if (rows is None or rows == n) and (cols is None or cols == m) and t.is_contiguous() and not (t.requires_grad or t.is_neg()) and n < 2 ** 31 and \
-                forward_ad._current_level < 0:
-            return shape
-    _rows(name, t, device, dtype, rows, cols)
-    return t.shape
+def _asks():
+    """The extension that looks tensors over (csrc/tensors.cpp).  Raises if it is not built."""
+    global _native
+    if _native is None:
+        try:
+            from . import _tensors
+        except ImportError as e:
+            raise RuntimeError("paper_2502_04557_amd/_tensors.so not found: build it first (python -m paper_2502_04557_amd.build)") from e
+        _native = _tensors
+    return _native
+
+
+def _no(*args):
+    return None
+
+
+def _looks():
+    """Its (rows, vector); inside a level of forward mode, whose tangents it does not see, everything takes the checks in Python."""
+    n = _native or _asks()
+    return (n.rows, n.vector) if forward_ad._current_level < 0 else (_no, _no)
+
+
+# What those say None of: the checks in Python, which raise, or let the uncommon (an empty tensor, one that asks for gradients where they are off) pass.
+def _matrix(name, t, device, dtype, rows, cols):
+    _rows(name, t, device, dtype, None if rows < 0 else rows, None if cols < 0 else cols)
+    for what, n in zip(("rows", "columns"), t.shape):
+        _int32(f"{name}'s {what}", n)
+    return (t.data_ptr(), t.stride(0), *t.shape)
+
+
+def _column(name, t, device, dtype, n):
+    _whole(name, t, device, dtype, n)
+    return t.data_ptr()
 
 
 def _layer(v):
     return v if type(v) is int and 0 <= v < 65536 else _int32("layer", v)
 
 
-def _words(visible, device, rows):
-    """The words of a row of `visible`."""
+def _words(rows, visible, device, n):
+    """The address of `visible` and the words of its rows."""
     if visible is None:
-        return 0
-    words = visible.shape[1] if isinstance(visible, torch.Tensor) and visible.dim() == 2 else 0
-    _whole("visible", visible, device, torch.int64, rows, max(1, words))
-    return words
-
-
-def _address(t):
-    return 0 if t is None else t.data_ptr()
-
-
-def _line(t):
-    """The address of a matrix and how far apart its rows lie."""
-    return (0, 0) if t is None else (t.data_ptr(), t.stride(0))
-
-
-def _wrote(t):
-    """A tensor that is written in place; one of inference mode counts no versions."""
-    if not t.is_inference():
-        _written(t)
+        return 0, 0
+    at, ld, _, words = rows(visible, device, torch.int64, n, -1) or (0, -1, 0, 0)
+    if ld != words or words < 1:
+        words = visible.shape[1] if isinstance(visible, Tensor) and visible.dim() == 2 else 0
+        _whole("visible", visible, device, torch.int64, n, max(1, words))
+        at = visible.data_ptr()
+    return at, words
 
 
 class PagedCache:
@@ -341,7 +344,6 @@ class PagedCache:
         self.n_layer, self.n_page, self.n_kv_head, self.page_size, self.d_head = shape
         self._cfg = CacheCfgC(DTYPES[keys.dtype], *(_int32("keys' sizes", shape[i]) for i in (0, 1, 3, 2, 4)))
         self._ref = C.byref(self._cfg)
-        self._counted = tuple(t for t in (keys, values) if not t.is_inference())   # (tensors of inference mode count no versions)
         self._need = {}
 
     def append(self, layer, keys, values, table, seq, slot, *, q=None, pos=None, freq=None, pairs="halves", q_out=None):
@@ -350,70 +352,71 @@ class PagedCache:
         With freq (float64 [n / 2]) the first n columns of each head of the keys and of q [T, n_head * d_head] are turned by the angles pos[t] * freq (pos int32
         [T], by default the slot), in the pairs (i, i + n / 2) ("halves") or (2 i, 2 i + 1) ("neighbours").  Rows are bfloat16 or float32, all of one
         type; what is written has the cache's.  A token of no sequence (-1) is padding.  q_out: where the turned q goes (q itself turns it in place)."""
-        dev, d = self.device, self.d_head
-        if not isinstance(keys, torch.Tensor) or keys.dtype not in DTYPES:
+        dev, d, i32 = self.device, self.d_head, torch.int32
+        rows, vector = _looks()
+        dtype = keys.dtype if isinstance(keys, Tensor) else None
+        if dtype not in DTYPES:
             raise ValueError("keys: bfloat16 or float32 rows are needed")
-        width, dtype = self.n_kv_head * d, keys.dtype
-        T, _ = _lines("keys", keys, dev, dtype, None, width)
-        _lines("values", values, dev, dtype, T, width)
-        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
-        _vector("seq", seq, dev, torch.int32, T)
-        _vector("slot", slot, dev, torch.int32, T)
-        if pos is not None:
-            _vector("pos", pos, dev, torch.int32, T)
-        n = 0
+        width = self.n_kv_head * d
+        k, ld_k, T, _ = rows(keys, dev, dtype, -1, width) or _matrix("keys", keys, dev, dtype, -1, width)
+        v, ld_v, _, _ = rows(values, dev, dtype, T, width) or _matrix("values", values, dev, dtype, T, width)
+        tab, ld_tab, n_seq, n_table = rows(table, dev, i32, -1, -1) or _matrix("table", table, dev, i32, -1, -1)
+        seq_at = vector(seq, dev, i32, T) or _column("seq", seq, dev, i32, T)
+        slot_at = vector(slot, dev, i32, T) or _column("slot", slot, dev, i32, T)
+        pos_at = 0 if pos is None else vector(pos, dev, i32, T) or _column("pos", pos, dev, i32, T)
+        n = freq_at = 0
         if freq is not None:
-            n = freq.shape[0] if isinstance(freq, torch.Tensor) and freq.dim() == 1 else 0
-            _vector("freq", freq, dev, torch.float64, n)
+            n = freq.shape[0] if isinstance(freq, Tensor) and freq.dim() == 1 else 0
+            freq_at = vector(freq, dev, torch.float64, n) or _column("freq", freq, dev, torch.float64, n)
         if pairs not in PAIRS:
             raise ValueError(f"pairs is one of {tuple(PAIRS)}")
-        H, given = 0, q_out is not None
+        H = q_at = ld_q = to = ld_to = 0
+        given = q_out is not None
         if q is not None:
-            _, wide = _lines("q", q, dev, dtype, T, None)
+            q_at, ld_q, _, wide = rows(q, dev, dtype, T, -1) or _matrix("q", q, dev, dtype, T, -1)
             H = wide // d
             if H < 1 or wide != H * d:
                 raise ValueError(f"q: {wide} columns are no heads of {d}")
-            if given:
-                _lines("q_out", q_out, dev, self.dtype, T, wide)
-            else:
-                q_out = torch.empty((T, wide), dtype=self.dtype, device=dev)
+            if not given:
+                q_out = _native.empty(T, wide, self.dtype, dev)
+            to, ld_to, _, _ = rows(q_out, dev, self.dtype, T, wide) or _matrix("q_out", q_out, dev, self.dtype, T, wide)
         elif given:
             raise ValueError("q_out: there is no q")
         _call("sprinter_cache_append", dev, self._ref, _APPEND.pack(
-            _layer(layer), n_seq, _int32("table's columns", n_table), T, self.keys.data_ptr(), self.values.data_ptr(), *_line(table), seq.data_ptr(), slot.data_ptr(),
-            _address(pos), _address(freq), *_line(keys), *_line(values), *_line(q), *_line(q_out), H, 2 * n, PAIRS[pairs], DTYPES[dtype]))
-        if self._counted:
-            _written(self._counted)
+            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, seq_at, slot_at, pos_at, freq_at, k, ld_k, v, ld_v, q_at, ld_q,
+            to, ld_to, H, 2 * n, PAIRS[pairs], DTYPES[dtype]))
         if given:
-            _wrote(q_out)
+            _native.written(self.keys, self.values, q_out)
+        else:
+            _native.written(self.keys, self.values)
         return q_out
 
     def attend(self, layer, q, table, lens, first, *, visible=None, scale=None, out=None):
         """q [T, n_head * d_head] of the cache's type -> y [T, n_head * d_head]: each node attends to the committed slots and to the nodes that it
         sees (sprinter_cache_attend).  scale: of the scores, by default d_head ** -0.5.  A row that sees nothing gives zeros; rows of no
         sequence are not written."""
-        dev = self.device
-        T, width = _lines("q", q, dev, self.dtype, None, None)
+        dev, dtype, i32 = self.device, self.dtype, torch.int32
+        rows, vector = _looks()
+        q_at, ld_q, T, width = rows(q, dev, dtype, -1, -1) or _matrix("q", q, dev, dtype, -1, -1)
         H = width // self.d_head
         if H < 1 or width != H * self.d_head:
             raise ValueError(f"q: {width} columns are no heads of {self.d_head}")
-        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
-        _vector("lens", lens, dev, torch.int32, n_seq)
-        _vector("first", first, dev, torch.int32, n_seq + 1)
-        words = _words(visible, dev, T)
+        tab, ld_tab, n_seq, n_table = rows(table, dev, i32, -1, -1) or _matrix("table", table, dev, i32, -1, -1)
+        lens_at = vector(lens, dev, i32, n_seq) or _column("lens", lens, dev, i32, n_seq)
+        first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
+        seen, words = _words(rows, visible, dev, T)
         given = out is not None
-        if given:
-            _lines("out", out, dev, self.dtype, T, width)
-        else:
-            out = torch.empty((T, width), dtype=self.dtype, device=dev)
+        if not given:
+            out = _native.empty(T, width, dtype, dev)
+        to, ld_to, _, _ = rows(out, dev, dtype, T, width) or _matrix("out", out, dev, dtype, T, width)
         scale = self.d_head ** -0.5 if scale is None else float(_number("scale", scale))
         need = self._workspace(H, n_seq, n_table, T)
-        work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        work = _native.empty(1, need, torch.uint8, dev) if need else None
         _call("sprinter_cache_attend", dev, self._ref, _ATTEND.pack(
-            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), *_line(table), lens.data_ptr(), first.data_ptr(), _address(visible),
-            *_line(q), *_line(out), _address(work), need, words, H, scale))
+            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, lens_at, first_at, seen, q_at, ld_q, to, ld_to,
+            0 if work is None else work.data_ptr(), need, words, H, scale))
         if given:
-            _wrote(out)
+            _native.written(out)
         return out
 
     def _workspace(self, H, n_seq, n_table, T):
@@ -431,17 +434,16 @@ class PagedCache:
     def keep(self, table, lens, first, path, n_keep):
         """Slot lens[b] + path[b, j] -> slot lens[b] + j in every layer, j < n_keep[b] (path int32 [n_seq, n], nodes in ascending order; n_keep int32
         [n_seq]): the accepted nodes become the next committed slots (sprinter_cache_keep).  lens is the caller's to advance."""
-        dev = self.device
-        n_seq, n_table = _lines("table", table, dev, torch.int32, None, None)
-        _vector("lens", lens, dev, torch.int32, n_seq)
-        _vector("first", first, dev, torch.int32, n_seq + 1)
-        _lines("path", path, dev, torch.int32, n_seq, None)
-        _vector("n_keep", n_keep, dev, torch.int32, n_seq)
-        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(
-            n_seq, _int32("table's columns", n_table), _int32("path's columns", path.shape[1]), self.keys.data_ptr(), self.values.data_ptr(), *_line(table),
-            lens.data_ptr(), first.data_ptr(), *_line(path), n_keep.data_ptr()))
-        if self._counted:
-            _written(self._counted)
+        dev, i32 = self.device, torch.int32
+        rows, vector = _looks()
+        tab, ld_tab, n_seq, n_table = rows(table, dev, i32, -1, -1) or _matrix("table", table, dev, i32, -1, -1)
+        lens_at = vector(lens, dev, i32, n_seq) or _column("lens", lens, dev, i32, n_seq)
+        first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
+        path_at, ld_path, _, n_path = rows(path, dev, i32, n_seq, -1) or _matrix("path", path, dev, i32, n_seq, -1)
+        keep_at = vector(n_keep, dev, i32, n_seq) or _column("n_keep", n_keep, dev, i32, n_seq)
+        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(n_seq, n_table, n_path, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, lens_at, first_at,
+                                                                path_at, ld_path, keep_at))
+        _native.written(self.keys, self.values)
 
 
 def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=None, repetition=None, presence=None, frequency=None, draft=None,
@@ -459,58 +461,43 @@ def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=Non
     if logits.dtype not in DTYPES:
         raise ValueError("logits: bfloat16 or float32 is needed")
     dtype, f32, i32 = logits.dtype, torch.float32, torch.int32
-    T, V = _lines("logits", logits, dev, dtype, None, None)
-    if V >= 2 ** 31:
-        _int32("logits' columns", V)
-    n_seq = T
+    rows, vector = _looks()
+    at, ld, T, V = rows(logits, dev, dtype, -1, -1) or _matrix("logits", logits, dev, dtype, -1, -1)
+    n_seq, first_at = T, 0
     if first is not None:
-        n_seq = first.shape[0] - 1 if isinstance(first, torch.Tensor) and first.dim() == 1 else -1
+        n_seq = first.shape[0] - 1 if isinstance(first, Tensor) and first.dim() == 1 else -1
         if n_seq < 0:
             raise ValueError("first: an int32 vector [n_seq + 1] is needed")
-        _vector("first", first, dev, i32, n_seq + 1)
-        if n_seq >= 2 ** 31:
-            _int32("n_seq", n_seq)
-    words = _words(visible, dev, T)
-    n_tokens = n_bias = n_mask = 0
-    if n_token is not None:
-        _vector("n_token", n_token, dev, i32, n_seq)
-    if n_prompt is not None:
-        _vector("n_prompt", n_prompt, dev, i32, n_seq)
-    if repetition is not None:
-        _vector("repetition", repetition, dev, f32, n_seq)
-    if presence is not None:
-        _vector("presence", presence, dev, f32, n_seq)
-    if frequency is not None:
-        _vector("frequency", frequency, dev, f32, n_seq)
+        first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
+    seen, words = _words(rows, visible, dev, T)
+    many = 0 if n_token is None else vector(n_token, dev, i32, n_seq) or _column("n_token", n_token, dev, i32, n_seq)
+    asked = 0 if n_prompt is None else vector(n_prompt, dev, i32, n_seq) or _column("n_prompt", n_prompt, dev, i32, n_seq)
+    rep = 0 if repetition is None else vector(repetition, dev, f32, n_seq) or _column("repetition", repetition, dev, f32, n_seq)
+    pre = 0 if presence is None else vector(presence, dev, f32, n_seq) or _column("presence", presence, dev, f32, n_seq)
+    frq = 0 if frequency is None else vector(frequency, dev, f32, n_seq) or _column("frequency", frequency, dev, f32, n_seq)
+    drafted = 0 if draft is None else vector(draft, dev, i32, T) or _column("draft", draft, dev, i32, T)
+    row = 0 if mask_row is None else vector(mask_row, dev, i32, T) or _column("mask_row", mask_row, dev, i32, T)
+    tok = ld_tok = n_tokens = ids = ld_ids = add = ld_add = n_bias = bits = ld_bits = n_mask = 0
     if tokens is not None:
-        _lines("tokens", tokens, dev, i32, n_seq, None)
-        n_tokens = _int32("tokens' columns", tokens.shape[1])
+        tok, ld_tok, _, n_tokens = rows(tokens, dev, i32, n_seq, -1) or _matrix("tokens", tokens, dev, i32, n_seq, -1)
         if n_tokens == 0:                                # (no history: an empty tensor has no address)
-            tokens = n_token = n_prompt = None
-    if draft is not None:
-        _vector("draft", draft, dev, i32, T)
+            tok = many = asked = 0
     if bias is not None or bias_ids is not None:
-        _lines("bias_ids", bias_ids, dev, i32, n_seq, None)
-        n_bias = _int32("bias' columns", bias_ids.shape[1])
-        _lines("bias", bias, dev, f32, n_seq, n_bias)
+        ids, ld_ids, _, n_bias = rows(bias_ids, dev, i32, n_seq, -1) or _matrix("bias_ids", bias_ids, dev, i32, n_seq, -1)
+        add, ld_add, _, _ = rows(bias, dev, f32, n_seq, n_bias) or _matrix("bias", bias, dev, f32, n_seq, n_bias)
     if mask is not None:
-        _lines("mask", mask, dev, i32, None, (V + 31) // 32)
-        n_mask = mask.shape[0]
-    if mask_row is not None:
-        _vector("mask_row", mask_row, dev, i32, T)
-    if mask is not None and n_mask == 0:
-        if mask_row is None and T > 0:
-            raise ValueError(f"mask: {T} rows without mask_row, and no masks")
-        mask = mask_row = None
+        bits, ld_bits, n_mask, _ = rows(mask, dev, i32, -1, (V + 31) // 32) or _matrix("mask", mask, dev, i32, -1, (V + 31) // 32)
+        if n_mask == 0:
+            if mask_row is None and T > 0:
+                raise ValueError(f"mask: {T} rows without mask_row, and no masks")
+            bits = row = 0
     given = out is not None
-    if given:
-        _lines("out", out, dev, dtype, T, V)
-    else:
-        out = torch.empty((T, V), dtype=dtype, device=dev)
+    if not given:
+        out = _native.empty(T, V, dtype, dev)
+    to, ld_to, _, _ = rows(out, dev, dtype, T, V) or _matrix("out", out, dev, dtype, T, V)
     _call("sprinter_adjust_logits", dev, _LOGITS.pack(
-        DTYPES[dtype], T, V, n_seq, *_line(logits), *_line(out), _address(first), *_line(tokens), _address(n_token), _address(n_prompt), _address(repetition),
-        _address(presence), _address(frequency), _address(draft), _address(visible), *_line(bias_ids), *_line(bias), *_line(mask), _address(mask_row),
+        DTYPES[dtype], T, V, n_seq, at, ld, to, ld_to, first_at, tok, ld_tok, many, asked, rep, pre, frq, drafted, seen, ids, ld_ids, add, ld_add, bits, ld_bits, row,
         n_tokens, words, n_bias, n_mask))
     if given:
-        _wrote(out)
+        _native.written(out)
     return out
