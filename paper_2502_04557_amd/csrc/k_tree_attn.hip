@@ -805,29 +805,30 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
   for (int r = it.part + it.parts * wave_index(); r < rows; r += it.parts * 4) {
     auto at = [&](int part) { return ((long long)(first + part) * a.c.KVH + kvh) * QB + r; };
     float2 ml = lane < parts ? *reinterpret_cast<const float2*>(plan.ml + at(lane) * 2) : make_float2(LOW, 0.f);
+    constexpr int U = 16;                          // shares whose loads leave together, the first of them with their statistics'
+    float v[U][N];
+    auto fetch = [&](int x) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[u][e] = plan.o[at(min(x + u, parts - 1)) * DH + lane * N + e];
+    };
+    fetch(0);
     float m = ml.x, l = 0.f, o[N] = {};
     for (int x = lane + 64; x < parts; x += 64) m = fmaxf(m, plan.ml[at(x) * 2]);
     m = wave_max(m);
     for (int x0 = 0; x0 < parts; x0 += 64) {
       if (x0) ml = x0 + lane < parts ? *reinterpret_cast<const float2*>(plan.ml + at(x0 + lane) * 2) : make_float2(LOW, 0.f);
-      const float f = __builtin_amdgcn_exp2f(ml.x - m);
+      const float f = x0 + lane < parts ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
       l += wave_sum(ml.y * f);
-      const int here = min(parts - x0, 64);
-      int x = 0;
-      for (; x + 4 <= here; x += 4) {              // (four shares' loads at a time)
-        float v[4][N];
+      for (int x = x0; x < min(parts, x0 + 64); x += U) {
+        if (x) fetch(x);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < U; ++u)
+          if (x + u < parts)                       // (scalar)
 #pragma unroll
-          for (int e = 0; e < N; ++e) v[u][e] = plan.o[at(x0 + x + u) * DH + lane * N + e];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int e = 0; e < N; ++e) o[e] += v[u][e] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x + u));
+            for (int e = 0; e < N; ++e) o[e] += v[u][e] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), (x + u) & 63));
       }
-      for (; x < here; ++x)
-#pragma unroll
-        for (int e = 0; e < N; ++e) o[e] += plan.o[at(x0 + x) * DH + lane * N + e] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x));
     }
     const long long i = (long long)it.block * QB + r;
     T* y = (T*)a.y + (it.f0 + i / G) * a.ld_y + (kvh * G + i % G) * DH + lane * N;
