@@ -534,7 +534,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   auto slots_of = [&](const void* array, int page) {   // (page 0 where the page is not there: read, not used)
     return (u64)array + (((u64)(ok(page) ? page : 0) * a.c.KVH + kvh) << shift) * (2 * DH);
   };
-  int e0 = k0 >> shift, now = table[min(e0 + lane, last)], then = table[min(e0 + 64 + lane, last)];
+  int e0 = k0 >> shift, now = -1, then = -1;
+  if (n_blk > 0) {                                 // (a table without columns is not read)
+    now = table[min(e0 + lane, last)];
+    then = table[min(e0 + 64 + lane, last)];
+  }
   u64 at_now = 0, ok_now = 0, ok_before = 0;       // ok: which of these, and of the 64 before them, are pages
   // A lane's 16 bytes of each of its pieces: whole rows of DH columns, from group `lane_g` of 8 keys of the block on, and the offset if all of the block lay in
   // one page.  A row's 16-byte pieces (keys) or 32-byte ones (values) lie where an exclusive-or with its number puts them.

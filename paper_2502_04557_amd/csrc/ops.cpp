@@ -238,7 +238,7 @@ int sprinter_cache_attend(const sprinter_cache_cfg* cfg, const sprinter_attend* 
   if (rc || (rc = check_heads(cfg, x.n_head, who)) || (rc = check_attended(x.n_rows, x.n_head, who))) return rc;
   if (x.visible && (x.n_words < 1 || x.n_words > MAX_NODE_WORDS))
     return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, x.n_words, MAX_NODE_WORDS);
-  if (!(x.scale - x.scale == 0.f)) return op_fail(SPRINTER_E_CONFIG, "%s: scale is not finite", who);
+  if (!(x.scale * 2.f - x.scale * 2.f == 0.f)) return op_fail(SPRINTER_E_CONFIG, "%s: scale is not finite, or too large", who);
   if (x.n_rows == 0 || x.n_seq == 0) return SPRINTER_OK;
   if (!x.len || !x.first || !x.q || !x.y) return op_fail(SPRINTER_E_NULL, "%s: NULL array", who);
   const int w = x.n_head * cfg->d_head;

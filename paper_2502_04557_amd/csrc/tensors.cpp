@@ -15,7 +15,7 @@ const at::Tensor* plain(PyObject* o, PyObject* device, PyObject* dtype) {
   if (!THPVariable_Check(o) || !THPDevice_Check(device) || !THPDtype_Check(dtype)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || t.layout() != at::kStrided || t.scalar_type() != ((THPDtype*)dtype)->scalar_type || t.device() != ((THPDevice*)device)->device ||
-      t.is_neg() || t.is_conj() || t.requires_grad())
+      t.is_neg() || t.is_conj() || t._is_zerotensor() || t.requires_grad())
     return nullptr;
   return &t;
 }
@@ -30,7 +30,7 @@ PyObject* vector(PyObject*, PyObject* const* a, Py_ssize_t n) {
   try {
     const at::Tensor* t = plain(a[0], a[1], a[2]);
     if (!t || t->dim() != 1 || t->size(0) != want || !t->is_contiguous()) return none();
-    return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t->const_data_ptr());
+    return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t->data_ptr());
   } catch (const std::exception&) {
     return none();
   }
@@ -47,7 +47,7 @@ PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const long long r = t->size(0), c = t->size(1);
     if ((want_rows >= 0 && r != want_rows) || (want_cols >= 0 && c != want_cols) || r >= 1ll << 31 || c >= 1ll << 31) return none();
     if (c > 1 && t->stride(1) != 1) return none();
-    return Py_BuildValue("KLLL", (unsigned long long)(uintptr_t)t->const_data_ptr(), (long long)t->stride(0), r, c);
+    return Py_BuildValue("KLLL", (unsigned long long)(uintptr_t)t->data_ptr(), (long long)t->stride(0), r, c);
   } catch (const std::exception&) {
     return none();
   }

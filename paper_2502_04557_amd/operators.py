@@ -299,12 +299,19 @@ def _matrix(name, t, device, dtype, rows, cols):
     _rows(name, t, device, dtype, None if rows < 0 else rows, None if cols < 0 else cols)
     for what, n in zip(("rows", "columns"), t.shape):
         _int32(f"{name}'s {what}", n)
-    return (t.data_ptr(), t.stride(0), *t.shape)
+    return (_memory(name, t), t.stride(0), *t.shape)
 
 
 def _column(name, t, device, dtype, n):
     _whole(name, t, device, dtype, n)
-    return t.data_ptr()
+    return _memory(name, t)
+
+
+def _memory(name, t):
+    at = t.data_ptr()
+    if at == 0 and t.numel() > 0:                        # (no address would stand for no tensor)
+        raise ValueError(f"{name}: a tensor without memory")
+    return at
 
 
 def _layer(v):
@@ -319,7 +326,7 @@ def _words(rows, visible, device, n):
     if ld != words or words < 1:
         words = visible.shape[1] if isinstance(visible, Tensor) and visible.dim() == 2 else 0
         _whole("visible", visible, device, torch.int64, n, max(1, words))
-        at = visible.data_ptr()
+        at = _memory("visible", visible)
     return at, words
 
 
@@ -327,7 +334,8 @@ class PagedCache:
     """A cache in pages on two tensors of the caller's: keys, values [n_layer, n_page, n_kv_head, page_size, d_head], bfloat16 or float32.
 
     Slot s of sequence b is place s % page_size of page table[b, s // page_size] (table int32 [n_seq, n], entries outside the cache: no page).  page_size is a
-    power of two in [8, 1024], d_head 64 or 128.  The tensors are written in place; the object keeps no state beside them.
+    power of two in [8, 1024], d_head 64 or 128.  The tensors are written in place; the object keeps no state beside them.  Rows that `attend` reads and writes are
+    16-byte aligned.
 
     A batch of trees: sequence b has lens[b] committed slots and the rows first[b] .. first[b + 1] - 1 as its drafted nodes (lens int32 [n_seq], first int32
     [n_seq + 1]), node i in slot lens[b] + i.  visible int64 [T, words]: bit j % 64 of word j // 64 says whether a row sees node j of its sequence,
@@ -340,11 +348,19 @@ class PagedCache:
         shape = tuple(keys.shape)
         for name, t in (("keys", keys), ("values", values)):
             _whole(name, t, dev, keys.dtype, *shape)
-        self.keys, self.values, self.device, self.dtype = keys, values, dev, keys.dtype
+        self._keys, self._values, self.device, self.dtype = keys, values, dev, keys.dtype
         self.n_layer, self.n_page, self.n_kv_head, self.page_size, self.d_head = shape
         self._cfg = CacheCfgC(DTYPES[keys.dtype], *(_int32("keys' sizes", shape[i]) for i in (0, 1, 3, 2, 4)))
         self._ref = C.byref(self._cfg)
         self._need = {}
+
+    @property
+    def keys(self):
+        return self._keys
+
+    @property
+    def values(self):
+        return self._values
 
     def append(self, layer, keys, values, table, seq, slot, *, q=None, pos=None, freq=None, pairs="halves", q_out=None):
         """Writes the rows keys, values [T, n_kv_head * d_head] to slot[t] of sequence seq[t] (both int32 [T]); -> q turned, or None (sprinter_cache_append).
@@ -383,12 +399,12 @@ class PagedCache:
         elif given:
             raise ValueError("q_out: there is no q")
         _call("sprinter_cache_append", dev, self._ref, _APPEND.pack(
-            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, seq_at, slot_at, pos_at, freq_at, k, ld_k, v, ld_v, q_at, ld_q,
+            _layer(layer), n_seq, n_table, T, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, seq_at, slot_at, pos_at, freq_at, k, ld_k, v, ld_v, q_at, ld_q,
             to, ld_to, H, 2 * n, PAIRS[pairs], DTYPES[dtype]))
         if given:
-            _native.written(self.keys, self.values, q_out)
+            _native.written(self._keys, self._values, q_out)
         else:
-            _native.written(self.keys, self.values)
+            _native.written(self._keys, self._values)
         return q_out
 
     def attend(self, layer, q, table, lens, first, *, visible=None, scale=None, out=None):
@@ -410,10 +426,12 @@ class PagedCache:
             out = _native.empty(T, width, dtype, dev)
         to, ld_to, _, _ = rows(out, dev, dtype, T, width) or _matrix("out", out, dev, dtype, T, width)
         scale = self.d_head ** -0.5 if scale is None else float(_number("scale", scale))
+        if 3.4e38 < abs(scale) < float("inf"):
+            raise ValueError(f"scale: {scale} is beyond float32")
         need = self._workspace(H, n_seq, n_table, T)
         work = _native.empty(1, need, torch.uint8, dev) if need else None
         _call("sprinter_cache_attend", dev, self._ref, _ATTEND.pack(
-            _layer(layer), n_seq, n_table, T, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, lens_at, first_at, seen, q_at, ld_q, to, ld_to,
+            _layer(layer), n_seq, n_table, T, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, lens_at, first_at, seen, q_at, ld_q, to, ld_to,
             0 if work is None else work.data_ptr(), need, words, H, scale))
         if given:
             _native.written(out)
@@ -441,9 +459,9 @@ class PagedCache:
         first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
         path_at, ld_path, _, n_path = rows(path, dev, i32, n_seq, -1) or _matrix("path", path, dev, i32, n_seq, -1)
         keep_at = vector(n_keep, dev, i32, n_seq) or _column("n_keep", n_keep, dev, i32, n_seq)
-        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(n_seq, n_table, n_path, self.keys.data_ptr(), self.values.data_ptr(), tab, ld_tab, lens_at, first_at,
+        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(n_seq, n_table, n_path, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, lens_at, first_at,
                                                                 path_at, ld_path, keep_at))
-        _native.written(self.keys, self.values)
+        _native.written(self._keys, self._values)
 
 
 def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=None, repetition=None, presence=None, frequency=None, draft=None,

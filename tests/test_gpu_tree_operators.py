@@ -670,6 +670,21 @@ def test_many_sequences_and_rows():
     assert y.isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes", [1, 9, 20, 70])
+def test_a_table_without_columns(dtype, nodes):
+    """No slot is there: zeros, and nothing is written."""
+    b = Batch(72, dtype, [5, 40], [nodes, nodes], 4, 2, 64, 8)
+    none = b.table[:, :0]
+    assert (b.cache.attend(0, b.q, none, b.lens, b.first) == 0).all()
+    assert (b.cache.attend(0, b.q, none, b.lens, b.first, visible=b.seen()) == 0).all()
+    keys = b.keys.clone()
+    seq, k = _ints([0] * nodes + [1] * nodes), b.q[:, :128]
+    b.cache.append(0, k, k, none, seq, seq)
+    b.cache.keep(none, b.lens, b.first, _ints([[0, 0], [0, 0]]), _ints([2, 2]))
+    assert torch.equal(keys, b.keys)
+
+
 def test_empty_batches():
     b = Batch(71, "bf16", [5], [1], 2, 1, 64, 8)
     none = torch.empty(0, 128, dtype=torch.bfloat16, device=DEV)

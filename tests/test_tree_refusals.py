@@ -129,7 +129,7 @@ def test_attend_arguments(lib):  # noqa: F811
         _refused(lib, _attend(lib, **{name: None}), NULL, "NULL array")
     for words in (0, 17, -1):
         _refused(lib, _attend(lib, words=words), RANGE, "n_words")
-    for scale in (float("nan"), float("inf")):
+    for scale in (float("nan"), float("inf"), 3e38):
         _refused(lib, _attend(lib, scale=scale), CONFIG, "scale")
     for name in ("ldq", "ldy"):
         _refused(lib, _attend(lib, **{name: 248}), RANGE, "closer")
@@ -209,7 +209,8 @@ GOOD = dict(append=lambda c, **kw: c.append(**{**dict(layer=0, keys=f(5, 128), v
     ("append", dict(keys=None), "keys"), ("attend", dict(q=f(5, 250)), "q"), ("attend", dict(q=f(5, 256).bfloat16()), "q"), ("attend", dict(lens=z(4)), "lens"),
     ("attend", dict(first=z(5)), "first"), ("attend", dict(first=z(0)), "first"), ("attend", dict(first=None), "first"),
     ("attend", dict(visible=torch.zeros(5, 0, dtype=torch.int64)), "visible"), ("attend", dict(visible=z(5, 1)), "visible"),
-    ("attend", dict(visible=torch.zeros(5, dtype=torch.int64)), "visible"), ("attend", dict(scale=torch.tensor(1.0)), "plain number"), ("attend", dict(scale="1"), "scale"),
+    ("attend", dict(visible=torch.zeros(5, dtype=torch.int64)), "visible"), ("attend", dict(scale=torch.tensor(1.0)), "plain number"), ("attend", dict(scale="1"), "scale"), ("attend", dict(scale=1e39), "float32"), ("logits", dict(presence=torch._efficientzerotensor(3)), "without memory"),
+    ("append", dict(pos=torch._efficientzerotensor(5, dtype=I)), "without memory"),
     ("attend", dict(out=f(5, 128)), "out"), ("attend", dict(q=f(256, 5).t()), "adjacent"), ("keep", dict(path=z(2, 4)), "path"), ("keep", dict(n_keep=z(4)), "n_keep"),
     ("keep", dict(first=z(3)), "first"), ("keep", dict(lens=z(3).long()), "lens"), ("logits", dict(logits=f(5, 100).half()), "logits"), ("logits", dict(logits=f(500)), "logits"),
     ("logits", dict(tokens=z(4, 9)), "tokens"), ("logits", dict(n_token=z(4)), "n_token"), ("logits", dict(repetition=f(3).double()), "repetition"),
@@ -235,6 +236,28 @@ def test_caches_that_are_none(no_device, lib):  # noqa: F811
                          (f(1, 2, 2, 16, 64), f(1, 2, 2, 16, 64).bfloat16()), (f(1, 2, 2, 64, 16).transpose(3, 4), f(1, 2, 2, 16, 64))):
         with pytest.raises(ValueError):
             ops.PagedCache(keys, values)
+
+
+def test_a_cache_keeps_its_tensors(no_device):  # noqa: F811
+    c = _cache()
+    for name in ("keys", "values"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, f(1, 1, 1, 8, 64))
+
+
+def test_gradients_are_no_matter_where_they_are_off(no_device, lib):  # noqa: F811
+    with torch.no_grad():
+        GOOD["attend"](_cache(), q=torch.ones(5, 256, requires_grad=True))
+        GOOD["logits"](_cache(), logits=torch.ones(5, 100, requires_grad=True), bias=torch.ones(3, 2, requires_grad=True))
+    assert len(no_device) == 2
+
+
+def test_lazy_clones_are_written_apart(no_device, lib):  # noqa: F811
+    """A lazy clone shares its memory until one of the two is written: its address is asked for writing."""
+    t = f(5, 256)
+    u = torch._lazy_clone(t)
+    GOOD["attend"](_cache(), out=u)
+    assert u.data_ptr() != t.data_ptr()
 
 
 def test_gradients_and_tangents_are_refused(no_device, lib):  # noqa: F811
