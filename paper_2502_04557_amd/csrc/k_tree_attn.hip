@@ -15,7 +15,7 @@ struct TreeItem {
 };
 struct TreePlan {
   int target, items, sort;                         // shares to aim for; the most items there can be (per KV head)
-  TreeItem* list;                                  // [items] parts 0: there is none
+  TreeItem* list;                                  // [items] parts 0: there is none.  NULL: no sequence is split
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
   float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
 };
@@ -61,7 +61,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
   }
   work = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_total(work)), 63));
   // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
-  const int share = (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1;
+  const int share = p.list ? (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1 : 1 << 22;
   // The longest sequences first, where workgroups wait for a place and one wave holds them all.
   int from = lane;                                 // the sequence that this lane stands for
   if (p.sort) {
@@ -855,11 +855,21 @@ static TreeShape tree_shape(int type, int dh, int H, int KVH, int n_seq, int T) 
   return rows <= 64 ? of(1, 4) : rows <= 128 ? of(2, 4) : of(2, 8);
 }
 
-static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
+// Splitting a sequence's slots over workgroups costs the merge, its launch and the sums on their way (10 us to 5.7 where it is not needed at all), and is decided
+// by what the table could hold, since only the device knows the lengths.  Measured, split / whole, us: 1 x 8 pairs of sequence and KV head, 250 slots 10.4 / 7.9, 500 10.4 / 10.2,
+// 1000 10.2 / 15.1; 16 x 25 of 400 16.0 / 11.7; 16 x 8 pairs of 50 - 990 slots, 24 nodes 43.0 / 37.3, 64 nodes of 950 84 / 55, 10 nodes 28 / 31; 64 x 8 pairs of up to
+// 2040 slots, 1 node 68 / 61, 9 89 / 77, 30 125 / 92; float32, 160 pairs of up to 1000 17.3 / 22.0, 24 of 132 10.5 / 7.5.
+static bool tree_whole(int type, int KVH, int n_seq, int T, long long slots) {
+  const long long pairs = (long long)std::min(n_seq, T) * KVH;
+  const int steps = pairs >= 512 ? 17 : pairs >= 128 ? 8 : 4;
+  return slots <= (long long)(type == X_F32 ? steps / 2 : steps) * STEP;
+}
+
+static TreePlan tree_plan(const TreeShape& shape, int type, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
   TreePlan p{};
   p.target = std::max(1, ((shape.NW == 8 ? 256 : 512) + KVH - 1) / KVH);
   const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
-  const bool whole = slots <= STEP;                // one share each
+  const bool whole = tree_whole(type, KVH, n_seq, T, slots);
   p.items = (int)(blocks + (whole ? 0 : p.target + 1));
   p.sort = n_seq > 1 && n_seq <= 64 && (long long)p.items * KVH > 512;
   bytes = 0;
@@ -876,14 +886,14 @@ static TreePlan tree_plan(const TreeShape& shape, int dh, int H, int KVH, int n_
 size_t attend_workspace(int type, int dh, int H, int KVH, int n_seq, int T, long long slots) {
   size_t bytes;
   if (n_seq < 1 || T < 1) return 0;
-  tree_plan(tree_shape(type, dh, H, KVH, n_seq, T), dh, H, KVH, n_seq, T, slots, bytes, nullptr);
+  tree_plan(tree_shape(type, dh, H, KVH, n_seq, T), type, dh, H, KVH, n_seq, T, slots, bytes, nullptr);
   return bytes;
 }
 
 void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
   size_t bytes;
   const TreeShape shape = tree_shape(a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T);
-  const TreePlan p = tree_plan(shape, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
+  const TreePlan p = tree_plan(shape, a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
   const dim3 grid(a.c.KVH * p.items), block(256);
   auto go = [&](auto type, auto dh) {
     using T = decltype(type);
