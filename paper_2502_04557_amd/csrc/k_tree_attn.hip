@@ -185,7 +185,11 @@ __device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsign
 //     those of the keys 8 (lane / 16) .. + 7, the operand layout of P.  float32: the 4 keys 4 (lane / 16) + r, one for each of four products.
 //   O^T += V^T P^T: a lane fetches DH / 16 neighbouring columns of each of its keys, whole rows by 16 lanes; operand c takes column c of each
 //     lane's, which for bf16 is one byte permutation per pair of keys.  The accumulators then hold DH / 4 neighbouring columns of a row.
-// P enters as two bf16 (16 bits, as the values of the plain bfloat16 path deserve: one alone would double the error of the result).
+// P enters as two bf16, 16 bits together: one alone would add an error as large as the result's own rounding (by its arithmetic 1.7e-3 ->
+// 2.4e-3), for 10 % of the largest case's time.  For up to 32 rows of a sequence; a key costs the same for any of them.
+// Bound by HBM where there is enough to read (128 sequences x 32 heads, 1 node, up to 1024 slots: 1.14 GB in 202 us = 5.6 TB/s; one sequence of 30000 slots: 26 us, its
+// 123 MB take 20), else by a chain of 4 - 5 loads (lengths, table and queries, keys and values: 6 us).  Measured and dropped: registers for three workgroups on a
+// compute unit (64 x 8 pairs, up to 2047 slots: 68 -> 75 us), 384 / 768 / 1024 / 1536 workgroups to split for instead of 512 (equal, or up to 15 % slower).
 template <typename T, int DH, int QT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan plan) {
   using P = Tree<T>;
@@ -510,7 +514,12 @@ __device__ __forceinline__ void piece_to_lds(u64 base, unsigned off, unsigned ld
 
 // The same for many rows (bf16): the NW waves share the keys and values of the item through a ring of S stages of 32 keys in LDS and have 16 QT rows each.
 // Half of the waves bring keys, half values, as whole rows of DH columns; the fragments of V^T are read with ds_read_b64_tr_b16, four keys of a column at a
-// time.  The pieces of a row lie where an exclusive-or with its number puts them, so that no read meets a bank twice.
+// time.  The pieces of a row lie where an exclusive-or with its number puts them, so that no read meets a bank twice (SQ_LDS_BANK_CONFLICT 0).
+// What bounds it: HBM up to 128 rows (4 sequences of 9000 - 40000 slots, 24 nodes x 4 heads: 493 MB in 103 us = 4.8 TB/s, and a merge of 10), above it matrix instructions next to the
+// softmax's vector work at the clock that their power leaves (64 sequences of 64 - 2047 slots, 64 nodes x 4: 135 us, 1.3 us per block of 32 keys and 256 rows, of which the
+// matrix instructions are 0.65 at 2.4 GHz; 60 launches in a row take 149 - 188 us each).  Measured there and dropped: a barrier for two blocks, the next block's scores under
+// this one's softmax, weights of one row tile under the products of the other, wave priorities, the two waves of a SIMD half a block apart (all equal), 64 rows a
+// wave (145 -> 177 us); without the low half of P 10 % faster, without memory traffic 9 %.  Eight waves with 256 rows against two blocks of 128: 150 -> 141 us.
 template <int DH, int QT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, TreePlan plan) {
   constexpr int QB = 16 * QT * NW, KF = DH / 32, CT = DH / 16, F = 2 * CT, LPW = F / NW, S = 4, PPR = DH / 8;   // F pieces of 1 KiB a stage, LPW of them by a wave
