@@ -18,12 +18,18 @@ __device__ __forceinline__ float logit_f32(bf16_t v) { return __uint_as_float((u
 __device__ __forceinline__ void put_logit(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put_logit(bf16_t* p, float v) { *p = f2bf(v); }
 
-// The sequence of row t, by a whole wave: the last b with first[b] <= t, or -1 where t is no row of it.
+// The sequence of row t, by a whole wave, 64 places at a time: the last b with first[b] <= t, or -1 where t is no row of it.
 __device__ __forceinline__ int row_sequence(const int* first, int n_seq, int n_rows, int t, int& f0, int& f1) {
   const int lane = threadIdx.x & 63;
-  int b = -1;
-  for (int b0 = 0; b0 < n_seq; b0 += 64) b += __popcll(__ballot(b0 + lane < n_seq && first[min(b0 + lane, n_seq)] <= t));
-  if (b < 0) return -1;
+  int b = 0;
+  for (int n = n_seq; n > 0;) {                    // among b .. b + n - 1
+    const int stride = (n + 63) >> 6;
+    const int below = __popcll(__ballot((long long)lane * stride < n && first[min((long long)b + (long long)lane * stride, (long long)n_seq)] <= t));
+    if (below == 0) return -1;
+    b += (below - 1) * stride;
+    n = stride == 1 ? 0 : min(stride, n - (below - 1) * stride);
+  }
+  if (n_seq < 1) return -1;
   f0 = max(first[b], 0);
   f1 = min(first[b + 1], n_rows);
   return t >= f0 && t < f1 ? b : -1;

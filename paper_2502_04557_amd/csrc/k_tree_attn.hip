@@ -7,15 +7,16 @@
 namespace sprinter {
 
 // A launch cuts the batch into items: a block of QB rows (node x head of one KV head) of a sequence against a share of its slots.  Lengths and trees are known
-// on the device alone, so every workgroup works the cut out for itself from `lens` and `first`: `steps` of STEP slots over all blocks of rows,
-// dealt out in shares of `share` steps so that about `target` items come out, however ragged the batch is.
+// on the device alone, so every workgroup works the cut out for itself from `lens` and `first` (more than 128 sequences: k_tree_plan does, once): `steps` of STEP slots
+// over all blocks of rows, dealt out in shares of `share` steps so that about `target` items come out, however ragged the batch is.
 struct TreeItem {
   int f0, n, len, b;                               // the sequence: rows f0 .. f0 + n - 1
   int block, part, parts, share;                   // block of rows, share of slots, how many of them, steps of each
 };
 struct TreePlan {
-  int target, items, sort;                         // shares to aim for; the most items there can be (per KV head)
-  TreeItem* list;                                  // [items] parts 0: there is none.  NULL: no sequence is split
+  int target, items;                               // shares to aim for; the most items there can be (per KV head)
+  int split, sort, planned;                        // sequences may be split; the longest first; the items are listed before the launch
+  TreeItem* list;                                  // [items] (split or planned) parts 0: there is none
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
   float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
 };
@@ -36,9 +37,10 @@ __device__ __forceinline__ TreeSeq tree_seq(const AttendArgs& a, int b, int QB, 
   return s;
 }
 
-// Sums over the lanes up to this one (itself among them); `all`: over the whole wave.
+// Sums over the lanes up to this one (itself among them) of numbers from 0 to 2^30, where they stay; `all`: over the whole wave.
+constexpr int MOST_ITEMS = 1 << 30;
 __device__ __forceinline__ int scan_to_lane(int v, int& all) {
-#define SPRINTER_SCAN_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+#define SPRINTER_SCAN_STEP(CTRL, ROWS) v = min(v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false), MOST_ITEMS)
   SPRINTER_SCAN_STEP(0x111, 0xF);   // row_shr:1, 2, 4, 8, then the last lanes of rows into the rows behind them
   SPRINTER_SCAN_STEP(0x112, 0xF);
   SPRINTER_SCAN_STEP(0x114, 0xF);
@@ -50,6 +52,12 @@ __device__ __forceinline__ int scan_to_lane(int v, int& all) {
   return v;
 }
 
+__device__ __forceinline__ int tree_share(const TreePlan& p, float work) {
+  // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
+  return p.split ? (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1 : 1 << 22;
+}
+__device__ __forceinline__ int tree_items(const TreeSeq& s, int parts) { return (int)min((long long)s.blocks * parts, (long long)MOST_ITEMS); }
+
 // The item of index `item`, by one wave; false: there is none.
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p, int QB, int item, TreeItem& out) {
   const int lane = threadIdx.x & 63, n = a.c.n_seq;
@@ -60,8 +68,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     work += (float)x.blocks * (float)x.steps;
   }
   work = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_total(work)), 63));
-  // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
-  const int share = p.list ? (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1 : 1 << 22;
+  const int share = tree_share(p, work);
   // The longest sequences first, where workgroups wait for a place and one wave holds them all.
   int from = lane;                                 // the sequence that this lane stands for
   if (p.sort) {
@@ -77,7 +84,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
   out.parts = 0;
   for (int b0 = 0; b0 < n; b0 += 64) {
     if (b0) s = tree_seq(a, b0 + lane, QB, b0 + lane < n);
-    const int parts = (s.steps + share - 1) / share, mine = s.blocks * parts;
+    const int parts = (s.steps + share - 1) / share, mine = tree_items(s, parts);
     int all;
     const int before = base + scan_to_lane(mine, all) - mine;
     const u64 hit = __ballot(item >= before && item < before + mine);
@@ -96,12 +103,16 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     }
     base += all;
   }
-  if (p.list && blockIdx.x % a.c.KVH == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
+  if (p.split && blockIdx.x % a.c.KVH == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
   return out.parts > 0;
 }
 // The same by a workgroup: its first wave looks, the others get it through LDS.
 __device__ __forceinline__ bool find_item_of_block(const AttendArgs& a, const TreePlan& p, int QB, TreeItem& out) {
   __shared__ TreeItem shared;
+  if (p.planned) {
+    out = p.list[blockIdx.x / a.c.KVH];
+    return out.parts > 0;
+  }
   if (wave_index() == 0) {
     find_item(a, p, QB, blockIdx.x / a.c.KVH, out);
     if (threadIdx.x == 0) shared = out;
@@ -112,6 +123,52 @@ __device__ __forceinline__ bool find_item_of_block(const AttendArgs& a, const Tr
   for (int i = 0; i < 8; ++i) v[i] = uniform(reinterpret_cast<const int*>(&shared)[i]);
   out = TreeItem{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
   return out.parts > 0;
+}
+
+// All items of a launch, by one workgroup: a list of as many entries as there is room for.
+__global__ __launch_bounds__(1024) void k_tree_plan(AttendArgs a, TreePlan p, int QB) {
+  __shared__ float wave_work[16];
+  __shared__ int wave_items[16];
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_index(), n = a.c.n_seq;
+  float work = 0.f;
+  for (int b = tid; b < n; b += 1024) {
+    const TreeSeq s = tree_seq(a, b, QB, true);
+    work += (float)s.blocks * (float)s.steps;
+  }
+  work = wave_total(work);
+  if (lane == 63) wave_work[w] = work;
+  __syncthreads();
+  work = 0.f;
+  for (int x = 0; x < 16; ++x) work += wave_work[x];
+  const int share = tree_share(p, work);
+  int base = 0;
+  for (int b0 = 0; b0 < n && base < p.items; b0 += 1024) {       // (the same for all threads)
+    const TreeSeq s = tree_seq(a, b0 + tid, QB, b0 + tid < n);
+    const int parts = (s.steps + share - 1) / share, mine = tree_items(s, parts);
+    int all;
+    const int upto = scan_to_lane(mine, all);
+    if (lane == 0) wave_items[w] = all;
+    __syncthreads();
+    int before = base, total = base;
+    for (int x = 0; x < 16; ++x) {
+      if (x < w) before = min(before + wave_items[x], MOST_ITEMS);
+      total = min(total + wave_items[x], MOST_ITEMS);
+    }
+    __syncthreads();
+    base = total;
+    before = min(before + (upto - mine), MOST_ITEMS);
+    for (u64 some = __ballot(mine > 0 && before < p.items); some; some &= some - 1) {   // a sequence's items by the whole wave
+      const int l = __builtin_ctzll(some), from = __builtin_amdgcn_readlane(before, l), count = min(__builtin_amdgcn_readlane(mine, l), p.items - from);
+      TreeItem it{__builtin_amdgcn_readlane(s.f0, l), __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.len, l), b0 + 64 * w + l, 0, 0,
+                  __builtin_amdgcn_readlane(parts, l), share};
+      for (int x = lane; x < count; x += 64) {
+        it.block = x / it.parts;
+        it.part = x - it.block * it.parts;
+        p.list[from + x] = it;
+      }
+    }
+  }
+  for (int x = base + tid; x < p.items; x += 1024) p.list[x].parts = 0;
 }
 
 // bf16: 32 keys a block, of which a lane ends up with the scores of 8; float32: 16 and 4.
@@ -880,15 +937,14 @@ static TreePlan tree_plan(const TreeShape& shape, int type, int dh, int H, int K
   const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
   const bool whole = tree_whole(type, KVH, n_seq, T, slots);
   p.items = (int)(blocks + (whole ? 0 : p.target + 1));
+  p.split = !whole;
   p.sort = n_seq > 1 && n_seq <= 64 && (long long)p.items * KVH > 512;
-  bytes = 0;
-  if (!whole) {
-    const size_t rows = (size_t)p.items * KVH * shape.QB;
-    bytes = rows * (dh + 2) * sizeof(float) + p.items * sizeof(TreeItem);
-    p.o = (float*)ws;
-    p.ml = p.o + rows * dh;
-    p.list = (TreeItem*)(p.ml + rows * 2);
-  }
+  p.planned = n_seq > 128;
+  const size_t rows = whole ? 0 : (size_t)p.items * KVH * shape.QB;
+  bytes = rows * (dh + 2) * sizeof(float) + (whole && !p.planned ? 0 : p.items * sizeof(TreeItem));
+  p.o = (float*)ws;
+  p.ml = p.o + rows * dh;
+  p.list = (TreeItem*)(p.ml + rows * 2);
   return p;
 }
 
@@ -904,6 +960,7 @@ void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
   const TreeShape shape = tree_shape(a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T);
   const TreePlan p = tree_plan(shape, a.type, a.c.dh, a.H, a.c.KVH, a.c.n_seq, a.T, (long long)a.c.n_table << a.c.shift, bytes, workspace);
   const dim3 grid(a.c.KVH * p.items), block(256);
+  if (p.planned) hipLaunchKernelGGL(k_tree_plan, dim3(1), dim3(1024), 0, s, a, p, shape.QB);
   auto go = [&](auto type, auto dh) {
     using T = decltype(type);
     constexpr int DH = decltype(dh)::value;
@@ -915,7 +972,7 @@ void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {
       else if (shape.NW == 4) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 4>), grid, block, 0, s, a, p);
       else if (shape.NW == 8) hipLaunchKernelGGL((k_tree_attn_shared<DH, 2, 8>), grid, dim3(512), 0, s, a, p);
     }
-    if (bytes) hipLaunchKernelGGL((k_tree_merge<T, DH>), grid, block, 0, s, a, p, shape.QB);
+    if (p.split) hipLaunchKernelGGL((k_tree_merge<T, DH>), grid, block, 0, s, a, p, shape.QB);
   };
   auto typed = [&](auto dh) { if (a.type == X_F32) go(float(), dh); else go(bf16_t(), dh); };
   if (a.c.dh == 64) typed(std::integral_constant<int, 64>()); else typed(std::integral_constant<int, 128>());

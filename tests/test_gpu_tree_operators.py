@@ -436,6 +436,15 @@ def test_logits_in_place_strides_and_rows_of_no_sequence(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_of_many_sequences(dtype):
+    g = np.random.default_rng(6)
+    for n in (63, 64, 65, 4097):
+        nodes = g.integers(0, 3, n).tolist()
+        logits, first, kw = _logits_case(n, dtype, n, nodes, 37, 5, 2)
+        _check_logits(logits, first, kw, dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_logits_that_are_not_finite(dtype):
     """-infinity stays, NaN stays where it is allowed, and nothing is left where the mask forbids."""
     logits, first, kw = _logits_case(4, dtype, 2, [3, 3], 300, 50, 6)
@@ -660,14 +669,47 @@ def test_the_same_call_gives_the_same_bits(dtype):
         assert torch.equal(b.cache.attend(0, b.q, b.table, b.lens, b.first, visible=vis), want)
 
 
-def test_many_sequences_and_rows():
-    """More sequences than a wave has lanes, and than a workgroup has threads; most of them with one node or none."""
-    g = np.random.default_rng(3)
-    lens, nodes = g.integers(0, 40, 700).tolist(), g.integers(0, 3, 700).tolist()
-    b = Batch(70, "bf16", lens, nodes, 2, 1, 64, 8)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, longest, most", [(65, 700, 3), (128, 40, 40), (129, 40, 3), (700, 40, 3), (1300, 3000, 2)])
+def test_many_sequences(dtype, n, longest, most):
+    """More sequences than a wave or a workgroup has lanes, most of them short, with one node or none, a few long ones that are split."""
+    g = np.random.default_rng(n)
+    lens, nodes = g.integers(0, 40, n), g.integers(0, most + 1, n)
+    lens[[0, n // 2, n - 1]], nodes[[0, n // 2, n - 1]] = longest, most
+    b = Batch(70, dtype, lens.tolist(), nodes.tolist(), 2, 1, 64, 8)
     b.check()
-    y = b.cache.attend(0, b.q, b.table, b.lens, b.first, visible=b.seen())
-    assert y.isfinite().all()
+    b.check(visible=b.seen())
+
+
+def test_very_many_sequences():
+    """Every sequence one row, as many as need four levels of the search for it; equal to sixteen batches of them."""
+    n = 1 << 19
+    b = Batch(73, "bf16", [3], [1], 2, 1, 64, 8)
+    table = torch.randint(0, b.keys.shape[1], (n, 1), generator=b.g).to(torch.int32).to(DEV)
+    lens = torch.randint(0, 8, (n,), generator=b.g).to(torch.int32).to(DEV)
+    q, first = b.normal(n, 128).bfloat16(), torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    y = b.cache.attend(0, q, table, lens, first)
+    part = n // 16
+    for i in range(0, n, part):
+        assert torch.equal(y[i:i + part], b.cache.attend(0, q[i:i + part], table[i:i + part], lens[i:i + part], first[:part + 1]))
+    x, rep, tokens = b.normal(n, 40), b.normal(n).abs() + 0.5, torch.randint(0, 40, (n, 3), generator=b.g).to(torch.int32).to(DEV)
+    assert torch.equal(_ops().adjust_logits(x, first, tokens=tokens, repetition=rep), _ops().adjust_logits(x, tokens=tokens, repetition=rep))
+
+
+@pytest.mark.parametrize("first", [[0, 9, 0, 9, 0, 9], [9, 8, 7, 3, 2, 0], [-5, 3, 100, 2, -7, 9], [5, 5, 5, 5, 5, 5]])
+@pytest.mark.parametrize("copies", [1, 200])
+def test_rows_that_do_not_ascend_end(first, copies):
+    """What `first` says then is nobody's: outputs are not said, but every call ends and writes within its rows."""
+    n = 5 * copies
+    b = Batch(74, "bf16", [40], [9], 4, 2, 64, 8)
+    table, lens = b.table.expand(n, -1).contiguous(), torch.full((n,), 40, dtype=torch.int32, device=DEV)
+    f = _ints((first[:5] * copies) + first[5:])
+    out = torch.full((9 + 2, 256), 3.0, dtype=torch.bfloat16, device=DEV)
+    b.cache.attend(0, b.q, table, lens, f, out=out[1:10])
+    assert (out[0] == 3).all() and (out[10] == 3).all()
+    x = b.normal(9, 50)
+    _ops().adjust_logits(x, f, tokens=torch.zeros(n, 2, dtype=torch.int32, device=DEV), repetition=torch.ones(n, device=DEV), draft=_ints([1] * 9))
+    torch.cuda.synchronize()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
