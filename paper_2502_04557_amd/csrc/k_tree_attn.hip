@@ -534,13 +534,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   for (int t = 0; t < QT; ++t) {
     if (!row_there[t]) continue;
     float x[4 * CPL];                              // columns 4 CPL lq .. of the row
-    const float inv = it.parts > 1 ? 1.f : l_all[t] == 0.f ? 0.f : 1.f / l_all[t];
+    const float inv = it.parts > 1 ? 1.f : 1.f / l_all[t];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int i = 0; i < CPL; ++i) x[CPL * r + i] = l_all[t] == 0.f ? 0.f : O[t][i][r] * inv;
     if (it.parts > 1) {
-      const long long at = (((long long)blockIdx.x) * QB + 16 * t + l16);
+      const long long at = (long long)blockIdx.x * QB + 16 * t + l16;
       float* dst = plan.o + at * DH + 4 * CPL * lq;
 #pragma unroll
       for (int i = 0; i < 4 * CPL; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
@@ -845,10 +845,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     if (!row_there[t]) continue;
     const int i = (int)(16 * QT * w + 16 * t + l16);
     if (it.parts > 1) {
-      const long long at = ((long long)blockIdx.x) * QB + i;
+      const long long at = (long long)blockIdx.x * QB + i;
 #pragma unroll
-      for (int x = 0; x < CT; ++x)
-        *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(O[t][x][0], O[t][x][1], O[t][x][2], O[t][x][3]);
+      for (int x = 0; x < CT; ++x) {
+        const f32x4 o = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t][x];
+        *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(o[0], o[1], o[2], o[3]);
+      }
       if (lq == 0) *reinterpret_cast<float2*>(plan.ml + at * 2) = make_float2(m_run[t], l);
     } else {
       const float inv = l == 0.f ? 0.f : 1.f / l;
