@@ -483,7 +483,7 @@ int sprinter_cache_keep(const sprinter_cache_cfg* cfg, const sprinter_keep* args
  * of which the first n_prompt[b] (NULL: none) were not generated, and draft[j] of the nodes j that the row sees (draft [n_rows], generated).
  * bias_ids, bias [n_seq, n_bias]: pairs of a token and its bias, the last of a token's pairs counts.  mask [n_mask, (vocab + 31) / 32]: bit v % 32 of word
  * v / 32; mask_row [n_rows] says which mask a row has, outside [0, n_mask) none (NULL: mask t, and n_rows <= n_mask).  A token outside [0, vocab) is
- * nobody's (padding).  Limits: vocab 2^24, n_tokens and - with draft - n_rows 2^19, n_bias 2047.  Rows lie ld_* elements apart. */
+ * nobody's (padding).  Limits: vocab 2^24, n_tokens and - with draft - n_rows 2^19 (not both), n_bias 2047.  Rows lie ld_* elements apart. */
 typedef struct {
   int32_t dtype, n_rows, vocab, n_seq;
   const void* logits; int64_t ld_logits;

@@ -294,6 +294,8 @@ int sprinter_adjust_logits(const sprinter_logits* args, void* hip_stream) {
   if (a.n_seq < 0 || a.n_seq > MAX_TREE_ROWS) return op_fail(SPRINTER_E_RANGE, "%s: %d sequences are not in [0, %d]", who, a.n_seq, MAX_TREE_ROWS);
   if (a.n_tokens < 0 || a.n_tokens > MAX_HISTORY) return op_fail(SPRINTER_E_RANGE, "%s: n_tokens %d outside [0, 2^19]", who, a.n_tokens);
   if (a.draft && a.n_rows > MAX_HISTORY) return op_fail(SPRINTER_E_RANGE, "%s: %d rows with draft are more than 2^19", who, a.n_rows);
+  if (a.draft && a.n_rows == MAX_HISTORY && a.n_tokens == MAX_HISTORY)   // (a token's count is below 2^20)
+    return op_fail(SPRINTER_E_RANGE, "%s: n_tokens and rows with draft are 2^20 together", who);
   if (a.visible && (a.n_words < 1 || a.n_words > MAX_NODE_WORDS))
     return op_fail(SPRINTER_E_RANGE, "%s: n_words %d outside [1, %d]", who, a.n_words, MAX_NODE_WORDS);
   if (a.n_bias < 0 || a.n_bias > MAX_BIASES) return op_fail(SPRINTER_E_RANGE, "%s: n_bias %d outside [0, %d]", who, a.n_bias, MAX_BIASES);

@@ -174,6 +174,8 @@ def test_logits_arguments(lib):  # noqa: F811
     for name in ("logits", "out", "first", "tokens", "n_token", "n_prompt", "repetition", "presence", "frequency", "draft", "visible", "bias_ids", "bias", "mask",
                  "mask_row"):
         _refused(lib, _logits(lib, **{name: A + (4 if name == "visible" else 2)}), RANGE, "aligned")
+    half = 1 << 19                                       # each is a limit that is allowed; together a token's count would be 2^20
+    _refused(lib, _logits(lib, n_rows=half, n_tokens=half, ld_tokens=half), RANGE, "together")
     assert _logits(lib, n_rows=0) == 0
 
 
