@@ -246,7 +246,8 @@ __device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsign
 // 2.4e-3), for 10 % of the largest case's time.  For up to 32 rows of a sequence; a key costs the same for any of them.
 // Bound by HBM where there is enough to read (128 sequences x 32 heads, 1 node, up to 1024 slots: 1.14 GB in 202 us = 5.6 TB/s; one sequence of 30000 slots: 26 us, its
 // 123 MB take 20), else by a chain of 4 - 5 loads (lengths, table and queries, keys and values: 6 us).  Measured and dropped: registers for three workgroups on a
-// compute unit (64 x 8 pairs, up to 2047 slots: 68 -> 75 us), 384 / 768 / 1024 / 1536 workgroups to split for instead of 512 (equal, or up to 15 % slower).
+// compute unit (64 x 8 pairs, up to 2047 slots: 68 -> 75 us), 384 / 768 / 1024 / 1536 workgroups to split for instead of 512 (equal, or up to 15 % slower),
+// 8 or 16 waves (one sequence of 500 / 1100 / 2000 slots unsplit: 4 waves 10.2 / 15.9 / 24.1 us, 8 waves 10.8 / 15.7 / 24.0: a compute unit fetches no faster).
 template <typename T, int DH, int QT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan plan) {
   using P = Tree<T>;
