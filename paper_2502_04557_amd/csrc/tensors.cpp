@@ -10,12 +10,20 @@
 
 namespace {
 
+// Whether the storage of `t` reaches to its last element: a program may have freed it, or a part of it, and kept the tensor.
+bool held(const at::Tensor& t) {
+  if (t.numel() == 0) return true;
+  int64_t last = t.storage_offset();
+  for (int64_t d = 0; d < t.dim(); ++d) last += (t.size(d) - 1) * t.stride(d);
+  return (size_t)(last + 1) * t.element_size() <= t.storage().nbytes();
+}
+
 // The tensor behind `o`, if it is one of this type on this device with nothing about it that the library's kernels do not know.
 const at::Tensor* plain(PyObject* o, PyObject* device, PyObject* dtype) {
   if (!THPVariable_Check(o) || !THPDevice_Check(device) || !THPDtype_Check(dtype)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || t.layout() != at::kStrided || t.scalar_type() != ((THPDtype*)dtype)->scalar_type || t.device() != ((THPDevice*)device)->device ||
-      t.is_neg() || t.is_conj() || t._is_zerotensor() || t.requires_grad())
+      t.is_neg() || t.is_conj() || t._is_zerotensor() || t.requires_grad() || !held(t))
     return nullptr;
   return &t;
 }
@@ -36,6 +44,20 @@ PyObject* vector(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// array(t, device, dtype, n) -> the address of a contiguous array of n elements in all
+PyObject* array(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) { PyErr_SetString(PyExc_TypeError, "array(t, device, dtype, n)"); return nullptr; }
+  const long long want = PyLong_AsLongLong(a[3]);
+  if (want == -1 && PyErr_Occurred()) return nullptr;
+  try {
+    const at::Tensor* t = plain(a[0], a[1], a[2]);
+    if (!t || t->numel() != want || !t->is_contiguous()) return none();
+    return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t->data_ptr());
+  } catch (const std::exception&) {
+    return none();
+  }
+}
+
 // rows(t, device, dtype, rows, cols) -> (address, distance of rows, rows, columns) of a matrix whose rows may lie apart; rows, cols: -1 for any
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 5) { PyErr_SetString(PyExc_TypeError, "rows(t, device, dtype, rows, cols)"); return nullptr; }
@@ -47,7 +69,9 @@ PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const long long r = t->size(0), c = t->size(1);
     if ((want_rows >= 0 && r != want_rows) || (want_cols >= 0 && c != want_cols) || r >= 1ll << 31 || c >= 1ll << 31) return none();
     if (c > 1 && t->stride(1) != 1) return none();
-    return Py_BuildValue("KLLL", (unsigned long long)(uintptr_t)t->data_ptr(), (long long)t->stride(0), r, c);
+    const void* at = t->data_ptr();
+    if (!at && r && c) return none();                  // (no address would stand for no tensor)
+    return Py_BuildValue("KLLL", (unsigned long long)(uintptr_t)at, (long long)t->stride(0), r, c);
   } catch (const std::exception&) {
     return none();
   }
@@ -74,6 +98,7 @@ PyObject* written(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyMethodDef methods[] = {{"vector", (PyCFunction)(void*)vector, METH_FASTCALL, "vector(t, device, dtype, n) -> address or None"},
+                         {"array", (PyCFunction)(void*)array, METH_FASTCALL, "array(t, device, dtype, n) -> address or None"},
                          {"rows", (PyCFunction)(void*)rows, METH_FASTCALL, "rows(t, device, dtype, rows, cols) -> (address, distance, rows, columns) or None"},
                          {"empty", (PyCFunction)(void*)empty, METH_FASTCALL, "empty(rows, cols, dtype, device) -> a new matrix"},
                          {"written", (PyCFunction)(void*)written, METH_FASTCALL, "written(t, ...): their versions go up"},

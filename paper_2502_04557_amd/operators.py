@@ -289,9 +289,9 @@ def _no(*args):
 
 
 def _looks():
-    """Its (rows, vector); inside a level of forward mode, whose tangents it does not see, everything takes the checks in Python."""
+    """Its (rows, vector, array); inside a level of forward mode, whose tangents it does not see, everything takes the checks in Python."""
     n = _native or _asks()
-    return (n.rows, n.vector) if forward_ad._current_level < 0 else (_no, _no)
+    return (n.rows, n.vector, n.array) if forward_ad._current_level < 0 else (_no, _no, _no)
 
 
 # What those say None of: the checks in Python, which raise, or let the uncommon (an empty tensor, one that asks for gradients where they are off) pass.
@@ -308,9 +308,12 @@ def _column(name, t, device, dtype, n):
 
 
 def _memory(name, t):
+    """The address of `t`, whose storage may have been freed, or a part of it (no address would stand for no tensor)."""
     at = t.data_ptr()
-    if at == 0 and t.numel() > 0:                        # (no address would stand for no tensor)
-        raise ValueError(f"{name}: a tensor without memory")
+    if t.numel() > 0:
+        last = t.storage_offset() + sum((n - 1) * d for n, d in zip(t.shape, t.stride()))
+        if at == 0 or (last + 1) * t.element_size() > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: a tensor without memory")
     return at
 
 
@@ -348,11 +351,22 @@ class PagedCache:
         shape = tuple(keys.shape)
         for name, t in (("keys", keys), ("values", values)):
             _whole(name, t, dev, keys.dtype, *shape)
+            _memory(name, t)
         self._keys, self._values, self.device, self.dtype = keys, values, dev, keys.dtype
         self.n_layer, self.n_page, self.n_kv_head, self.page_size, self.d_head = shape
         self._cfg = CacheCfgC(DTYPES[keys.dtype], *(_int32("keys' sizes", shape[i]) for i in (0, 1, 3, 2, 4)))
         self._ref = C.byref(self._cfg)
+        self._shape, self._elements = shape, keys.numel()
         self._need = {}
+
+    def _arrays(self, array):
+        """The addresses of keys and values: theirs of this call, as their memory may have moved or gone."""
+        dev, dtype, n = self.device, self.dtype, self._elements
+        return (array(self._keys, dev, dtype, n) or self._array("keys", self._keys), array(self._values, dev, dtype, n) or self._array("values", self._values))
+
+    def _array(self, name, t):
+        _whole(name, t, self.device, self.dtype, *self._shape)
+        return _memory(name, t)
 
     @property
     def keys(self):
@@ -369,7 +383,8 @@ class PagedCache:
         [T], by default the slot), in the pairs (i, i + n / 2) ("halves") or (2 i, 2 i + 1) ("neighbours").  Rows are bfloat16 or float32, all of one
         type; what is written has the cache's.  A token of no sequence (-1) is padding.  q_out: where the turned q goes (q itself turns it in place)."""
         dev, d, i32 = self.device, self.d_head, torch.int32
-        rows, vector = _looks()
+        rows, vector, array = _looks()
+        cache_keys, cache_values = self._arrays(array)
         dtype = keys.dtype if isinstance(keys, Tensor) else None
         if dtype not in DTYPES:
             raise ValueError("keys: bfloat16 or float32 rows are needed")
@@ -399,7 +414,7 @@ class PagedCache:
         elif given:
             raise ValueError("q_out: there is no q")
         _call("sprinter_cache_append", dev, self._ref, _APPEND.pack(
-            _layer(layer), n_seq, n_table, T, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, seq_at, slot_at, pos_at, freq_at, k, ld_k, v, ld_v, q_at, ld_q,
+            _layer(layer), n_seq, n_table, T, cache_keys, cache_values, tab, ld_tab, seq_at, slot_at, pos_at, freq_at, k, ld_k, v, ld_v, q_at, ld_q,
             to, ld_to, H, 2 * n, PAIRS[pairs], DTYPES[dtype]))
         if given:
             _native.written(self._keys, self._values, q_out)
@@ -412,7 +427,8 @@ class PagedCache:
         sees (sprinter_cache_attend).  scale: of the scores, by default d_head ** -0.5.  A row that sees nothing gives zeros; rows of no
         sequence are not written."""
         dev, dtype, i32 = self.device, self.dtype, torch.int32
-        rows, vector = _looks()
+        rows, vector, array = _looks()
+        keys, values = self._arrays(array)
         q_at, ld_q, T, width = rows(q, dev, dtype, -1, -1) or _matrix("q", q, dev, dtype, -1, -1)
         H = width // self.d_head
         if H < 1 or width != H * self.d_head:
@@ -431,7 +447,7 @@ class PagedCache:
         need = self._workspace(H, n_seq, n_table, T)
         work = _native.empty(1, need, torch.uint8, dev) if need else None
         _call("sprinter_cache_attend", dev, self._ref, _ATTEND.pack(
-            _layer(layer), n_seq, n_table, T, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, lens_at, first_at, seen, q_at, ld_q, to, ld_to,
+            _layer(layer), n_seq, n_table, T, keys, values, tab, ld_tab, lens_at, first_at, seen, q_at, ld_q, to, ld_to,
             0 if work is None else work.data_ptr(), need, words, H, scale))
         if given:
             _native.written(out)
@@ -453,13 +469,14 @@ class PagedCache:
         """Slot lens[b] + path[b, j] -> slot lens[b] + j in every layer, j < n_keep[b] (path int32 [n_seq, n], nodes in ascending order; n_keep int32
         [n_seq]): the accepted nodes become the next committed slots (sprinter_cache_keep).  lens is the caller's to advance."""
         dev, i32 = self.device, torch.int32
-        rows, vector = _looks()
+        rows, vector, array = _looks()
+        keys, values = self._arrays(array)
         tab, ld_tab, n_seq, n_table = rows(table, dev, i32, -1, -1) or _matrix("table", table, dev, i32, -1, -1)
         lens_at = vector(lens, dev, i32, n_seq) or _column("lens", lens, dev, i32, n_seq)
         first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
         path_at, ld_path, _, n_path = rows(path, dev, i32, n_seq, -1) or _matrix("path", path, dev, i32, n_seq, -1)
         keep_at = vector(n_keep, dev, i32, n_seq) or _column("n_keep", n_keep, dev, i32, n_seq)
-        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(n_seq, n_table, n_path, self._keys.data_ptr(), self._values.data_ptr(), tab, ld_tab, lens_at, first_at,
+        _call("sprinter_cache_keep", dev, self._ref, _KEEP.pack(n_seq, n_table, n_path, keys, values, tab, ld_tab, lens_at, first_at,
                                                                 path_at, ld_path, keep_at))
         _native.written(self._keys, self._values)
 
@@ -479,7 +496,7 @@ def adjust_logits(logits, first=None, *, tokens=None, n_token=None, n_prompt=Non
     if logits.dtype not in DTYPES:
         raise ValueError("logits: bfloat16 or float32 is needed")
     dtype, f32, i32 = logits.dtype, torch.float32, torch.int32
-    rows, vector = _looks()
+    rows, vector, _ = _looks()
     at, ld, T, V = rows(logits, dev, dtype, -1, -1) or _matrix("logits", logits, dev, dtype, -1, -1)
     n_seq, first_at = T, 0
     if first is not None:

@@ -289,3 +289,59 @@ def test_tensors_written_in_place_are_known_to_autograd(no_device, lib):  # noqa
         c = _cache()
         GOOD["append"](c)
         GOOD["logits"](c, out=f(5, 100))
+
+
+def _shrunk(t, left):
+    """`t` after its storage was cut to `left` bytes, as programs do that free a tensor's memory and keep the tensor."""
+    t.untyped_storage().resize_(left)
+    return t
+
+
+WITHOUT = dict(append=dict(keys=lambda: f(5, 128), values=lambda: f(5, 128), table=lambda: z(3, 4), seq=lambda: z(5), slot=lambda: z(5), q=lambda: f(5, 256), pos=lambda: z(5),
+                           freq=lambda: torch.ones(32, dtype=torch.float64), q_out=lambda: f(5, 256)),
+               attend=dict(q=lambda: f(5, 256), table=lambda: z(3, 4), lens=lambda: z(3), first=lambda: z(4), visible=lambda: torch.zeros(5, 1, dtype=torch.int64),
+                           out=lambda: f(5, 256)),
+               keep=dict(table=lambda: z(3, 4), lens=lambda: z(3), first=lambda: z(4), path=lambda: z(3, 4), n_keep=lambda: z(3)),
+               logits=dict(logits=lambda: f(5, 100), first=lambda: z(4), tokens=lambda: z(3, 9), n_token=lambda: z(3), n_prompt=lambda: z(3), repetition=lambda: f(3),
+                           presence=lambda: f(3), frequency=lambda: f(3), draft=lambda: z(5), visible=lambda: torch.zeros(5, 1, dtype=torch.int64), bias_ids=lambda: z(3, 2),
+                           bias=lambda: f(3, 2), mask=lambda: z(2, 4), mask_row=lambda: z(5), out=lambda: f(5, 100)))
+
+
+@pytest.mark.parametrize("call, name", [(c, n) for c, names in WITHOUT.items() for n in names])
+def test_tensors_whose_memory_was_freed(no_device, lib, call, name):  # noqa: F811
+    """All of it, the last byte of it, and a view's that begins behind it: none is taken for an array that is not given."""
+    make = WITHOUT[call][name]
+    whole = make()
+    behind = torch.cat([whole, make()])[whole.shape[0]:]
+    for t, left in ((whole, 0), (make(), whole.numel() * whole.element_size() - 1), (behind, 0), (torch.cat([make(), make()])[whole.shape[0]:], whole.numel() * whole.element_size())):
+        t = _shrunk(t, left)
+        with pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+            GOOD[call](_cache(), **{name: t})
+        with torch.no_grad(), pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+            GOOD[call](_cache(), **{name: t})
+    with pytest.raises(ValueError, match="mask: a tensor without memory"):
+        ops.adjust_logits(f(2, 100), mask=_shrunk(z(2, 4), 0))
+    assert not no_device
+
+
+@pytest.mark.parametrize("name", ["keys", "values"])
+def test_caches_whose_memory_was_freed(no_device, lib, name):  # noqa: F811
+    """Before the object is made, or afterwards: neither its address nor its sizes are kept."""
+    shape = (2, 10, 2, 16, 64)
+    good = {"keys": f(*shape), "values": f(*shape)}
+    with pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+        ops.PagedCache(**{**good, name: _shrunk(f(*shape), 0)})
+    for left in (0, 2 * 10 * 2 * 16 * 64 * 4 - 1):
+        for both in (f(*shape), f(2, *shape)[1]):
+            cache = ops.PagedCache(**{**good, name: both})
+            _shrunk(both, left)
+            for call in ("append", "attend", "keep"):
+                with pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+                    GOOD[call](cache)
+    t = f(*shape)
+    cache = ops.PagedCache(**{**good, name: t})
+    t.resize_(1, 10, 2, 16, 64)
+    for call in ("append", "attend", "keep"):
+        with pytest.raises(ValueError, match=f"{name}: "):
+            GOOD[call](cache)
+    assert not no_device
