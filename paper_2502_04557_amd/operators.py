@@ -107,8 +107,18 @@ def _number(name, v):
 _written = torch.autograd.graph.increment_version          # what autograd has kept of a tensor that is written in place is out of date
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _memory(name, t):
+    """The address of `t`, whose storage may have been freed, or a part of it (no address would stand for no tensor)."""
+    at = t.data_ptr()
+    if t.numel() > 0:
+        last = t.storage_offset() + sum((n - 1) * d for n, d in zip(t.shape, t.stride()))
+        if at == 0 or (last + 1) * t.element_size() > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: a tensor without memory")
+    return at
+
+
+def _ptr(name, t):
+    return None if t is None else _memory(name, t)
 
 
 @lru_cache(maxsize=256)
@@ -136,7 +146,7 @@ def route(logits, top_k, *, score="softmax", bias=None, n_group=1, top_group=1, 
     n = max(0, top_k + n_shared)
     ids = torch.empty(T, n, dtype=torch.int32, device=dev)
     weights = torch.empty(T, n, dtype=torch.float32, device=dev)
-    _call("sprinter_route", dev, cfg[1], logits.data_ptr(), logits.stride(0), _ptr(bias), T, ids.data_ptr(), weights.data_ptr())
+    _call("sprinter_route", dev, cfg[1], logits.data_ptr(), logits.stride(0), _ptr("bias", bias), T, ids.data_ptr(), weights.data_ptr())
     return ids, weights
 
 
@@ -236,6 +246,7 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
     gate_row = gate_col = 0
     if gate is not None:
         _tensor("gate", gate, dev, torch.float32)
+        _memory("gate", gate)
         try:
             gate = gate.expand(T, d)
         except RuntimeError as e:
@@ -247,8 +258,8 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
     else:
         h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
     out = torch.empty(T, d, dtype=y.dtype, device=dev)
-    _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr(post_gain), _ptr(post_offset),
-          _ptr(gate), gate_row, gate_col, gain.data_ptr(), _ptr(offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
+    _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr("post_gain", post_gain), _ptr("post_offset", post_offset),
+          _ptr("gate", gate), gate_row, gate_col, gain.data_ptr(), _ptr("offset", offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
     if given:
         _written(h_out)
     return h_out, out
@@ -305,16 +316,6 @@ def _matrix(name, t, device, dtype, rows, cols):
 def _column(name, t, device, dtype, n):
     _whole(name, t, device, dtype, n)
     return _memory(name, t)
-
-
-def _memory(name, t):
-    """The address of `t`, whose storage may have been freed, or a part of it (no address would stand for no tensor)."""
-    at = t.data_ptr()
-    if t.numel() > 0:
-        last = t.storage_offset() + sum((n - 1) * d for n, d in zip(t.shape, t.stride()))
-        if at == 0 or (last + 1) * t.element_size() > t.untyped_storage().nbytes():
-            raise ValueError(f"{name}: a tensor without memory")
-    return at
 
 
 def _layer(v):

@@ -127,3 +127,21 @@ def test_negated_views_are_refused(no_device, lib):  # noqa: F811
             call()
     assert not no_device
     ops.block_norm(f(3, 8), f(3, 8), f(8), gate=view(3, 8).resolve_neg())
+
+
+def test_optional_tensors_whose_memory_was_freed_are_refused(no_device, lib):  # noqa: F811
+    """They have no address, which stands for an array that is not given: a bias or a gate would be left out without a word."""
+    def freed(*s):
+        t = torch.ones(*s)
+        t.untyped_storage().resize_(0)
+        return t
+
+    f = torch.ones
+    for call, name in ((lambda: ops.route(f(3, 8), 2, bias=freed(8)), "bias"), (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), gate=freed(3, 1)), "gate"),
+                       (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), offset=freed(8)), "offset"),
+                       (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), post_gain=freed(8)), "post_gain"),
+                       (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), post_gain=f(8), post_offset=freed(8)), "post_offset")):
+        with pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+            call()
+    assert not no_device
+    ops.block_norm(f(0, 8), f(0, 8), f(8), gate=f(0, 8))  # an empty one is a tensor
