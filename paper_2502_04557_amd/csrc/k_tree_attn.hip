@@ -1,6 +1,7 @@
 // HIP kernels of the attention of trees of drafted tokens over a cache in pages, for gfx950.
 #include "ops.h"
 #include "dev.h"
+#include "tree_items.h"
 #include <algorithm>
 #include <type_traits>
 
@@ -20,7 +21,6 @@ struct TreePlan {
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
   float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
 };
-constexpr int STEP = 128;
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -52,10 +52,6 @@ __device__ __forceinline__ int scan_to_lane(int v, int& all) {
   return v;
 }
 
-__device__ __forceinline__ int tree_share(const TreePlan& p, float work) {
-  // (a little more than the quotient, so that the roundings of the sum cannot make more items than there is room for)
-  return p.split ? (int)fminf(work * (1.001f / (float)p.target), 4194303.f) + 1 : 1 << 22;
-}
 __device__ __forceinline__ int tree_items(const TreeSeq& s, int parts) { return (int)min((long long)s.blocks * parts, (long long)MOST_ITEMS); }
 
 // The item of index `item`, by one wave; false: there is none.
@@ -68,7 +64,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     work += (float)x.blocks * (float)x.steps;
   }
   work = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_total(work)), 63));
-  const int share = tree_share(p, work);
+  const int share = steps_of_share(p.split, work, p.target);
   // The longest sequences first, where workgroups wait for a place and one wave holds them all.
   int from = lane;                                 // the sequence that this lane stands for
   if (p.sort) {
@@ -84,7 +80,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
   out.parts = 0;
   for (int b0 = 0; b0 < n; b0 += 64) {
     if (b0) s = tree_seq(a, b0 + lane, QB, b0 + lane < n);
-    const int parts = (s.steps + share - 1) / share, mine = tree_items(s, parts);
+    const int parts = shares(s.steps, share), mine = tree_items(s, parts);
     int all;
     const int before = base + scan_to_lane(mine, all) - mine;
     const u64 hit = __ballot(item >= before && item < before + mine);
@@ -140,11 +136,11 @@ __global__ __launch_bounds__(1024) void k_tree_plan(AttendArgs a, TreePlan p, in
   __syncthreads();
   work = 0.f;
   for (int x = 0; x < 16; ++x) work += wave_work[x];
-  const int share = tree_share(p, work);
+  const int share = steps_of_share(p.split, work, p.target);
   int base = 0;
   for (int b0 = 0; b0 < n && base < p.items; b0 += 1024) {       // (the same for all threads)
     const TreeSeq s = tree_seq(a, b0 + tid, QB, b0 + tid < n);
-    const int parts = (s.steps + share - 1) / share, mine = tree_items(s, parts);
+    const int parts = shares(s.steps, share), mine = tree_items(s, parts);
     int all;
     const int upto = scan_to_lane(mine, all);
     if (lane == 0) wave_items[w] = all;
@@ -936,10 +932,9 @@ static bool tree_whole(int type, int KVH, int n_seq, int T, long long slots) {
 
 static TreePlan tree_plan(const TreeShape& shape, int type, int dh, int H, int KVH, int n_seq, int T, long long slots, size_t& bytes, void* ws) {
   TreePlan p{};
-  p.target = std::max(1, ((shape.NW == 8 ? 256 : 512) + KVH - 1) / KVH);
-  const long long blocks = (long long)T * (H / KVH) / shape.QB + std::min(n_seq, T);   // at most
+  p.target = tree_target(KVH, shape.NW == 8 ? 256 : 512);
   const bool whole = tree_whole(type, KVH, n_seq, T, slots);
-  p.items = (int)(blocks + (whole ? 0 : p.target + 1));
+  p.items = (int)most_items(most_blocks((long long)T * (H / KVH), shape.QB, std::min(n_seq, T)), !whole, p.target);
   p.split = !whole;
   p.sort = n_seq > 1 && n_seq <= 64 && (long long)p.items * KVH > 512;
   p.planned = n_seq > 128;

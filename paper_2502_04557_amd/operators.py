@@ -243,10 +243,10 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
         _whole("post_gain", post_gain, dev, torch.float32, d)
     if post_offset is not None:
         _whole("post_offset", post_offset, dev, torch.float32, d)
-    gate_row = gate_col = 0
+    gate_at, gate_row, gate_col = None, 0, 0
     if gate is not None:
         _tensor("gate", gate, dev, torch.float32)
-        _memory("gate", gate)
+        gate_at = _memory("gate", gate)
         try:
             gate = gate.expand(T, d)
         except RuntimeError as e:
@@ -259,7 +259,7 @@ def block_norm(h, y, gain, *, offset=None, post_gain=None, post_offset=None, gat
         h_out = torch.empty(T, d, dtype=torch.float32, device=dev)
     out = torch.empty(T, d, dtype=y.dtype, device=dev)
     _call("sprinter_block_norm", dev, cfg[1], h.data_ptr(), h.stride(0), y.data_ptr(), y.stride(0), _ptr("post_gain", post_gain), _ptr("post_offset", post_offset),
-          _ptr("gate", gate), gate_row, gate_col, gain.data_ptr(), _ptr("offset", offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
+          gate_at, gate_row, gate_col, gain.data_ptr(), _ptr("offset", offset), T, h_out.data_ptr(), h_out.stride(0), out.data_ptr(), out.stride(0))
     if given:
         _written(h_out)
     return h_out, out
