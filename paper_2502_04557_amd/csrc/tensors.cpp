@@ -44,15 +44,15 @@ PyObject* vector(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
-// array(t, device, dtype, n) -> the address of a contiguous array of n elements in all
-PyObject* array(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) { PyErr_SetString(PyExc_TypeError, "array(t, device, dtype, n)"); return nullptr; }
-  const long long want = PyLong_AsLongLong(a[3]);
+// arrays(t, u, device, dtype, n) -> the addresses of two contiguous arrays of n elements each
+PyObject* arrays(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) { PyErr_SetString(PyExc_TypeError, "arrays(t, u, device, dtype, n)"); return nullptr; }
+  const long long want = PyLong_AsLongLong(a[4]);
   if (want == -1 && PyErr_Occurred()) return nullptr;
   try {
-    const at::Tensor* t = plain(a[0], a[1], a[2]);
-    if (!t || t->numel() != want || !t->is_contiguous()) return none();
-    return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t->data_ptr());
+    const at::Tensor *t = plain(a[0], a[2], a[3]), *u = t ? plain(a[1], a[2], a[3]) : nullptr;
+    if (!u || t->numel() != want || u->numel() != want || !t->is_contiguous() || !u->is_contiguous()) return none();
+    return Py_BuildValue("KK", (unsigned long long)(uintptr_t)t->data_ptr(), (unsigned long long)(uintptr_t)u->data_ptr());
   } catch (const std::exception&) {
     return none();
   }
@@ -98,7 +98,7 @@ PyObject* written(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyMethodDef methods[] = {{"vector", (PyCFunction)(void*)vector, METH_FASTCALL, "vector(t, device, dtype, n) -> address or None"},
-                         {"array", (PyCFunction)(void*)array, METH_FASTCALL, "array(t, device, dtype, n) -> address or None"},
+                         {"arrays", (PyCFunction)(void*)arrays, METH_FASTCALL, "arrays(t, u, device, dtype, n) -> two addresses or None"},
                          {"rows", (PyCFunction)(void*)rows, METH_FASTCALL, "rows(t, device, dtype, rows, cols) -> (address, distance, rows, columns) or None"},
                          {"empty", (PyCFunction)(void*)empty, METH_FASTCALL, "empty(rows, cols, dtype, device) -> a new matrix"},
                          {"written", (PyCFunction)(void*)written, METH_FASTCALL, "written(t, ...): their versions go up"},

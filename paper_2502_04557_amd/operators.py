@@ -300,9 +300,9 @@ def _no(*args):
 
 
 def _looks():
-    """Its (rows, vector, array); inside a level of forward mode, whose tangents it does not see, everything takes the checks in Python."""
+    """Its (rows, vector, arrays); inside a level of forward mode, whose tangents it does not see, everything takes the checks in Python."""
     n = _native or _asks()
-    return (n.rows, n.vector, n.array) if forward_ad._current_level < 0 else (_no, _no, _no)
+    return (n.rows, n.vector, n.arrays) if forward_ad._current_level < 0 else (_no, _no, _no)
 
 
 # What those say None of: the checks in Python, which raise, or let the uncommon (an empty tensor, one that asks for gradients where they are off) pass.
@@ -360,14 +360,11 @@ class PagedCache:
         self._shape, self._elements = shape, keys.numel()
         self._need = {}
 
-    def _arrays(self, array):
+    def _arrays(self):
         """The addresses of keys and values: theirs of this call, as their memory may have moved or gone."""
-        dev, dtype, n = self.device, self.dtype, self._elements
-        return (array(self._keys, dev, dtype, n) or self._array("keys", self._keys), array(self._values, dev, dtype, n) or self._array("values", self._values))
-
-    def _array(self, name, t):
-        _whole(name, t, self.device, self.dtype, *self._shape)
-        return _memory(name, t)
+        for name, t in (("keys", self._keys), ("values", self._values)):
+            _whole(name, t, self.device, self.dtype, *self._shape)
+        return _memory("keys", self._keys), _memory("values", self._values)
 
     @property
     def keys(self):
@@ -384,8 +381,8 @@ class PagedCache:
         [T], by default the slot), in the pairs (i, i + n / 2) ("halves") or (2 i, 2 i + 1) ("neighbours").  Rows are bfloat16 or float32, all of one
         type; what is written has the cache's.  A token of no sequence (-1) is padding.  q_out: where the turned q goes (q itself turns it in place)."""
         dev, d, i32 = self.device, self.d_head, torch.int32
-        rows, vector, array = _looks()
-        cache_keys, cache_values = self._arrays(array)
+        rows, vector, arrays = _looks()
+        cache_keys, cache_values = arrays(self._keys, self._values, dev, self.dtype, self._elements) or self._arrays()
         dtype = keys.dtype if isinstance(keys, Tensor) else None
         if dtype not in DTYPES:
             raise ValueError("keys: bfloat16 or float32 rows are needed")
@@ -428,8 +425,8 @@ class PagedCache:
         sees (sprinter_cache_attend).  scale: of the scores, by default d_head ** -0.5.  A row that sees nothing gives zeros; rows of no
         sequence are not written."""
         dev, dtype, i32 = self.device, self.dtype, torch.int32
-        rows, vector, array = _looks()
-        keys, values = self._arrays(array)
+        rows, vector, arrays = _looks()
+        keys, values = arrays(self._keys, self._values, dev, self.dtype, self._elements) or self._arrays()
         q_at, ld_q, T, width = rows(q, dev, dtype, -1, -1) or _matrix("q", q, dev, dtype, -1, -1)
         H = width // self.d_head
         if H < 1 or width != H * self.d_head:
@@ -470,8 +467,8 @@ class PagedCache:
         """Slot lens[b] + path[b, j] -> slot lens[b] + j in every layer, j < n_keep[b] (path int32 [n_seq, n], nodes in ascending order; n_keep int32
         [n_seq]): the accepted nodes become the next committed slots (sprinter_cache_keep).  lens is the caller's to advance."""
         dev, i32 = self.device, torch.int32
-        rows, vector, array = _looks()
-        keys, values = self._arrays(array)
+        rows, vector, arrays = _looks()
+        keys, values = arrays(self._keys, self._values, dev, self.dtype, self._elements) or self._arrays()
         tab, ld_tab, n_seq, n_table = rows(table, dev, i32, -1, -1) or _matrix("table", table, dev, i32, -1, -1)
         lens_at = vector(lens, dev, i32, n_seq) or _column("lens", lens, dev, i32, n_seq)
         first_at = vector(first, dev, i32, n_seq + 1) or _column("first", first, dev, i32, n_seq + 1)
