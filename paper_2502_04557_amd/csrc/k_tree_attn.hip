@@ -3,6 +3,7 @@
 #include "dev.h"
 #include "tree_items.h"
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace sprinter {
@@ -19,7 +20,7 @@ struct TreePlan {
   int split, sort, planned;                        // sequences may be split; the longest first; the items are listed before the launch
   TreeItem* list;                                  // [items] (split or planned) parts 0: there is none
   float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
-  float* ml;                                       // [items][KVH][QB][2] their maxima (base-2 units) and sums of weights
+  float* ml;                                       // [items][KVH][QB][2] the largest products q.k and the sums of weights
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -195,12 +196,21 @@ __device__ __forceinline__ unsigned seen_keys(const AttendArgs& a, u64 first, lo
   return see & there;
 }
 
-// The scores of a lane's NK keys (of one row, in p) become weights in units of the running maximum m, a base-2 exponent; l is the lane's sum of them.  The
-// maximum moves only when a score passes it by more than 2^8 (uniform: any row of the wave), so that the common block needs no exchange between lanes: weights up
-// to 2^8 cost float32 sums and bf16 pairs nothing.  masked: keys outside `bits` have weight 0.
-constexpr float LOW = -3.402823466e38f;
+// The scores of a lane's NK keys (of one row, in p) become weights; m is their running maximum, l the lane's sum of weights.  A weight is a power of 2 with the exponent
+// p c - m c, where m c stands for its rounding, as long as that is at most 2^24: the rounding is the same for all and at most 1.  Beyond (steep) it could be any
+// power, and the exponent is (p - m) c, which is 0 for the largest and finite or -infinity for every finite score.  lacks: how much less than m c a weight's exponent is taken from;
+// rescaling: what brings weights of the maximum `from` to those of `to`.
+constexpr float LOW = -3.402823466e38f, STEEP = 16777216.f;
+__device__ __forceinline__ float lacks(float m, float c) {
+  const float x = m * c;
+  return fabsf(x) > STEEP ? 0.f : fmaf(m, c, -x);
+}
+__device__ __forceinline__ float rescaling(float from, float to, float c) { return __builtin_amdgcn_exp2f((from - to) * c + (lacks(to, c) - lacks(from, c))); }
+
+// The maximum moves only when a score passes it by more than 2^8 (uniform: any row of the wave), so that the common block needs no exchange between lanes: weights
+// up to 2^8 cost float32 sums and bf16 pairs nothing.  masked: keys outside `bits` have weight 0.
 template <int NK, int N>
-__device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsigned bits, float c, float& m, float& l, f32x4 (&O)[N]) {
+__device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsigned bits, const Base2& sc, float& m, float& l, f32x4 (&O)[N]) {
   if (masked) {
 #pragma unroll
     for (int e = 0; e < NK; ++e) p[e] = bits >> e & 1 ? p[e] : -INFINITY;
@@ -208,17 +218,25 @@ __device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsign
   float mx = p[0];
 #pragma unroll
   for (int e = 1; e < NK; ++e) mx = fmaxf(mx, p[e]);
-  mx *= c;
-  if (__any(mx > m + 8.f)) {
+  float c = sc.c, mc = m * c;
+  if (__any(mx > m + sc.lag || fabsf(mc) > STEEP)) {
     const float mn = fmaxf(m, fmaxf(quarter_max(mx), LOW));   // (NaN: left out here, and in the weights below)
-    const float corr = __builtin_amdgcn_exp2f(m - mn);
+    const float corr = rescaling(m, mn, c);
     l *= corr;
 #pragma unroll
     for (int i = 0; i < N; ++i) O[i] *= corr;
     m = mn;
+    mc = m * c;
+    const bool steep = fabsf(mc) > STEEP;
+    if (__any(steep)) {
+#pragma unroll
+      for (int e = 0; e < NK; ++e) p[e] = steep ? (p[e] - m) * c : fmaf(p[e], c, -mc);
+      c = 1.f;
+      mc = 0.f;
+    }
   }
 #pragma unroll
-  for (int e = 0; e < NK; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -m));
+  for (int e = 0; e < NK; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -mc));
   if (masked) {                                    // (also where -infinity times a scale of 0 is NaN)
 #pragma unroll
     for (int e = 0; e < NK; ++e) p[e] = bits >> e & 1 ? p[e] : 0.f;
@@ -267,9 +285,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   bool row_there[QT];
   u64 first_word[QT];
   u32x4 q[QT][KF];
-  float c = a.scale * 1.4426950408889634f;
-  const unsigned flip = c < 0.f ? (HALF ? 0x80008000u : 0x80000000u) : 0u;   // (a negative scale: the queries change their sign)
-  c = fabsf(c);
+  const Base2 scale = a.scale;
+  const unsigned flip = scale.flip ? (HALF ? 0x80008000u : 0x80000000u) : 0u;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const long long i = (long long)it.block * QB + 16 * t + l16;
@@ -324,7 +341,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   };
 
   f32x4 O[QT][CPL];
-  float m_run[QT], l_run[QT];                      // maximum (base-2 units) and this lane's sum of weights
+  float m_run[QT], l_run[QT];                      // largest product q.k and this lane's sum of weights
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     m_run[t] = LOW; l_run[t] = 0.f;
@@ -378,7 +395,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
 #pragma unroll
       for (int e = 0; e < NK; ++e) p[t][e] = sc[t][e >> 2][e & 3];
       bits[t] = plain ? there : seen_keys<NK>(a, first_word[t], at_q[t], node[t], kl - it.len, there);
-      softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
+      softmax_step(p[t], !plain, bits[t], scale, m_run[t], l_run[t], O[t]);
       if constexpr (HALF) {
         split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
         split2(p[t][2], p[t][3], ph[t].y, pl[t].y);
@@ -504,8 +521,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
     m_all[t] = LOW;
     for (int x = 0; x < NW; ++x) m_all[t] = fmaxf(m_all[t], stats[x][16 * t + l16][0]);
     l_all[t] = 0.f;
-    for (int x = 0; x < NW; ++x) l_all[t] += stats[x][16 * t + l16][1] * __builtin_amdgcn_exp2f(stats[x][16 * t + l16][0] - m_all[t]);
-    const float f = __builtin_amdgcn_exp2f(m_run[t] - m_all[t]);
+    for (int x = 0; x < NW; ++x) l_all[t] += stats[x][16 * t + l16][1] * rescaling(stats[x][16 * t + l16][0], m_all[t], scale.c);
+    const float f = rescaling(m_run[t], m_all[t], scale.c);
 #pragma unroll
     for (int i = 0; i < CPL; ++i) O[t][i] *= f;
   }
@@ -652,9 +669,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   bool row_there[QT];
   u64 first_word[QT];
   u32x4 q[QT][KF];
-  float c = a.scale * 1.4426950408889634f;
-  const unsigned flip = c < 0.f ? 0x80008000u : 0u;
-  c = fabsf(c);
+  const Base2 scale = a.scale;
+  const unsigned flip = scale.flip ? 0x80008000u : 0u;
   const long long r0 = (long long)it.block * QB + 16 * QT * w;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -731,7 +747,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[t][e] = sc[t][e >> 2][e & 3];
       bits[t] = plain ? there : seen_keys<8>(a, first_word[t], at_q[t], node[t], kl - it.len, there);
-      softmax_step(p[t], !plain, bits[t], c, m_run[t], l_run[t], O[t]);
+      softmax_step(p[t], !plain, bits[t], scale, m_run[t], l_run[t], O[t]);
       split2(p[t][0], p[t][1], ph[t].x, pl[t].x);
       split2(p[t][2], p[t][3], ph[t].y, pl[t].y);
       split2(p[t][4], p[t][5], ph[t].z, pl[t].z);
@@ -869,6 +885,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
   const int item = blockIdx.x / a.c.KVH;
   const TreeItem it = plan.list[item];
   if (it.parts < 2) return;
+  const float c = a.scale.c;
   const int G = a.H / a.c.KVH, kvh = blockIdx.x - item * a.c.KVH, lane = threadIdx.x & 63, first = item - it.part, parts = min(it.parts, plan.items - first);
   const int rows = (int)min((long long)QB, (long long)it.n * G - (long long)it.block * QB);
   for (int r = it.part + it.parts * wave_index(); r < rows; r += it.parts * 4) {
@@ -888,7 +905,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
     m = wave_max(m);
     for (int x0 = 0; x0 < parts; x0 += 64) {
       if (x0) ml = x0 + lane < parts ? *reinterpret_cast<const float2*>(plan.ml + at(x0 + lane) * 2) : make_float2(LOW, 0.f);
-      const float f = x0 + lane < parts ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+      const float f = x0 + lane < parts ? rescaling(ml.x, m, c) : 0.f;
       l += wave_sum(ml.y * f);
       for (int x = x0; x < min(parts, x0 + 64); x += U) {
         if (x) fetch(x);
@@ -951,6 +968,11 @@ size_t attend_workspace(int type, int dh, int H, int KVH, int n_seq, int T, long
   if (n_seq < 1 || T < 1) return 0;
   tree_plan(tree_shape(type, dh, H, KVH, n_seq, T), type, dh, H, KVH, n_seq, T, slots, bytes, nullptr);
   return bytes;
+}
+
+Base2 base2(float scale) {
+  const float c = fabsf(scale) * 1.4426950408889634f;
+  return Base2{c, 8.f / c, scale < 0.f};           // (a scale of 0: the maximum never moves)
 }
 
 void launch_cache_attend(const AttendArgs& a, void* workspace, hipStream_t s) {

@@ -254,7 +254,7 @@ int sprinter_cache_attend(const sprinter_cache_cfg* cfg, const sprinter_attend* 
   if (!aligned(x.workspace, 256)) return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace is not 256-byte aligned", who);
   if (x.workspace_bytes < need)
     return op_fail(SPRINTER_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, (size_t)x.workspace_bytes, need);
-  a.H = x.n_head; a.T = x.n_rows; a.n_words = x.n_words; a.scale = x.scale; a.lens = x.len; a.first = x.first;
+  a.H = x.n_head; a.T = x.n_rows; a.n_words = x.n_words; a.scale = base2(x.scale); a.lens = x.len; a.first = x.first;
   a.visible = (const unsigned long long*)x.visible; a.q = x.q; a.ld_q = x.ld_q; a.y = x.y; a.ld_y = x.ld_y;
   launching();
   launch_cache_attend(a, x.workspace, (hipStream_t)hip_stream);

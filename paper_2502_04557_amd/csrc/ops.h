@@ -69,10 +69,13 @@ struct KeepArgs {
   const int *lens, *first, *path, *n_keep; long long ld_path; int n_path;
 };
 void launch_cache_keep(const KeepArgs& a, hipStream_t s);
+// The scale of scores as a base-2 exponent's, the difference of products q.k that is an exponent of 8, and whether the scale is negative.
+struct Base2 { float c, lag; int flip; };
+Base2 base2(float scale);
 struct AttendArgs {
   PagedArgs c;
   int type, H, T, n_words;
-  float scale;
+  Base2 scale;
   const int *lens, *first;
   const unsigned long long* visible;             // [T][n_words], or NULL: the nodes up to the row's own
   const void* q; long long ld_q;
