@@ -14,13 +14,14 @@ namespace sprinter {
 struct TreeItem {
   int f0, n, len, b;                               // the sequence: rows f0 .. f0 + n - 1
   int block, part, parts, share;                   // block of rows, share of slots, how many of them, steps of each
+  int sums;                                        // (parts > 1) which item it is among those of split sequences
 };
 struct TreePlan {
   int target, items;                               // shares to aim for; the most items there can be (per KV head)
   int split, sort, planned;                        // sequences may be split; the longest first; the items are listed before the launch
   TreeItem* list;                                  // [items] (split or planned) parts 0: there is none
-  float* o;                                        // [items][KVH][QB][DH] sums of split sequences, not divided, and
-  float* ml;                                       // [items][KVH][QB][2] the largest products q.k and the sums of weights
+  float* o;                                        // [most_sums][KVH][QB][DH] sums of split sequences, not divided, and
+  float* ml;                                       // [most_sums][KVH][QB][2] the largest products q.k and the sums of weights
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -77,13 +78,15 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
     s.f0 = to(s.f0); s.n = to(s.n); s.len = to(s.len); s.blocks = to(s.blocks); s.steps = to(s.steps);
     from = to(lane);
   }
-  int base = 0;
+  int base = 0, base_sums = 0;
   out.parts = 0;
   for (int b0 = 0; b0 < n; b0 += 64) {
     if (b0) s = tree_seq(a, b0 + lane, QB, b0 + lane < n);
     const int parts = shares(s.steps, share), mine = tree_items(s, parts);
     int all;
-    const int before = base + scan_to_lane(mine, all) - mine;
+    const int before = base + scan_to_lane(mine, all) - mine, sums = parts > 1 ? mine : 0;
+    int before_sums = base_sums, all_sums = 0;
+    if (p.split) before_sums += scan_to_lane(sums, all_sums) - sums;
     const u64 hit = __ballot(item >= before && item < before + mine);
     if (hit) {
       const int l = __builtin_ctzll(hit);
@@ -96,9 +99,11 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const TreePlan& p
       const int i = item - __builtin_amdgcn_readlane(before, l);
       out.block = i / out.parts;
       out.part = i - out.block * out.parts;
+      out.sums = __builtin_amdgcn_readlane(before_sums, l) + i;
       break;
     }
     base += all;
+    base_sums += all_sums;
   }
   if (p.split && blockIdx.x % a.c.KVH == 0 && threadIdx.x == 0) p.list[item] = out;   // for k_tree_merge
   return out.parts > 0;
@@ -115,17 +120,17 @@ __device__ __forceinline__ bool find_item_of_block(const AttendArgs& a, const Tr
     if (threadIdx.x == 0) shared = out;
   }
   __syncthreads();
-  int v[8];
+  int v[9];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = uniform(reinterpret_cast<const int*>(&shared)[i]);
-  out = TreeItem{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  for (int i = 0; i < 9; ++i) v[i] = uniform(reinterpret_cast<const int*>(&shared)[i]);
+  out = TreeItem{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8]};
   return out.parts > 0;
 }
 
 // All items of a launch, by one workgroup: a list of as many entries as there is room for.
 __global__ __launch_bounds__(1024) void k_tree_plan(AttendArgs a, TreePlan p, int QB) {
   __shared__ float wave_work[16];
-  __shared__ int wave_items[16];
+  __shared__ int wave_items[16], wave_sums[16];
   const int tid = threadIdx.x, lane = tid & 63, w = wave_index(), n = a.c.n_seq;
   float work = 0.f;
   for (int b = tid; b < n; b += 1024) {
@@ -138,29 +143,34 @@ __global__ __launch_bounds__(1024) void k_tree_plan(AttendArgs a, TreePlan p, in
   work = 0.f;
   for (int x = 0; x < 16; ++x) work += wave_work[x];
   const int share = steps_of_share(p.split, work, p.target);
-  int base = 0;
+  int base = 0, base_sums = 0;
   for (int b0 = 0; b0 < n && base < p.items; b0 += 1024) {       // (the same for all threads)
     const TreeSeq s = tree_seq(a, b0 + tid, QB, b0 + tid < n);
-    const int parts = shares(s.steps, share), mine = tree_items(s, parts);
-    int all;
-    const int upto = scan_to_lane(mine, all);
-    if (lane == 0) wave_items[w] = all;
+    const int parts = shares(s.steps, share), mine = tree_items(s, parts), sums = parts > 1 ? mine : 0;
+    int all, all_sums;
+    const int upto = scan_to_lane(mine, all), upto_sums = scan_to_lane(sums, all_sums);
+    if (lane == 0) { wave_items[w] = all; wave_sums[w] = all_sums; }
     __syncthreads();
-    int before = base, total = base;
+    int before = base, total = base, before_sums = base_sums;
     for (int x = 0; x < 16; ++x) {
       if (x < w) before = min(before + wave_items[x], MOST_ITEMS);
       total = min(total + wave_items[x], MOST_ITEMS);
+      if (x < w) before_sums += wave_sums[x];
+      base_sums += wave_sums[x];
     }
     __syncthreads();
     base = total;
     before = min(before + (upto - mine), MOST_ITEMS);
+    before_sums += upto_sums - sums;
     for (u64 some = __ballot(mine > 0 && before < p.items); some; some &= some - 1) {   // a sequence's items by the whole wave
       const int l = __builtin_ctzll(some), from = __builtin_amdgcn_readlane(before, l), count = min(__builtin_amdgcn_readlane(mine, l), p.items - from);
       TreeItem it{__builtin_amdgcn_readlane(s.f0, l), __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.len, l), b0 + 64 * w + l, 0, 0,
-                  __builtin_amdgcn_readlane(parts, l), share};
+                  __builtin_amdgcn_readlane(parts, l), share, 0};
+      const int from_sums = __builtin_amdgcn_readlane(before_sums, l);
       for (int x = lane; x < count; x += 64) {
         it.block = x / it.parts;
         it.part = x - it.block * it.parts;
+        it.sums = from_sums + x;
         p.list[from + x] = it;
       }
     }
@@ -554,7 +564,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
 #pragma unroll
       for (int i = 0; i < CPL; ++i) x[CPL * r + i] = l_all[t] == 0.f ? 0.f : O[t][i][r] * inv;
     if (it.parts > 1) {
-      const long long at = (long long)blockIdx.x * QB + 16 * t + l16;
+      const long long at = ((long long)it.sums * a.c.KVH + kvh) * QB + 16 * t + l16;
       float* dst = plan.o + at * DH + 4 * CPL * lq;
 #pragma unroll
       for (int i = 0; i < 4 * CPL; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
@@ -858,7 +868,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
     if (!row_there[t]) continue;
     const int i = (int)(16 * QT * w + 16 * t + l16);
     if (it.parts > 1) {
-      const long long at = (long long)blockIdx.x * QB + i;
+      const long long at = ((long long)it.sums * a.c.KVH + kvh) * QB + i;
 #pragma unroll
       for (int x = 0; x < CT; ++x) {
         const f32x4 o = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t][x];
@@ -886,7 +896,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(AttendArgs a, TreePlan plan,
   const TreeItem it = plan.list[item];
   if (it.parts < 2) return;
   const float c = a.scale.c;
-  const int G = a.H / a.c.KVH, kvh = blockIdx.x - item * a.c.KVH, lane = threadIdx.x & 63, first = item - it.part, parts = min(it.parts, plan.items - first);
+  const int G = a.H / a.c.KVH, kvh = blockIdx.x - item * a.c.KVH, lane = threadIdx.x & 63, first = it.sums - it.part, parts = min(it.parts, plan.items - (item - it.part));
   const int rows = (int)min((long long)QB, (long long)it.n * G - (long long)it.block * QB);
   for (int r = it.part + it.parts * wave_index(); r < rows; r += it.parts * 4) {
     auto at = [&](int part) { return ((long long)(first + part) * a.c.KVH + kvh) * QB + r; };
@@ -955,7 +965,7 @@ static TreePlan tree_plan(const TreeShape& shape, int type, int dh, int H, int K
   p.split = !whole;
   p.sort = n_seq > 1 && n_seq <= 64 && (long long)p.items * KVH > 512;
   p.planned = n_seq > 128;
-  const size_t rows = whole ? 0 : (size_t)p.items * KVH * shape.QB;
+  const size_t rows = (size_t)most_sums(p.items, p.split, p.target) * KVH * shape.QB;
   bytes = rows * (dh + 2) * sizeof(float) + (whole && !p.planned ? 0 : p.items * sizeof(TreeItem));
   p.o = (float*)ws;
   p.ml = p.o + rows * dh;

@@ -22,5 +22,8 @@ constexpr int tree_target(int KVH, int workgroups) { return (workgroups + KVH - 
 // The most blocks of rows there can be (rows: nodes x heads of a KV head; sequences: those with a node at most), and the most items.
 constexpr long long most_blocks(long long rows, int QB, long long sequences) { return rows / QB + sequences; }
 constexpr long long most_items(long long blocks, bool split, int target) { return blocks + (split ? target + 1 : 0); }
+// The most items that leave sums to be merged, those of sequences of two shares or more: these have fewer than 2 steps / share each, and a share is more than a
+// target-th of all steps.
+constexpr long long most_sums(long long items, bool split, int target) { return !split ? 0 : items < 2ll * target ? items : 2ll * target; }
 
 }  // namespace sprinter

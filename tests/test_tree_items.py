@@ -1,6 +1,9 @@
 """The items of a launch of the attention of drafted trees against the room that the host leaves for them, up to the limits of its arguments, on the CPU."""
+import ctypes as C
 import os
 import subprocess
+import pytest
+from test_abi_cpu import lib  # noqa: F401
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_04557_amd", "csrc")
 
@@ -14,7 +17,7 @@ struct Seq { int nodes; long long slots; };
 
 // as the kernels do: blocks and steps of each sequence, the work as a float32 sum
 bool fits(const std::vector<Seq>& batch, int G, int QB, int KVH, int workgroups, bool split) {
-  long long rows = 0, items = 0;
+  long long rows = 0, items = 0, sums = 0;
   float work = 0;
   auto blocks = [&](const Seq& s) { return (int)(((long long)s.nodes * G + QB - 1) / QB); };
   auto steps = [&](const Seq& s) { const long long n = (s.slots + STEP - 1) / STEP; return (int)(n > 1 ? n : 1); };
@@ -26,6 +29,7 @@ bool fits(const std::vector<Seq>& batch, int G, int QB, int KVH, int workgroups,
   for (const Seq& s : batch) {
     const int parts = shares(steps(s), share);
     items += (long long)blocks(s) * parts;
+    sums += parts > 1 ? (long long)blocks(s) * parts : 0;
     if (!split && parts != 1) return std::printf("split: %lld slots\n", s.slots), false;
     // every step is in a share, none is empty, and no slot of a share passes 31 bits
     if ((long long)parts * share < steps(s) || (long long)(parts - 1) * share >= steps(s) || ((long long)(parts - 1) * share + share) * STEP >= 1ll << 31)
@@ -35,6 +39,7 @@ bool fits(const std::vector<Seq>& batch, int G, int QB, int KVH, int workgroups,
   if (items > room)
     return std::printf("%zu sequences, first %d nodes, %lld slots, %d heads each of %d, blocks of %d: %lld items, room for %lld\n", batch.size(), batch[0].nodes, batch[0].slots, G,
                        KVH, QB, items, room), false;
+  if (sums > most_sums(room, split, target)) return std::printf("%zu sequences: %lld sums, room for %lld\n", batch.size(), sums, most_sums(room, split, target)), false;
   return true;
 }
 
@@ -71,3 +76,18 @@ def test_there_is_room_for_every_item(tmp_path):
     assert r.returncode == 0, r.stderr
     r = subprocess.run([str(tmp_path / "items")], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout
+
+
+@pytest.mark.parametrize("dtype, H, KVH, dh, n_seq, slots, T, most", [
+    (1, 32, 32, 128, 1024, 4096, 1024, 9 << 20),          # decode steps of a large batch
+    (1, 32, 8, 128, 1, 1 << 17, 4096, 72 << 20),          # a piece of a prompt
+    (1, 64, 8, 128, 1 << 17, 1 << 20, 1 << 17, 96 << 20), # the most rows
+    (0, 1, 1, 128, 1 << 20, 1 << 20, 1 << 20, 96 << 20),
+    (1, 32, 8, 128, 64, 2048, 4096, 0)])                  # sequences that are not split
+def test_sums_of_split_sequences_alone_take_workspace(lib, dtype, H, KVH, dh, n_seq, slots, T, most):  # noqa: F811
+    """Twice as many items as the launch aims for leave sums at most, however large the batch is: 2 x 512 x 256 rows x 130 x 4 bytes, and the list of items."""
+    from paper_2502_04557_amd import operators as ops
+    n = C.c_size_t(0)
+    cfg = ops.CacheCfgC(dtype, 1, 1 << 20, 16, KVH, dh)
+    assert lib.sprinter_cache_attend_bytes(C.byref(cfg), H, n_seq, slots // 16, T, C.byref(n)) == 0
+    assert n.value <= most
