@@ -65,3 +65,133 @@ def test_scores_around_two_to_the_24(dtype, lens, nodes, H, KVH, dh, page):
         bound = (2 * (2.0 ** -16 if half else 0.0) + 2 * 26 * 2.0 ** -20 + (2 * n + 16) * M.F32) * float(b.values.abs().max()) + (M.B16 if half else M.F32) * want.abs()
         good = bool(mine.all() and ((y - want).abs() <= bound).all())
         assert good, float((y - want).abs().max())
+
+
+# --------------------------------------------------------------------------------------- plans and variants of larger calls
+def _check(b, visible=None, scale=None, small=True):
+    """b's call against float64 on the GPU, with the bounds of tree_math.attend, sequence by sequence.  small: queries and keys of a few units, whose scores leave little."""
+    y = b.cache.attend(0, b.q, b.table, b.lens, b.first, visible=visible, scale=scale).double().reshape(b.T, b.KVH, -1, b.dh)
+    scale = b.dh ** -0.5 if scale is None else scale
+    half, F, INF = b.dtype == torch.bfloat16, M.F32, float("inf")
+    lens, first, G, t, off, norm = b.lens.tolist(), b.first.tolist(), b.H // b.KVH, b.table.long(), 0.0, 0.0
+    for s, l in enumerate(lens):
+        n = first[s + 1] - first[s]
+        if n == 0:
+            continue
+        slots = torch.arange(min(l + n, b.table.shape[1] * b.page), device=DEV)
+        pages = t[s, slots // b.page]
+        there = (pages >= 0) & (pages < b.keys.shape[1])
+        pages = torch.where(there, pages, 0)
+        node, j = torch.arange(n, device=DEV)[:, None], slots[None] - l
+        rows = slice(first[s], first[s + 1])
+        if visible is None:
+            seen = j <= node
+        else:
+            w = visible[rows].shape[1]
+            word = visible[rows].gather(1, (j.clamp(min=0) // 64).clamp(max=w - 1).expand(n, -1))
+            seen = (j < 0) | ((j < 64 * w) & ((word >> (j.clamp(min=0) % 64)) & 1 == 1))
+        seen = (seen & there).repeat_interleave(G, 0)                     # [n G, slots]
+        for h in range(b.KVH):
+            k, v = (torch.where(there[:, None], a[0, pages, h, slots % b.page].double(), 0.0) for a in (b.keys, b.values))
+            q = b.q.reshape(b.T, b.H, b.dh)[rows, h * G:(h + 1) * G].double().reshape(n * G, b.dh)
+            kt = k.t().contiguous()
+            x = (scale * (q @ kt)).masked_fill(~seen, -INF)
+            ds = (abs(scale) * (b.dh + 6) * F * (q.abs() @ kt.abs())).masked_fill(~seen, 0.0)
+            top = x.amax(1, keepdim=True)
+            dead = top == -INF
+            top = torch.where(dead, 0.0, top)
+            p = torch.exp(x - top)
+            e = torch.where(p > 0, ds + ds.amax(1, keepdim=True) + 4 * F * torch.where(seen, x.abs() + top.abs(), 0.0) + 16 * F, 0.0)
+            total = torch.where(dead, 1.0, p.sum(1, keepdim=True))
+            want, size = p @ v / total, p @ v.abs() / total
+            wrong = (p * e) @ v.abs() / total + size * (p * e).sum(1, keepdim=True)
+            lost = ((2.0 ** -16 if half else 0.0) + (2 * seen.sum(1, keepdim=True) + 16) * F) * size
+            bound = wrong + lost + (M.B16 if half else F) * (want.abs() + wrong + lost) + 1e-38
+            d = (y[rows, h].reshape(n * G, b.dh) - want).abs()
+            good = bool((d <= bound).all())
+            assert good, (s, h, float((d - bound).max()), torch.nonzero(~(d <= bound))[:3].tolist())
+            off, norm = off + float((d * d).sum()), norm + float((want * want).sum())
+    # In the mean: bf16, the result's rounding.  float32: weights 2^-8 of the largest and more, whose exponents span 8, have errors of 1.5 x 2^-24 x 8 (the scale's two
+    # roundings), 2^-22 (the exponent's), 2^-22 (the product's, of 64 or 128 terms) and 2^-23 (the exponential's), together below 2^-19, and so has a sum of values of any sign
+    if small:
+        assert off ** 0.5 <= (M.B16 if half else 2.0 ** -19) * norm ** 0.5, (off / max(norm, 1e-300)) ** 0.5
+    return y
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("H", [16, 32, 64])
+@pytest.mark.parametrize("page, low", [(8, 480), (8, 600), (16, 900)])
+def test_attend_whole_sequences_over_many_pages(dh, H, page, low):
+    """More pages than a wave has lanes, in one item: 64, 128 or 256 rows that share their keys; pages that are not there around the 64th and near the end."""
+    lens = [low + 61 * i % (1000 - low) for i in range(16)]
+    b = Batch(low + H, "bf16", lens, [24 - i % 3 for i in range(16)], H, 8, dh, page)
+    assert b.table.shape[1] * page <= 1024                # (whole: 128 pairs of sequence and KV head of up to 1024 slots)
+    _check(b)
+    _check(b, b.seen())
+    for s, gone in enumerate(([63], [64], [61, 62, 63, 64, 65], [0, 63, 64], [66], list(range(58, 64)), [127], [60, 65, 124])):
+        for i in gone:
+            b.table[s, min(i, b.table.shape[1] - 1)] = -1
+    _check(b)
+    _check(b, b.seen())
+
+
+@pytest.mark.parametrize("dh, H, nodes, page", [(128, 8, 24, 8), (64, 8, 24, 16), (128, 4, 20, 8), (64, 20, 24, 8), (128, 16, 20, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_shares_of_many_steps(dtype, dh, H, nodes, page):
+    """Contexts of up to 40001 slots whose shares are several steps long, many groups of 64 pages each; some of the pages are not there."""
+    b = Batch(H + dh, dtype, [9000, 40001, 23456, 12000], [nodes, nodes - 3, nodes, nodes - 1], H, 2, dh, page)
+    _check(b)
+    b.table[:, ::37] = -1
+    b.table[1, 1000:1130] = b.keys.shape[1]
+    _check(b, b.seen())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, H, KVH, dh, most, longest", [(129, 4, 2, 64, 20, 900), (130, 6, 3, 128, 40, 700), (150, 16, 2, 64, 25, 800), (140, 4, 2, 128, 25, 5000),
+                                                          (135, 12, 3, 64, 30, 6000), (130, 16, 2, 128, 30, 4000), (200, 8, 8, 128, 1, 3000), (1024, 4, 4, 64, 1, 9000)])
+def test_attend_many_sequences_of_several_heads(dtype, n, H, KVH, dh, most, longest):
+    """Items that are listed before the launch: blocks of 16 to 256 rows, whole and split, most sequences shorter than a share."""
+    g = np.random.default_rng(n)
+    lens, nodes = g.integers(0, 300, n), g.integers(max(1, most - 4), most + 1, n)
+    lens[[0, n // 2, n - 1]], nodes[3] = longest, 0
+    b = Batch(n + dh, dtype, lens.tolist(), nodes.tolist(), H, KVH, dh, 16)
+    _check(b)
+    _check(b, b.seen())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_float32_in_the_mean(dtype):
+    """Small batches of both kernels of few rows."""
+    for lens, nodes, H, KVH, dh in (([40, 127, 90], [5, 5, 4], 8, 8, 64), ([700, 300], [9, 12], 8, 4, 64), ([1500], [20], 4, 2, 128)):
+        b = Batch(sum(lens), dtype, lens, nodes, H, KVH, dh, 16)
+        _check(b)
+        _check(b, b.seen())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, V, L", [(90, 50257, 300), (700, 50257, 60), (330, 24593, 200)])
+def test_logits_in_several_slices(dtype, rows, V, L):
+    """Rows past the caches, cut into slices of the vocabulary, one or several rows of a workgroup: tokens, biases and masks on both sides of the slices' borders."""
+    g = np.random.default_rng(rows)
+    nodes = []
+    while sum(nodes) < rows:
+        nodes.append(int(min(g.integers(0, 9), rows - sum(nodes))))
+    logits, first, kw = _logits_case(V, dtype, len(nodes), nodes, V, L, 40)
+    slices = -(-V // 6144)
+    slice_ = -(-(-(-V // slices)) // 32) * 32
+    edges = np.array([e + d for e in range(0, V + 1, slice_) for d in (-33, -2, -1, 0, 1, 31, 32)])
+    edges = np.append(edges, [V - 1, V - 2, V])
+    for name in ("tokens", "draft", "bias_ids"):
+        a = kw[name]
+        kw[name] = np.where(g.random(a.shape) < 0.3, edges[g.integers(0, len(edges), a.shape)], a).astype(np.int32)
+    half = dtype == "bf16"
+    want = _check_logits(logits, first, kw, half)
+    dev = {k: torch.from_numpy(v).to(DEV) for k, v in kw.items()}
+    x, f = logits.to(DEV), torch.from_numpy(first).to(DEV)
+    assert _ops().adjust_logits(x, f, out=x, **dev) is x and torch.equal(x, want)
+    wide = torch.full((rows, V + 9), 3.0, dtype=TYPES[dtype], device=DEV)
+    wide[:, 5:V + 5] = logits.to(DEV)
+    out = torch.full((rows, V + 6), 3.0, dtype=TYPES[dtype], device=DEV)
+    assert torch.equal(_ops().adjust_logits(wide[:, 5:V + 5], f, out=out[:, 3:V + 3], **dev), want)
+    assert (out[:, :3] == 3).all() and (out[:, V + 3:] == 3).all()
+    _check_logits(logits, first, {k: kw[k] if k in ("draft", "visible", "frequency", "mask", "mask_row") else None for k in kw}, half)
