@@ -1,6 +1,7 @@
 """Builds libsprinter.so (HIP kernels + C ABI) in-tree for gfx950 with hipcc."""
 from __future__ import annotations
 import os
+import shutil
 import subprocess
 import sys
 
@@ -28,7 +29,22 @@ def _run(cmd, verbose):
     if out.strip() and verbose:
         print(out, flush=True)
     if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+        raise RuntimeError(f"{cmd[0]} failed:\n" + out)
+
+
+def tensors_lack() -> str:
+    """What the extension of the torch entry points needs and is not here; callers of the C library need hipcc alone."""
+    import sysconfig
+    if shutil.which("g++") is None:
+        return "g++"
+    try:
+        from torch.utils import cpp_extension
+    except ImportError:
+        return "torch"
+    for where, name in (([sysconfig.get_paths()["include"]], "Python.h"), (cpp_extension.include_paths(), os.path.join("torch", "extension.h"))):
+        if not any(os.path.exists(os.path.join(p, name)) for p in where):
+            return name
+    return ""
 
 
 def build_tensors(verbose: bool = True) -> None:
@@ -42,16 +58,22 @@ def build_tensors(verbose: bool = True) -> None:
 
 
 def build_library(verbose: bool = True) -> str:
-    """Every source is compiled (in parallel) on each call, then linked into the shared library."""
+    """Every source is compiled (in parallel) on each call, then linked into the shared library.  The extension is left out, with a word, where what it needs is not here."""
     from concurrent.futures import ThreadPoolExecutor
+    lack = tensors_lack()
+    if lack:
+        print(f"no {lack}: _tensors.so, which the cache in pages and the adjustments of logits need on torch tensors, is not built", flush=True)
+        if os.path.exists(TENSORS):
+            os.remove(TENSORS)                           # (of other sources)
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
     objs = [os.path.join(objdir, s + ".o") for s in SOURCES]
     cmds = [["hipcc", *FLAGS, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
     with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
-        tensors = ex.submit(build_tensors, verbose)
+        tensors = None if lack else ex.submit(build_tensors, verbose)
         list(ex.map(lambda c: _run(c, verbose), cmds))
-        tensors.result()
+        if tensors:
+            tensors.result()
     _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], verbose)
     # the Python-free runner of dumped workloads (hardware-counter runs); it only uses the public C ABI
     _run(["hipcc", *FLAGS, "-x", "hip", os.path.join(CSRC, "native_bench.cpp"), "-L" + PKG, "-lsprinter",
