@@ -37,23 +37,26 @@ __device__ __forceinline__ int row_sequence(const int* first, int n_seq, int n_r
 
 // A workgroup takes `slice` tokens of the vocabulary of `per` rows one after the other.  What the history says of those tokens is counted once for all of its
 // rows of one sequence; the tokens of a row's path are added for the row and taken out again.  Reads and writes 16 bytes a lane whatever the rows'
-// alignment; all but a few words are 0, and their logits go through as they are.  Bound by HBM: 448 rows of 128256 float32, 460 MB in 104 us = 4.4 TB/s, of the 4.7
+// alignment; all but a few words are 0, and their logits go through as they are.  Bound by HBM: 448 rows of 128256 float32, 460 MB in 103 us = 4.5 TB/s, of the 4.7
 // that a large copy reaches; counting 2000 tokens of history for every third row is 8 us of them.
-// MANY: past the caches, 8 pieces a thread on their way (through them, 4 pieces: 129 us); else the logits stay in L2 for who draws from them.
+// MANY: past the caches (through them, 129 us), slices of up to MANY_SLICE tokens, all of a thread's pieces of a row on their way at once (6 in float32, 3 in bf16); else one
+// piece a thread, and the logits stay in L2 for who draws from them.
+constexpr int MANY_SLICE = 6144;
 template <typename T, bool MANY>
 __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int slice, int per) {
   extern __shared__ unsigned word[];               // [slice]
-  constexpr int VEC = 16 / sizeof(T), UNROLL = MANY ? 8 : 4, RUN = 256 * VEC;
+  constexpr int VEC = 16 / sizeof(T), RUN = 256 * VEC, UNROLL = MANY ? MANY_SLICE / RUN : 1;   // pieces of a thread: slice <= UNROLL * RUN
+  static_assert(MANY_SLICE % RUN == 0, "whole pieces");
   using Vec = std::conditional_t<sizeof(T) == 4, Vec4, Vec2>;
   const int tid = threadIdx.x, v0 = blockIdx.y * slice, n = min(slice, a.vocab - v0), whole = n / VEC * VEC, t1 = min((int)(blockIdx.x + 1) * per, a.n_rows);
   int now = -2, b = -1, f0 = 0, f1 = 0;            // the sequence that the words are of
   float rep = 1.f, pre = 0.f, freq = 0.f;
   Vec x[UNROLL];
-  auto fetch = [&](const T* in, int i0) {
+  auto fetch = [&](const T* in) {
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const int i = i0 + u * RUN;
-      if (i >= whole) break;
+      const int i = tid * VEC + u * RUN;
+      if (i >= whole) continue;
       if constexpr (MANY) x[u] = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(in + i));
       else x[u] = *reinterpret_cast<const Vec*>(in + i);
     }
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int sl
         if (v >= v0 && v - v0 < n) atomicAdd(&word[v - v0], by);
       }
   };
-  fetch((const T*)a.logits + (long long)blockIdx.x * per * a.ld_logits + v0, tid * VEC);   // (on its way while the tokens are counted)
+  fetch((const T*)a.logits + (long long)blockIdx.x * per * a.ld_logits + v0);   // (on its way while the tokens are counted)
   for (int t = blockIdx.x * per; t < t1; ++t) {
     const T* in = (const T*)a.logits + t * a.ld_logits + v0;
     T* out = (T*)a.out + t * a.ld_out + v0;
@@ -123,34 +126,31 @@ __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int sl
       }
       return allowed ? y : -INFINITY;
     };
-    for (int i0 = tid * VEC; i0 < whole; i0 += UNROLL * RUN) {
-      if (i0 != tid * VEC) fetch(in, i0);
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int i = i0 + u * RUN;
-        if (i >= whole) break;
-        unsigned w[VEC], any = 0;
+    for (int u = 0; u < UNROLL; ++u) {
+      const int i = tid * VEC + u * RUN;
+      if (i >= whole) continue;
+      unsigned w[VEC], any = 0;
 #pragma unroll
-        for (int e = 0; e < VEC; e += 4) *reinterpret_cast<uint4*>(&w[e]) = *reinterpret_cast<const uint4*>(&word[i + e]);
+      for (int e = 0; e < VEC; e += 4) *reinterpret_cast<uint4*>(&w[e]) = *reinterpret_cast<const uint4*>(&word[i + e]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) any |= w[e];
-        const unsigned allowed = mask ? (unsigned)mask[(v0 + i) >> 5] >> ((v0 + i) & 31) : 0xffffffffu;
-        if (any || mask) {                         // (what no step touches keeps its bits)
+      for (int e = 0; e < VEC; ++e) any |= w[e];
+      const unsigned allowed = mask ? (unsigned)mask[(v0 + i) >> 5] >> ((v0 + i) & 31) : 0xffffffffu;
+      if (any || mask) {                         // (what no step touches keeps its bits)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const bool touched = w[e] || !(allowed >> e & 1);
-            if constexpr (sizeof(T) == 4) {
-              if (touched) x[u][e] = __float_as_uint(adjusted(__uint_as_float(x[u][e]), w[e], allowed >> e & 1));
-            } else if (touched) {
-              const unsigned sh = 16 * (e & 1);
-              const unsigned y = f2bf(adjusted(__uint_as_float(x[u][e >> 1] >> sh << 16), w[e], allowed >> e & 1));
-              x[u][e >> 1] = (x[u][e >> 1] & ~(0xffffu << sh)) | y << sh;
-            }
+        for (int e = 0; e < VEC; ++e) {
+          const bool touched = w[e] || !(allowed >> e & 1);
+          if constexpr (sizeof(T) == 4) {
+            if (touched) x[u][e] = __float_as_uint(adjusted(__uint_as_float(x[u][e]), w[e], allowed >> e & 1));
+          } else if (touched) {
+            const unsigned sh = 16 * (e & 1);
+            const unsigned y = f2bf(adjusted(__uint_as_float(x[u][e >> 1] >> sh << 16), w[e], allowed >> e & 1));
+            x[u][e >> 1] = (x[u][e >> 1] & ~(0xffffu << sh)) | y << sh;
           }
         }
-        if constexpr (MANY) __builtin_nontemporal_store(x[u], reinterpret_cast<Vec*>(out + i));
-        else *reinterpret_cast<Vec*>(out + i) = x[u];
       }
+      if constexpr (MANY) __builtin_nontemporal_store(x[u], reinterpret_cast<Vec*>(out + i));
+      else *reinterpret_cast<Vec*>(out + i) = x[u];
     }
     if (whole + tid < n) {                         // (the last few of the vocabulary)
       const int i = whole + tid;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int sl
       out[i] = y;
     }
     if (t + 1 < t1) {
-      fetch(in + a.ld_logits, tid * VEC);
+      fetch(in + a.ld_logits);
       __syncthreads();                             // (this row's words have been read)
     }
   }
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int sl
 void launch_adjust_logits(const sprinter_logits& a, hipStream_t s) {
   const int run = a.dtype == SPRINTER_F32 ? 1024 : 2048;
   const bool many = (long long)((a.vocab + run - 1) / run) * a.n_rows > 2048;
-  const int slices = many ? (a.vocab + 6143) / 6144 : (a.vocab + run - 1) / run, slice = many ? round_up((a.vocab + slices - 1) / slices, 32) : run;
+  const int slices = many ? (a.vocab + MANY_SLICE - 1) / MANY_SLICE : (a.vocab + run - 1) / run, slice = many ? round_up((a.vocab + slices - 1) / slices, 32) : run;
   const int per = (int)std::max(1ll, std::min(8ll, (long long)slices * a.n_rows / 2048));
   const dim3 grid((a.n_rows + per - 1) / per, slices);
   auto go = [&](auto type) {
