@@ -442,7 +442,7 @@ int sprinter_cache_append(const sprinter_cache_cfg* cfg, const sprinter_append* 
 /* y[t, h] = sum over the slots j that row t sees of softmax_j(scale q[t, h] . key_j) value_j, with the keys and values of KV head h / (n_head /
  * n_kv_head): the committed slots of t's sequence and its visible nodes, as far as they are there.  q and y [n_rows, n_head * d_head] have the cache's dtype, rows 16-byte
  * aligned.  A product q . key is float32; times scale it may be any number, also one beyond float32.  A score of -infinity has no weight; a row that sees nothing, or nothing else, gives zeros.  What a row does not see does not reach
- * it, not as infinity or NaN either.  float32: float32 throughout.  bf16: products of bf16 with float32 sums, the weights of the values as two
+ * it, not as infinity or NaN either; an infinity that it sees is its result.  Sums are divided at their end: values from 2^119 / (its slots) on may make them infinite.  float32: float32 throughout.  bf16: products of bf16 with float32 sums, the weights of the values as two
  * bf16 each (16 bits), statistics float32.  The same call gives the same bits.  workspace: sprinter_cache_attend_bytes, 256-byte aligned, in use
  * until the call's work is done (0 bytes: may be NULL). */
 typedef struct {

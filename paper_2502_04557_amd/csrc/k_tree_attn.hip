@@ -261,6 +261,40 @@ __device__ __forceinline__ void softmax_step(float (&p)[NK], bool masked, unsign
   l += s[0];
 }
 
+// An infinity among the committed values meets the two halves of a weight in bf16, the second of which may be 0 or negative: NaN, and so do sums of x[N], columns `col` of
+// a row, whose sum of weights is l.  Where they are not finite (rare), what the row sees of infinities and NaN among the slots k0 .. end - 1 takes their place: weights are
+// positive, so its plain sum has the value.  By a whole wave whose lanes with one lane / 16 have the same columns.
+template <int N, typename Col>
+__device__ __forceinline__ void take_infinities(const AttendArgs& a, const TreeItem& it, int kvh, int k0, int end, long long row, int node, float l, Col col, float (&x)[N]) {
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) z = fmaf(x[i], 0.f, z);
+  if (!__any(z != z)) return;
+  float sum[N] = {};
+  auto add = [&](int s, bool sees) {
+    const int page = a.c.table[(long long)it.b * a.c.ld_table + (s >> a.c.shift)];
+    if (!sees || (unsigned)page >= (unsigned)a.c.n_page) return;
+    const bf16_t* v = (const bf16_t*)a.c.values + ((((long long)page * a.c.KVH + kvh) << a.c.shift) + (s & ((1 << a.c.shift) - 1))) * a.c.dh;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float e = __uint_as_float((unsigned)v[col(i)] << 16);
+      sum[i] += fabsf(e) < INFINITY ? 0.f : e;
+    }
+  };
+  for (int s = k0 + (threadIdx.x & 15); s < min(it.len, end); s += 16) add(s, true);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    for (int d = 1; d < 16; d <<= 1) sum[i] += __shfl_xor(sum[i], d);
+  for (int s = max(k0, it.len); s < end; ++s) {
+    const int j = s - it.len;
+    add(s, a.visible ? j < 64 * a.n_words && (a.visible[row * a.n_words + min(j >> 6, a.n_words - 1)] >> (j & 63) & 1) : j <= node);
+  }
+  if (l > 0.f && l < INFINITY) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = fabsf(sum[i]) < INFINITY ? x[i] : sum[i];
+  }
+}
+
 // The attention of one item by NW waves, each with all QB = 16 QT rows and every NW-th block of the item's keys; one pass with running maxima and sums.
 //   S^T = K Q^T: a lane holds the scores of one row (lane % 16).  bf16: row i of key tile t is key 8 (i / 4) + 4 t + i % 4, so that a lane's 8 scores are
 //     those of the keys 8 (lane / 16) .. + 7, the operand layout of P.  float32: the 4 keys 4 (lane / 16) + r, one for each of four products.
@@ -556,13 +590,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn(AttendArgs a, TreePlan
   if (w) return;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    if (!row_there[t]) continue;
     float x[4 * CPL];                              // columns 4 CPL lq .. of the row
     const float inv = it.parts > 1 ? 1.f : 1.f / l_all[t];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int i = 0; i < CPL; ++i) x[CPL * r + i] = l_all[t] == 0.f ? 0.f : O[t][i][r] * inv;
+    if constexpr (HALF) take_infinities(a, it, kvh, k0, end, at_q[t], node[t], l_all[t], [&](int i) { return 4 * CPL * lq + i; }, x);
+    if (!row_there[t]) continue;
     if (it.parts > 1) {
       const long long at = ((long long)it.sums * a.c.KVH + kvh) * QB + 16 * t + l16;
       float* dst = plan.o + at * DH + 4 * CPL * lq;
@@ -864,26 +899,25 @@ __global__ __launch_bounds__(NW * 64, 2) void k_tree_attn_shared(AttendArgs a, T
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last stages' loads still write to LDS)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const float l = quarter_sum(l_run[t]);
+    const float l = quarter_sum(l_run[t]), inv = it.parts > 1 ? 1.f : 1.f / l;
+    float y[4 * CT];                               // columns 16 x + 4 lq .. of the row
+#pragma unroll
+    for (int x = 0; x < CT; ++x)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[4 * x + r] = l == 0.f ? 0.f : O[t][x][r] * inv;
+    take_infinities(a, it, kvh, k0, end, at_q[t], node[t], l, [&](int i) { return 16 * (i >> 2) + 4 * lq + (i & 3); }, y);
     if (!row_there[t]) continue;
     const int i = (int)(16 * QT * w + 16 * t + l16);
     if (it.parts > 1) {
       const long long at = ((long long)it.sums * a.c.KVH + kvh) * QB + i;
 #pragma unroll
-      for (int x = 0; x < CT; ++x) {
-        const f32x4 o = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t][x];
-        *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(o[0], o[1], o[2], o[3]);
-      }
+      for (int x = 0; x < CT; ++x) *reinterpret_cast<float4*>(plan.o + at * DH + 16 * x + 4 * lq) = make_float4(y[4 * x], y[4 * x + 1], y[4 * x + 2], y[4 * x + 3]);
       if (lq == 0) *reinterpret_cast<float2*>(plan.ml + at * 2) = make_float2(m_run[t], l);
     } else {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
       const int g = (int)((r0 + 16 * t + l16) % G);
       bf16_t* dst = (bf16_t*)a.y + at_q[t] * a.ld_y + (kvh * G + g) * DH + 4 * lq;
 #pragma unroll
-      for (int x = 0; x < CT; ++x) {
-        const f32x4 o = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t][x] * inv;
-        *reinterpret_cast<uint2*>(dst + 16 * x) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
-      }
+      for (int x = 0; x < CT; ++x) *reinterpret_cast<uint2*>(dst + 16 * x) = make_uint2(pk_bf16(y[4 * x], y[4 * x + 1]), pk_bf16(y[4 * x + 2], y[4 * x + 3]));
     }
   }
 }

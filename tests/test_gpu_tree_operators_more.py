@@ -195,3 +195,47 @@ def test_logits_in_several_slices(dtype, rows, V, L):
     assert torch.equal(_ops().adjust_logits(wide[:, 5:V + 5], f, out=out[:, 3:V + 3], **dev), want)
     assert (out[:, :3] == 3).all() and (out[:, V + 3:] == 3).all()
     _check_logits(logits, first, {k: kw[k] if k in ("draft", "visible", "frequency", "mask", "mask_row") else None for k in kw}, half)
+
+
+# ------------------------------------------------------------------------------------- committed values that are not finite
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens, nodes, H, KVH, dh, page", ENDS)
+def test_committed_values_that_are_not_finite(dtype, lens, nodes, H, KVH, dh, page):
+    """Infinities of one sign give that infinity, of both signs or NaN give NaN, in their columns alone; as they do in nodes."""
+    b = Batch(sum(nodes) + dh, dtype, lens, nodes, H, KVH, dh, page)
+    vis = b.seen()
+    half = b.dtype == torch.bfloat16
+    want, bound, _ = M.attend(b.keys[0], b.values[0], b.table, b.lens, b.first, vis, b.q.reshape(b.T, H, dh), dh ** -0.5, half)
+    what = {3: float("inf"), 7: -float("inf"), 20: float("nan"), 41: None}
+    hit = {c: torch.zeros(b.T, dtype=torch.bool) for c in what}
+    for s, l in enumerate(lens):
+        for n, c in enumerate(what):
+            at = sorted({0, l // 2, l - 1, (17 * n) % l} if n != 1 else {l - 1})
+            for i, slot in enumerate(at):
+                p = M.slot_of(b.table.cpu().numpy(), b.keys.shape[1], page, s, slot)
+                b.values[0, p[0], :, p[1], c] = what[c] if what[c] is not None else (-1) ** i * float("inf")
+            hit[c][int(b.first[s]):int(b.first[s + 1])] = True
+        assert l > 1
+    got = b.cache.attend(0, b.q, b.table, b.lens, b.first, visible=vis).double().cpu().reshape(b.T, H, dh)
+    assert torch.equal(b.cache.attend(0, b.q, b.table, b.lens, b.first, visible=vis).double().cpu().reshape(b.T, H, dh).nan_to_num(9.0), got.nan_to_num(9.0))
+    for c in what:
+        y = got[hit[c], :, c]
+        good = bool(y.isnan().all() if c > 7 else (y == what[c]).all())
+        assert good, (c, y.isnan().float().mean(), (y == float("inf")).float().mean())
+    rest = [c for c in range(dh) if c not in what]
+    good = bool(((got - want).abs() <= bound)[..., rest].all())
+    assert good
+
+
+def test_committed_values_in_a_few_of_many_sequences():
+    """Sequences without infinities keep their bits."""
+    for H, nodes in ((4, 1), (16, 6), (16, 20)):
+        b = Batch(H + nodes, "bf16", [37 * i % 900 + 2 for i in range(40)], [nodes] * 40, H, 2, 64, 16)
+        want = b.cache.attend(0, b.q, b.table, b.lens, b.first)
+        rows = torch.zeros(b.T, dtype=torch.bool, device=DEV)
+        for s in (0, 7, 39):
+            p = M.slot_of(b.table.cpu().numpy(), b.keys.shape[1], 16, s, 1)
+            b.values[0, p[0], :, p[1]] = float("inf")
+            rows[nodes * s:nodes * (s + 1)] = True
+        got = b.cache.attend(0, b.q, b.table, b.lens, b.first)
+        assert torch.equal(got[~rows], want[~rows]) and (got[rows] == float("inf")).all()
