@@ -42,7 +42,7 @@ __device__ __forceinline__ void turn_pair(float& x, float& y, float2 cs) {
 
 // One token per workgroup (few tokens: its heads dealt out to up to 4), its angles shared by all heads.  A thread takes pairs of columns in units of two
 // pieces of N elements that turn together: its reads of a unit come before its writes, so that queries may be turned in place.  N = 8: rows are 16-byte
-// aligned and n_turned a multiple of 16; N = 1: any.  Bound by HBM: 4095 tokens of 32 heads of 128 columns in bf16, 201 MB in 42 us = 4.8 TB/s, what a large
+// aligned and n_turned a multiple of 16; N = 1: any.  Bound by HBM: 4091 tokens of 32 heads of 128 columns in bf16, 201 MB in 42 us = 4.8 TB/s, what a large
 // copy reaches (a pair at a time: 69 us).
 template <typename X, typename C, int N>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {

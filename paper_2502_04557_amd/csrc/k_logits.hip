@@ -37,7 +37,7 @@ __device__ __forceinline__ int row_sequence(const int* first, int n_seq, int n_r
 
 // A workgroup takes `slice` tokens of the vocabulary of `per` rows one after the other.  What the history says of those tokens is counted once for all of its
 // rows of one sequence; the tokens of a row's path are added for the row and taken out again.  Reads and writes 16 bytes a lane whatever the rows'
-// alignment; all but a few words are 0, and their logits go through as they are.  Bound by HBM: 448 rows of 128256 float32, 460 MB in 103 us = 4.5 TB/s, of the 4.7
+// alignment; all but a few words are 0, and their logits go through as they are.  Bound by HBM: 448 rows of 128256 float32, 460 MB in 101 us = 4.6 TB/s, of the 4.7
 // that a large copy reaches; counting 2000 tokens of history for every third row is 8 us of them.
 // MANY: past the caches (through them, 129 us), slices of up to MANY_SLICE tokens, all of a thread's pieces of a row on their way at once (6 in float32, 3 in bf16); else one
 // piece a thread, and the logits stay in L2 for who draws from them.
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256) void k_adjust_logits(sprinter_logits a, int sl
 }
 
 // Few rows: as many workgroups as the vocabulary has runs of 256 pieces, so that all of a row is on its way at once.  Many (from 8 MB on): slices of at most
-// 6144 tokens, all of one size (24 KB of words, six workgroups on a compute unit: 104 us; 4096 / 5120 / 7168 / 8192 in the same launch: 121 / 110 / 112 / 113, the last of
-// which leave a short slice at the end), and rows of a sequence share the count of its history, as long as 2048 workgroups are left.
+// 6144 tokens, all of one size (24 KB of words, six workgroups on a compute unit: 103 us a call; 4096 / 8192: 123 / 112, the latter leaves a short slice at the end),
+// and rows of a sequence share the count of its history, as long as 2048 workgroups are left.
 void launch_adjust_logits(const sprinter_logits& a, hipStream_t s) {
   const int run = a.dtype == SPRINTER_F32 ? 1024 : 2048;
   const bool many = (long long)((a.vocab + run - 1) / run) * a.n_rows > 2048;

@@ -165,6 +165,36 @@ def test_attend_many_sequences_of_several_heads(dtype, n, H, KVH, dh, most, long
     _check(b, b.seen())
 
 
+@pytest.mark.parametrize("n, H, nodes, longest", [(130, 4, 3, 5000), (40, 16, 20, 6000), (150, 16, 20, 900)])
+def test_attend_replayed_with_other_lengths(n, H, nodes, longest):
+    """A graph of a call whose items are listed before the launch, or counted in it: which sequences are split changes from replay to replay."""
+    g = np.random.default_rng(n)
+    b = Batch(n, "bf16", [longest] * 3 + [300] * (n - 3), [nodes] * n, H, 2, 64, 16)
+    out = torch.zeros_like(b.q)
+    most = b.lens.cpu().numpy()
+
+    def run():
+        b.cache.attend(0, b.q, b.table, b.lens, b.first, out=out)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for turn in range(5):
+        b.lens.copy_(_ints((most * g.random(n) ** turn).astype(int).tolist()))
+        b.q.copy_(b.normal(b.T, H * 64))
+        want = b.cache.attend(0, b.q, b.table, b.lens, b.first)
+        torch.cuda.synchronize()
+        out.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        _check(b)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_float32_in_the_mean(dtype):
     """Small batches of both kernels of few rows."""
