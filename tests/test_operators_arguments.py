@@ -145,3 +145,19 @@ def test_optional_tensors_whose_memory_was_freed_are_refused(no_device, lib):  #
             call()
     assert not no_device
     ops.block_norm(f(0, 8), f(0, 8), f(8), gate=f(0, 8))  # an empty one is a tensor
+
+
+def test_optional_views_whose_memory_was_freed_are_refused(no_device, lib):  # noqa: F811
+    """A view behind the storage's begin has an address without it."""
+    def freed(n):
+        t = torch.ones(2 * n)
+        v = t[n:]
+        t.untyped_storage().resize_(0)
+        return v
+
+    f = torch.ones
+    for call, name in ((lambda: ops.route(f(3, 8), 2, bias=freed(8)), "bias"), (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), offset=freed(8)), "offset"),
+                       (lambda: ops.block_norm(f(3, 8), f(3, 8), f(8), gate=freed(8)), "gate")):
+        with pytest.raises(ValueError, match=f"{name}: a tensor without memory"):
+            call()
+    assert not no_device
